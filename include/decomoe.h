@@ -58,11 +58,14 @@ typedef enum {
 } decomoe_status;
 
 /* Storage dtype of activations and weights. Accumulation is always fp32 (fp64
- * for the activated mass). */
-enum { DECOMOE_BF16 = 0, DECOMOE_F32 = 1 };
+ * for the activated mass). DECOMOE_E4M3 (8 bits, sign, 4 exponent and 3
+ * mantissa bits, no infinities) is taken only where a call names it. */
+enum { DECOMOE_BF16 = 0, DECOMOE_F32 = 1, DECOMOE_E4M3 = 2 };
 
 /* Gate/up interleave granule of the fused weight layout (rows of one block). */
 #define DECOMOE_GU_BLOCK 64
+/* Most requests of one call on a paged cache. */
+#define DECOMOE_MAX_REQUESTS 4096
 /* Largest expert pool and largest top-k any kernel here takes. */
 #define DECOMOE_MAX_E 256
 #define DECOMOE_MAX_TOPK 32
@@ -578,6 +581,121 @@ DECOMOE_API size_t decomoe_attention_workspace_bytes(int64_t n, int64_t C, int H
 DECOMOE_API int decomoe_attention(const void* q, int64_t n, const void* k_cache, const void* v_cache, int64_t C,
                                   int Hq, int Hkv, int D, float scale, void* out, void* ws, size_t ws_bytes,
                                   int32_t* status_dev, decomoe_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * A paged key-value cache: several requests of different lengths share one
+ * pool of pages (decoding on the text-only cache, Section 3.2 and Algorithm 2,
+ * last step, for a batch of requests). The pool of one layer is [num_pages,
+ * page_size, Hkv, D] for keys and the same for values; page_size is a power of
+ * two; page_stride (elements, >= page_size * Hkv * D) lies between pages, so
+ * that keys and values may be interleaved page by page. A slot is a row of the
+ * pool, page * page_size + offset (num_pages * page_size < 2^31; offsets in
+ * bytes are 64-bit). block_table [B, max_pages] int32 holds the page of rows
+ * [i * page_size, (i + 1) * page_size) of request b at [b, i]; entries that
+ * no row uses may hold anything. B <= DECOMOE_MAX_REQUESTS.
+ *
+ * decomoe_paged_plan: what a step needs to know about its rows, from the
+ * requests' lengths alone. cached [B]: rows that a request has in the cache;
+ * fresh [B]: rows that the step adds (0, 1, or a whole prompt). With have_b =
+ * ceil(cached_b / page_size) and need_b = ceil((cached_b + fresh_b) /
+ * page_size), request b takes need_b - have_b pages from the list free_pages
+ * [n_free], in request order from entry *free_head on (free_head NULL: 0):
+ *   block_table[b, have_b .. need_b) = those pages (other entries are kept);
+ *   seq_len[b] = cached_b + fresh_b;
+ *   row_start[b] = sum of fresh over the requests before b, row_start[B] all;
+ *   for row r = row_start[b] + i: positions[r] = cached_b + i and slot_map[r]
+ *   = the slot of that position. Rows from row_start[B] up to N get -1 in both.
+ *   *free_head_out = the next unused entry of the list (may be NULL).
+ * Pages are given out in a fixed order, so the same lengths give the same
+ * tables; a call repeated with the same inputs writes the same values. Whatever
+ * cannot be given is marked in status_dev as DECOMOE_ERR_BAD_INPUT: a negative
+ * length counts as 0; where the list runs out, the table gets -1; where the
+ * table is too narrow, the request ends at max_pages * page_size rows; a row
+ * without a page (or whose held page is negative) has slot -1; rows past N are
+ * left out. seq_len must not overlap cached or fresh, nor free_head_out free_head.
+ * positions may be NULL. One launch, no host synchronisation.
+ *
+ * decomoe_paged_append: the step's new rows into their slots, keys and values
+ * in one launch. k_new, v_new: [N, width] dtype (bf16 or f32), rows
+ * k_row_stride and v_row_stride elements apart (the rows of a fused projection
+ * can be read in place); k_pages, v_pages: the pools, width = Hkv * D. A slot
+ * of -1 is skipped; one outside the pool is skipped and marks
+ * DECOMOE_ERR_BAD_INPUT. Two rows of the same slot: either may remain. width
+ * and strides are multiples of 16 bytes, pointers 16-byte aligned.
+ *
+ * decomoe_paged_attention: one new token per request over its cache, which
+ * already holds the token's own row. q: [B, Hq, D] bf16, requests q_stride
+ * elements apart; out: [B, Hq, D] bf16, contiguous. Request b sees rows
+ * [0, seq_len[b]) but for [hide_begin[b], hide_begin[b] + hide_count[b]) (both
+ * arrays NULL: all rows): the visual block of a request after its exit, which
+ * thereby leaves the cache without a copy. Hidden rows are not read, and pages
+ * that hold nothing else may have been given back (any table entry). Query
+ * head h reads KV head h / (Hq / Hkv); out = softmax(scale q k^T) v with fp32
+ * scores, softmax and sums, weights rounded to bf16 for the value product,
+ * scale <= 0 meaning 1 / sqrt(D). A request that sees no row gets zeros (so do
+ * scores that are all minus infinity). Other keys and values that are not finite
+ * give what the formula gives, in their own request and KV head; rows past the
+ * length or hidden never reach a result.
+ * D is 64 or 128, Hq a multiple of Hkv, pointers and strides multiples of 16
+ * bytes. A length beyond max_pages * page_size is cut there, and a page outside
+ * the pool counts as hidden; both mark DECOMOE_ERR_BAD_INPUT.
+ * The visible rows of all requests are divided evenly over the SMs; a request
+ * cut by that leaves partial rows in the workspace, which a second small launch
+ * joins in key order. Deterministic: the same call gives the same bits, but the
+ * last bits of a row depend on the other requests of the call and on the number
+ * of SMs. ws: decomoe_paged_attention_workspace_bytes(...) bytes, 16-byte
+ * aligned, any content. No host synchronisation: lengths, tables and slots
+ * stay on the device, so a captured step can be replayed as they grow.
+ * ------------------------------------------------------------------------ */
+DECOMOE_API int decomoe_paged_plan(const int32_t* cached, const int32_t* fresh, int64_t B, int page_size,
+                                   const int32_t* free_pages, int64_t n_free, const int32_t* free_head,
+                                   int32_t* free_head_out, int32_t* block_table, int64_t max_pages,
+                                   int32_t* seq_len, int32_t* row_start, int32_t* slot_map, int32_t* positions,
+                                   int64_t N, int32_t* status_dev, decomoe_stream_t stream);
+DECOMOE_API int decomoe_paged_append(const void* k_new, int64_t k_row_stride, const void* v_new, int64_t v_row_stride,
+                                     int64_t N, int width, int dtype, const int32_t* slot_map, void* k_pages,
+                                     void* v_pages, int64_t num_pages, int page_size, int64_t page_stride,
+                                     int32_t* status_dev, decomoe_stream_t stream);
+DECOMOE_API size_t decomoe_paged_attention_workspace_bytes(int64_t B, int Hq, int Hkv, int D);
+DECOMOE_API int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t B, const void* k_pages,
+                                        const void* v_pages, int64_t num_pages, int page_size, int64_t page_stride,
+                                        const int32_t* block_table, int64_t max_pages, const int32_t* seq_len,
+                                        const int32_t* hide_begin, const int32_t* hide_count, int Hq, int Hkv, int D,
+                                        float scale, void* out, void* ws, size_t ws_bytes, int32_t* status_dev,
+                                        decomoe_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * The dense steps around the attention of a decode layer (base-model steps
+ * that the method leaves unchanged).
+ *
+ * decomoe_add_rmsnorm_q8: s = x + residual (residual NULL: s = x);
+ *   sum_out = s; v = s / sqrt(mean(s^2) + eps) * weight (weight NULL: 1);
+ *   y = v; and in 8 bits with one scale per row: a = max(max_j |v_j|, 2^-100),
+ *   y8 = e4m3(v * (448 / a)), y8_scale = a / 448, so that v ~ y8 * y8_scale.
+ * x, residual, sum_out, y: [T, d] dtype (bf16 or f32); weight: [d] dtype;
+ * y8: [T, d] bytes (e4m3); y8_scale: [T] fp32. sum_out, y and the pair y8,
+ * y8_scale may each be NULL (not wanted). fp32 math on the unrounded s, each
+ * output rounded once. sum_out may be residual or x, y may be x (not both x).
+ * Rows of a multiple of 16 bytes, 16-byte aligned pointers (y8: 8-byte).
+ *
+ * decomoe_w4_linear: out[t, n] = sum_k x[t, k] * w[n, k] for a matrix in 4
+ * bits with group scales: w[n, k] = (q[n, k] - 8) * w_scale[n, k / group],
+ * q in 0..15, two to a byte, even k in the low four bits: w [N, K / 2] bytes;
+ * w_scale: [N, K / group] bf16; group 32, 64 or 128, K a multiple of group.
+ * x: [T, K] rows x_stride elements apart, x_dtype DECOMOE_BF16 (x_scale NULL)
+ * or DECOMOE_E4M3 with x_scale [T] fp32, one factor per row (as
+ * decomoe_add_rmsnorm_q8 leaves them). out: [T, N] contiguous, out_dtype
+ * DECOMOE_BF16 or DECOMOE_F32. Products are exact, sums of a group and over the
+ * groups fp32, scales applied to whole group sums, one rounding at the end. For
+ * decode sizes (the weights are read once per 32 rows); any T >= 0 and N >= 1
+ * are right. x and w 16-byte aligned, x_stride a multiple of 16 bytes.
+ * ------------------------------------------------------------------------ */
+DECOMOE_API int decomoe_add_rmsnorm_q8(const void* x, const void* residual, const void* weight, int64_t T, int d,
+                                       float eps, int dtype, void* sum_out, void* y, void* y8, float* y8_scale,
+                                       decomoe_stream_t stream);
+DECOMOE_API int decomoe_w4_linear(const void* x, int x_dtype, int64_t x_stride, const float* x_scale, int64_t T, int K,
+                                  const void* w, const void* w_scale, int group, int64_t N, void* out, int out_dtype,
+                                  decomoe_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Bounded-wait status. Kernels that wait on device barriers give up after a

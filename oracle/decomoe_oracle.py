@@ -485,3 +485,80 @@ def attention(q, k_cache, v_cache, scale=None):
             w = softmax(s)
             out[i, h, :] = w @ v_cache[:last + 1, g, :]
     return out
+
+
+# ---------------------------------------------------------------------------
+# A decode step of several requests on a paged cache, and the dense steps around
+# its attention (base-model steps; the paper leaves them unchanged)
+# ---------------------------------------------------------------------------
+
+def paged_plan(cached, fresh, page_size, free_pages, free_head, table, N):
+    """Pages, slots and positions of a step's new rows, request by request.
+
+    Returns (table, seq_len, row_start, slot_map [N], positions [N], head, ok).
+    Pages come from free_pages[free_head:] in request order; -1 where the list
+    has run out. A request ends at the width of its table row; rows without a
+    page have slot -1, rows past the last one slot and position -1.
+    """
+    table = np.array(table, np.int64)
+    B, width = table.shape
+    cap = width * page_size
+    slots, positions = np.full(N, -1, np.int64), np.full(N, -1, np.int64)
+    seq_len, row_start = np.zeros(B, np.int64), np.zeros(B + 1, np.int64)
+    head, r, ok = int(free_head), 0, True
+    for b in range(B):
+        c, f = int(cached[b]), int(fresh[b])
+        ok &= c >= 0 and f >= 0 and c <= cap
+        c, f = min(max(c, 0), cap), max(f, 0)
+        ok &= c + f <= cap
+        row_start[b] = r
+        seq_len[b] = min(c + f, cap)
+        for e in range(-(-c // page_size), -(-seq_len[b] // page_size)):
+            there = 0 <= head < len(free_pages)
+            table[b, e] = free_pages[head] if there else -1
+            head, ok = head + 1, ok and there
+        for i in range(f):
+            if r < N and c + i < cap:
+                page = table[b, (c + i) // page_size]
+                positions[r] = c + i
+                slots[r] = page * page_size + (c + i) % page_size if page >= 0 else -1
+            ok &= r < N and slots[r] >= 0
+            r += 1
+    row_start[B] = r
+    return table, seq_len, row_start, slots, positions, min(head, max(len(free_pages), int(free_head))), bool(ok)
+
+
+def paged_attention(q, k_pages, v_pages, table, seq_len, hide_begin=None, hide_count=None, scale=None):
+    """One new token per request over its visible rows: q [B, Hq, D], pools
+    [P, page_size, Hkv, D]. A request that sees nothing gets zeros."""
+    q = np.asarray(q, F64)
+    B, Hq, D = q.shape
+    ps, Hkv = k_pages.shape[1], k_pages.shape[2]
+    out = np.zeros((B, Hq, D), F64)
+    for b in range(B):
+        h0, h1 = (0, 0) if hide_begin is None else (int(hide_begin[b]), int(hide_begin[b]) + max(int(hide_count[b]), 0))
+        rows = [j for j in range(int(seq_len[b])) if not h0 <= j < h1]
+        if not rows:
+            continue
+        k = np.stack([np.asarray(k_pages[table[b, j // ps], j % ps], F64) for j in rows])
+        v = np.stack([np.asarray(v_pages[table[b, j // ps], j % ps], F64) for j in rows])
+        # the token's own row is the last one of its cache: it sees every row
+        out[b] = attention(q[b:b + 1], k, v, scale)[0]
+    return out
+
+
+def e4m3_values():
+    """The finite values of the 8-bit format (4 exponent bits, bias 7, 3
+    mantissa bits), ascending."""
+    pos = [(m / 8.0) * 2.0 ** -6 if e == 0 else (1 + m / 8.0) * 2.0 ** (e - 7)
+           for e in range(16) for m in range(8) if not (e == 15 and m == 7)]
+    return np.array(sorted({-p for p in pos} | set(pos)), F64)
+
+
+def w4_dequant(w, w_scale):
+    """4-bit weights [N, K / 2] bytes (even k in the low four bits) with group
+    scales [N, K / group]: (q - 8) * scale as float64 [N, K]."""
+    w = np.asarray(w).astype(np.int64)
+    q = np.stack([w % 16, w // 16], axis=-1).reshape(w.shape[0], -1) - 8
+    s = np.asarray(w_scale, F64)
+    return q * np.repeat(s, q.shape[1] // s.shape[1], axis=1)
