@@ -7,76 +7,548 @@
 
 namespace decomoe {
 
+// The visible keys of every (request, KV head) pair are cut into tiles (16 keys
+// of 128 features, 32 of 64), the tiles of all pairs are numbered in order, and
+// every warp of the launch takes the same number of consecutive tiles, one block
+// of eight warps per SM, whatever the lengths are. A warp streams its tiles
+// through a ring of its own (16-byte asynchronous copies, row by row through the
+// block table, three tiles of 8 KB) and meets no other warp until it has read its
+// last tile. Where a pair's tiles end inside a warp's share the result goes
+// straight out; what a warp holds of a pair that goes on in another warp is joined
+// in key order, first among the warps of the block, then, by a second small
+// launch, among the blocks. No counters, and the result does not depend on timing.
+//
+// Both products run transposed on the tensor cores (mma.m16n8k16, bf16 in, fp32
+// accumulate): S^T = K Q^T with 16 keys by 8 queries, O^T += V^T P^T with 16
+// features by 8 queries, so that the 8 query heads of a KV head fill a tile (16
+// rows by 8 keys would leave half of each product empty). The accumulator of the
+// first becomes the operand of the second by two 8x8 transposes (movmatrix), and
+// a query's maximum, sum and outputs all lie in the same lanes.
+constexpr int PGA_WARPS = 8;
+constexpr int PGA_THREADS = 32 * PGA_WARPS;
+constexpr int PGA_STAGES = 3;
+constexpr int PGA_STAGE = 8192;  // bytes of one tile: keys, then values
+
+template <int D>
+struct PgaTile {
+  static constexpr int KEYS = PGA_STAGE / (4 * D);  // 16 or 32
+  static constexpr int VECS = D / 8;                // 16-byte pieces of a row
+  static constexpr int ROW = D + 4;                 // floats of a partial row: outputs, m, l (bank-conflict-free stores)
+};
+
 struct PagedArgs {
   const __nv_bfloat16* q;
   const __nv_bfloat16 *k, *v;
   const int32_t *table, *len, *hide_begin, *hide_count;
   __nv_bfloat16* out;
+  float* early;  // [warps][rows][ROW] pieces that end inside a warp's share
+  float* part;   // [blocks][2][rows][ROW] joined pieces of a block: of a pair begun before it, of one that goes on after it
+  int4* info;    // [blocks] the pair that begins in a block and ends in a later one: (valid, request, head tile, last block)
   int32_t* status;
   int64_t q_stride, page_stride, num_pages, max_pages;
   int B, hq, hkv, shift;
-  float sl2;  // scale * log2(e)
+  int qt, hv;    // query tiles per KV head, (KV head, query tile) pairs
+  float sl2;     // scale * log2(e)
 };
 
-// One block per (request, query head), a warp every eighth visible key.
-template <int D>
-__global__ void __launch_bounds__(256) k_paged_attention(PagedArgs a) {
-  constexpr int PER = D / 32;
-  __shared__ float sm[8], sl[8], so[8][D];
-  pdl_enter();
-  const int b = blockIdx.x, h = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t cap = a.max_pages << a.shift;
-  int64_t n = a.len[b];
-  if (threadIdx.x == 0 && (n < 0 || n > cap)) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
-  n = min(max(n, int64_t{0}), cap);
-  int64_t h0 = n, hc = 0;
+// What a request shows: its visible rows, and where its hidden block lies.
+struct PgaReq {
+  int seen, h0, hc;
+};
+__device__ __forceinline__ PgaReq pga_request(const PagedArgs& a, int b, bool* bad) {
+  const int cap = static_cast<int>(a.max_pages << a.shift);
+  int n = a.len[b];
+  *bad |= n < 0 || n > cap;
+  n = min(max(n, 0), cap);
+  PgaReq r;
+  r.h0 = n;
+  r.hc = 0;
   if (a.hide_begin != nullptr) {
-    h0 = min(max(static_cast<int64_t>(a.hide_begin[b]), int64_t{0}), n);
-    hc = min(max(static_cast<int64_t>(a.hide_count[b]), int64_t{0}), n - h0);
+    r.h0 = min(max(a.hide_begin[b], 0), n);
+    r.hc = min(max(a.hide_count[b], 0), n - r.h0);
   }
-  const int64_t seen = n - hc;
-  const int g = h / (a.hq / a.hkv);
-  float q[PER], o[PER] = {};
-  for (int i = 0; i < PER; ++i) q[i] = __bfloat162float(a.q[b * a.q_stride + h * D + lane * PER + i]);
-  float m = -INFINITY, l = 0.f;
-  for (int64_t j = warp; j < seen; j += 8) {
-    const int64_t p = j < h0 ? j : j + hc;
-    const int64_t page = a.table[b * a.max_pages + (p >> a.shift)];
-    if (page < 0 || page >= a.num_pages) {
-      if (lane == 0) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
-      continue;
+  r.seen = n - r.hc;
+  return r;
+}
+
+// The first tile of warp i's share, of `total` tiles over `workers` warps: equal
+// shares, or one tile each where there are fewer tiles than warps.
+__device__ __forceinline__ int pga_share(int64_t total, int workers, int i) {
+  return static_cast<int>(total >= workers ? i * total / workers : min(static_cast<int64_t>(i), total));
+}
+// The warp whose share holds tile t.
+__device__ __forceinline__ int pga_holder(int64_t total, int workers, int t) {
+  return static_cast<int>(total >= workers ? ((static_cast<int64_t>(t) + 1) * workers - 1) / total : t);
+}
+
+__device__ __forceinline__ float pga_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ void pga_ldsm(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ void pga_ldsm_t(uint32_t addr, uint32_t (&r)[4]) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+               : "r"(addr));
+}
+__device__ __forceinline__ uint32_t pga_transpose(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+__device__ __forceinline__ void pga_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// 16 bytes into shared memory, zeros where !ok (src is then not read).
+__device__ __forceinline__ void pga_copy(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(ok ? 16 : 0) : "memory");
+}
+
+// A position in the numbered tiles: tile t of pair (request b, head tile h).
+template <int D>
+struct PgaWalk {
+  int b, h, t, tiles;
+  PgaReq r;
+  __device__ __forceinline__ void enter(const PagedArgs& a) {
+    bool bad = false;  // marked by the launch's first look at the lengths
+    r = pga_request(a, b, &bad);
+    tiles = (r.seen + PgaTile<D>::KEYS - 1) / PgaTile<D>::KEYS;
+  }
+  __device__ __forceinline__ void seek(const PagedArgs& a, const int* pre, int tile) {
+    int lo = 0, hi = a.B;  // the last request with pre * hv <= tile: it is not empty
+    const int at = tile / a.hv;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (pre[mid] <= at) lo = mid;
+      else hi = mid;
     }
-    const int64_t at = page * a.page_stride +
-                       ((p & ((int64_t{1} << a.shift) - 1)) * a.hkv + g) * D + lane * PER;
-    float s = 0.f;
-    for (int i = 0; i < PER; ++i) s = fmaf(q[i], __bfloat162float(a.k[at + i]), s);
-    for (int off = 16; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-    s *= a.sl2;
-    const float mn = fmaxf(m, s), ref = mn == -INFINITY ? 0.f : mn;
-    const float f = exp2f(m - ref), w = exp2f(s - ref);
-    l = l * f + w;
-    for (int i = 0; i < PER; ++i) o[i] = o[i] * f + w * __bfloat162float(a.v[at + i]);
-    m = mn;
+    b = lo;
+    enter(a);
+    const int in = tile - pre[b] * a.hv;
+    h = in / tiles;
+    t = in - h * tiles;
   }
-  if (lane == 0) {
-    sm[warp] = m;
-    sl[warp] = l;
+  // To the next tile; in the last pair it stays past the end (nobody looks).
+  __device__ __forceinline__ void next(const PagedArgs& a, const int* pre) {
+    if (++t < tiles) return;
+    t = 0;
+    if (++h < a.hv) return;
+    h = 0;
+    do ++b;
+    while (b < a.B && pre[b + 1] == pre[b]);
+    if (b < a.B) enter(a);
   }
-  for (int i = 0; i < PER; ++i) so[warp][lane * PER + i] = o[i];
+};
+
+template <int D, int NT>
+__global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a) {
+  using T = PgaTile<D>;
+  constexpr int KS = D / 16;     // 16-feature steps of the scores, and 16-feature tiles of the outputs
+  constexpr int SUB = T::KEYS / 16;
+  constexpr int ROWS = 8 * NT;
+  extern __shared__ __align__(1024) uint8_t pga_smem[];
+  __shared__ int scan_w[PGA_WARPS];
+  __shared__ uint32_t seen_mask[PGA_WARPS][PGA_STAGES];
+  __shared__ int3 meta[PGA_WARPS];  // last piece goes on (1: begun in the share, 2: before it), its request and head tile
+  int* pre = reinterpret_cast<int*>(pga_smem + PGA_WARPS * PGA_STAGES * PGA_STAGE);  // [B + 1] tiles per head before a request
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_enter();
+
+  // ---- tiles of every request, added up
+  {
+    const int per = (a.B + PGA_THREADS - 1) / PGA_THREADS;
+    const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
+    bool bad = false;
+    int sum = 0;
+    for (int b = b0; b < b1; ++b) {
+      const int n = (pga_request(a, b, &bad).seen + T::KEYS - 1) / T::KEYS;
+      pre[b + 1] = n;
+      sum += n;
+    }
+    if (bad && blockIdx.x == 0) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
+    int inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u = __shfl_up_sync(0xffffffffu, inc, o);
+      if (lane >= o) inc += u;
+    }
+    if (lane == 31) scan_w[warp] = inc;
+    __syncthreads();
+    int at = inc - sum;
+#pragma unroll
+    for (int w = 0; w < PGA_WARPS; ++w)
+      if (w < warp) at += scan_w[w];
+    for (int b = b0; b < b1; ++b) {
+      at += pre[b + 1];
+      pre[b + 1] = at;
+    }
+    if (tid == 0) pre[0] = 0;
+    __syncthreads();
+  }
+  // requests that see nothing
+  for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+    if (pre[b] == pre[b + 1]) {
+      uint4* o = reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(b) * a.hq * D);
+      for (int i = tid; i < a.hq * D / 8; i += PGA_THREADS) o[i] = make_uint4(0, 0, 0, 0);
+    }
+  const int64_t total = static_cast<int64_t>(pre[a.B]) * a.hv;
+  const int workers = gridDim.x * PGA_WARPS, me = blockIdx.x * PGA_WARPS + warp;
+  const int r0 = pga_share(total, workers, me), r1 = pga_share(total, workers, me + 1);
+  const int gs = a.hq / a.hkv;
+
+  uint8_t* ring = pga_smem + warp * PGA_STAGES * PGA_STAGE;
+  const uint32_t ring_s = smem_u32(ring);
+  float* mine = reinterpret_cast<float*>(ring);  // the last piece, once the ring is drained
+  if (lane == 0) meta[warp] = make_int3(0, 0, 0);
+  float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * ROWS * T::ROW;
+
+  if (r0 < r1) {
+    // ---- lookup, copy and use, each at its own tile
+    PgaWalk<D> look, use;
+    look.seek(a, pre, r0);
+    use = look;
+    const int64_t row_elems = static_cast<int64_t>(a.hkv) * D;
+    const int in_page = (1 << a.shift) - 1;
+    int page = -1, off = 0, head = 0;
+    bool want = false;
+    auto lookup = [&]() {  // the page of this lane's key
+      const int j = look.t * T::KEYS + lane;
+      want = lane < T::KEYS && j < look.r.seen;
+      const int p = j < look.r.h0 ? j : j + look.r.hc;
+      off = p & in_page;
+      head = look.h / a.qt;
+      if (want) page = a.table[look.b * a.max_pages + (p >> a.shift)];
+    };
+    auto issue = [&](int slot) {
+      const bool there = want && page >= 0 && page < a.num_pages;
+      if (want && !there) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
+      const uint32_t mask = __ballot_sync(0xffffffffu, there);
+      if (lane == 0) seen_mask[warp][slot] = mask;
+      const int64_t base = there ? page * a.page_stride + off * row_elems + static_cast<int64_t>(head) * D : -1;
+      constexpr int PER = 32 / T::VECS;  // rows per copy instruction
+      const int c = lane % T::VECS;
+      const uint32_t stage = ring_s + slot * PGA_STAGE;
+#pragma unroll
+      for (int i = 0; i < T::KEYS / PER; ++i) {
+        const int row = i * PER + lane / T::VECS;
+        const int64_t at = __shfl_sync(0xffffffffu, base, row);
+        const bool ok = at >= 0;
+        const int64_t e = ok ? at + c * 8 : 0;
+        const uint32_t dst = stage + row * (2 * D) + ((c ^ (row & 7)) << 4);
+        pga_copy(dst, a.k + e, ok);
+        pga_copy(dst + PGA_STAGE / 2, a.v + e, ok);
+      }
+    };
+    const int n = r1 - r0;
+    lookup();
+#pragma unroll
+    for (int s = 0; s < PGA_STAGES - 1; ++s) {
+      if (s < n) {
+        issue(s);
+        if (s + 1 < n) {
+          look.next(a, pre);
+          lookup();
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+
+    uint32_t qf[NT][KS][2];
+    float o[KS][NT][4], m[NT][2], l[NT][2];
+    auto begin_piece = [&]() {
+      const int g = use.h / a.qt, q0 = (use.h - g * a.qt) * ROWS;
+      const __nv_bfloat16* q = a.q + use.b * a.q_stride + static_cast<int64_t>(g) * gs * D;
+#pragma unroll
+      for (int x = 0; x < NT; ++x) {
+        const int r = q0 + x * 8 + (lane >> 2);
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            qf[x][s][i] = r < gs ? *reinterpret_cast<const uint32_t*>(q + static_cast<int64_t>(r) * D + s * 16 +
+                                                                      i * 8 + 2 * (lane & 3))
+                                 : 0u;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          m[x][i] = -INFINITY;
+          l[x][i] = 0.f;
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[s][x][i] = 0.f;
+      }
+    };
+    // a finished piece as partial rows
+    auto keep_piece = [&](float* dst) {
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float* row = dst + (x * 8 + 2 * (lane & 3) + i) * T::ROW;
+#pragma unroll
+          for (int s = 0; s < KS; ++s) {
+            row[s * 16 + (lane >> 2)] = o[s][x][i];
+            row[s * 16 + 8 + (lane >> 2)] = o[s][x][i + 2];
+          }
+          if (lane < 4) {
+            row[D] = m[x][i];
+            row[D + 1] = l[x][i];
+          }
+        }
+    };
+    begin_piece();
+    bool began = use.t > 0;  // the piece's pair began in an earlier share
+    int slot = 0;
+    for (int i = 0; i < n; ++i) {
+      if (i + PGA_STAGES - 1 < n) {
+        issue(slot == 0 ? PGA_STAGES - 1 : slot - 1);
+        if (i + PGA_STAGES < n) {
+          look.next(a, pre);
+          lookup();
+        }
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      asm volatile("cp.async.wait_group %0;" ::"n"(PGA_STAGES - 1) : "memory");
+      __syncwarp();
+      const uint32_t ks = ring_s + slot * PGA_STAGE, vs = ks + PGA_STAGE / 2;
+      const uint32_t mask = seen_mask[warp][slot];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        float sc[NT][4] = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const int row = u * 16 + (lane & 15), c = 2 * s + (lane >> 4);
+          uint32_t f[4];
+          pga_ldsm(ks + row * (2 * D) + ((c ^ (row & 7)) << 4), f);
+#pragma unroll
+          for (int x = 0; x < NT; ++x) pga_mma(sc[x], f, qf[x][s][0], qf[x][s][1]);
+        }
+        const bool lo = (mask >> (u * 16 + (lane >> 2))) & 1u, hi = (mask >> (u * 16 + 8 + (lane >> 2))) & 1u;
+        uint32_t p[NT][2];
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+          float mx[2];
+#pragma unroll
+          for (int i2 = 0; i2 < 2; ++i2) {
+            sc[x][i2] = lo ? sc[x][i2] * a.sl2 : -INFINITY;
+            sc[x][i2 + 2] = hi ? sc[x][i2 + 2] * a.sl2 : -INFINITY;
+            mx[i2] = fmaxf(sc[x][i2], sc[x][i2 + 2]);
+          }
+#pragma unroll
+          for (int w = 4; w < 32; w <<= 1) {
+            mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], w));
+            mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], w));
+          }
+          if (__any_sync(0xffffffffu, mx[0] > m[x][0] || mx[1] > m[x][1])) {
+#pragma unroll
+            for (int i2 = 0; i2 < 2; ++i2) {
+              const float to = fmaxf(m[x][i2], mx[i2]);
+              // nothing seen so far, and nothing here: any factor does
+              const float f = to == -INFINITY ? 1.f : pga_ex2(m[x][i2] - to);
+              m[x][i2] = to;
+              l[x][i2] *= f;
+#pragma unroll
+              for (int s = 0; s < KS; ++s) {
+                o[s][x][i2] *= f;
+                o[s][x][i2 + 2] *= f;
+              }
+            }
+          }
+          float w[4];
+#pragma unroll
+          for (int i2 = 0; i2 < 4; ++i2) {
+            const float ref = m[x][i2 & 1] == -INFINITY ? 0.f : m[x][i2 & 1];
+            w[i2] = pga_ex2(sc[x][i2] - ref);
+          }
+          l[x][0] += w[0] + w[2];
+          l[x][1] += w[1] + w[3];
+          p[x][0] = pga_transpose(pack_bf16x2(w[0], w[1]));
+          p[x][1] = pga_transpose(pack_bf16x2(w[2], w[3]));
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const int row = u * 16 + ((lane >> 4) << 3) + (lane & 7), c = 2 * s + ((lane >> 3) & 1);
+          uint32_t f[4];
+          pga_ldsm_t(vs + row * (2 * D) + ((c ^ (row & 7)) << 4), f);
+#pragma unroll
+          for (int x = 0; x < NT; ++x) pga_mma(o[s][x], f, p[x][0], p[x][1]);
+        }
+      }
+      __syncwarp();
+      slot = slot + 1 == PGA_STAGES ? 0 : slot + 1;
+      const bool ends = use.t + 1 == use.tiles;
+      if (ends || i + 1 == n) {
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+#pragma unroll
+          for (int i2 = 0; i2 < 2; ++i2)
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) l[x][i2] += __shfl_xor_sync(0xffffffffu, l[x][i2], w);
+        if (!ends) {  // goes on in the next share; the ring is empty
+          keep_piece(mine);
+          if (lane == 0) meta[warp] = make_int3(began ? 2 : 1, use.b, use.h);
+        } else if (began) {
+          // begun before the block: it is all that the block holds of its pair
+          keep_piece(warp == 0 ? part : a.early + static_cast<int64_t>(me) * ROWS * T::ROW);
+        } else {
+          const int g = use.h / a.qt, q0 = (use.h - g * a.qt) * ROWS;
+#pragma unroll
+          for (int x = 0; x < NT; ++x)
+#pragma unroll
+            for (int i2 = 0; i2 < 2; ++i2) {
+              const int r = q0 + x * 8 + 2 * (lane & 3) + i2;
+              if (r < gs) {
+                const float f = l[x][i2] != 0.f ? 1.f / l[x][i2] : 0.f;
+                __nv_bfloat16* dst = a.out + (static_cast<int64_t>(use.b) * a.hq + g * gs + r) * D + (lane >> 2);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) {
+                  dst[s * 16] = __float2bfloat16_rn(o[s][x][i2] * f);
+                  dst[s * 16 + 8] = __float2bfloat16_rn(o[s][x][i2 + 2] * f);
+                }
+              }
+            }
+        }
+        if (i + 1 < n) {
+          use.next(a, pre);
+          began = false;
+          begin_piece();
+        }
+      } else {
+        ++use.t;
+      }
+    }
+  }
   __syncthreads();
-  for (int c = threadIdx.x; c < D; c += blockDim.x) {
-    float mm = -INFINITY;
-    for (int w = 0; w < 8; ++w) mm = fmaxf(mm, sm[w]);
-    const float ref = mm == -INFINITY ? 0.f : mm;
-    float ll = 0.f, oo = 0.f;
-    for (int w = 0; w < 8; ++w) {
-      const float f = exp2f(sm[w] - ref);
-      ll += sl[w] * f;
-      oo += so[w][c] * f;
+
+  // ---- the block's pieces joined in key order, a warp per row: the last piece of a
+  // warp, the whole shares of the next ones, and the first piece of the one in which
+  // the pair ends. What began before the block or goes on after it leaves joined.
+  int4 info = make_int4(0, 0, 0, 0);
+  for (int w0 = 0; w0 < PGA_WARPS; ++w0) {
+    const int3 first = meta[w0];
+    if (first.x == 0 || (first.x == 2 && w0 > 0)) continue;
+    int w1 = w0 + 1;
+    while (w1 < PGA_WARPS && meta[w1].x == 2) ++w1;
+    const bool open_begin = first.x == 2, open_end = w1 == PGA_WARPS;
+    const int b = first.y, h = first.z, g = h / a.qt;
+    if (open_end && !open_begin) info = make_int4(1, b, h, 0);
+    for (int r = warp; r < ROWS; r += PGA_WARPS) {
+      const int q = (h - g * a.qt) * ROWS + r;
+      if (q >= gs) continue;
+      auto piece = [&](int i) -> const float* {
+        const int w = w0 + i;
+        return (w == w1 ? a.early + static_cast<int64_t>(blockIdx.x * PGA_WARPS + w) * ROWS * T::ROW
+                        : reinterpret_cast<const float*>(pga_smem + w * PGA_STAGES * PGA_STAGE)) +
+               r * T::ROW;
+      };
+      constexpr int C = D / 32;
+      const int n = (open_end ? w1 : w1 + 1) - w0;
+      float m = -INFINITY;
+      for (int i = 0; i < n; ++i) m = fmaxf(m, piece(i)[D]);
+      const float ref = m == -INFINITY ? 0.f : m;
+      float l = 0.f, o[C] = {};
+      for (int i = 0; i < n; ++i) {
+        const float* p = piece(i);
+        const float f = pga_ex2(p[D] - ref);
+        l = fmaf(p[D + 1], f, l);
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = fmaf(p[lane * C + c], f, o[c]);
+      }
+      if (open_begin || open_end) {
+        float* dst = part + ((open_begin ? 0 : ROWS) + r) * T::ROW;
+#pragma unroll
+        for (int c = 0; c < C; ++c) dst[lane * C + c] = o[c];
+        if (lane == 0) {
+          dst[D] = m;
+          dst[D + 1] = l;
+        }
+      } else {
+        const float f = l != 0.f ? 1.f / l : 0.f;
+        uint32_t* dst =
+            reinterpret_cast<uint32_t*>(a.out + (static_cast<int64_t>(b) * a.hq + g * gs + q) * D + lane * C);
+#pragma unroll
+        for (int c = 0; c < C; c += 2) dst[c / 2] = pack_bf16x2(o[c] * f, o[c + 1] * f);
+      }
     }
-    a.out[(static_cast<int64_t>(b) * a.hq + h) * D + c] = __float2bfloat16_rn(ll != 0.f ? oo / ll : 0.f);
+  }
+  if (tid == 0) {
+    if (info.x != 0) {
+      const int tiles = pre[info.y + 1] - pre[info.y];
+      const int last = pre[info.y] * a.hv + (info.z + 1) * tiles - 1;
+      info.w = pga_holder(total, workers, last) / PGA_WARPS;
+    }
+    a.info[blockIdx.x] = info;
   }
 }
+
+// Pairs that end in a later block than they begin in: block k joins the pair that
+// begins in block k of the launch before. A row's pieces are shared by several
+// warps, each with its loads in flight together, whose sums are then added in order.
+constexpr int PGM_WARPS = 32;
+template <int D, int NT>
+__global__ void __launch_bounds__(32 * PGM_WARPS) k_paged_join(PagedArgs a) {
+  using T = PgaTile<D>;
+  constexpr int ROWS = 8 * NT, PER = PGM_WARPS / ROWS, C = D / 32;
+  __shared__ float so[PGM_WARPS][D + 2];
+  pdl_enter();
+  const int4 info = a.info[blockIdx.x];
+  if (info.x == 0) return;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int r = warp / PER, s = warp % PER;
+  const int gs = a.hq / a.hkv, g = info.z / a.qt, q = (info.z - g * a.qt) * ROWS + r;
+  const int n = info.w - static_cast<int>(blockIdx.x) + 1;
+  const int i0 = s * n / PER, i1 = (s + 1) * n / PER;
+  auto piece = [&](int i) {
+    return a.part + ((static_cast<int64_t>(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + r) * T::ROW;
+  };
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += 32) m = fmaxf(m, piece(i)[D]);
+#pragma unroll
+  for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f, o[C] = {};
+#pragma unroll 8
+  for (int i = i0; i < i1; ++i) {
+    const float* p = piece(i);
+    const float f = pga_ex2(p[D] - ref);
+    l = fmaf(p[D + 1], f, l);
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = fmaf(p[lane * C + c], f, o[c]);
+  }
+#pragma unroll
+  for (int c = 0; c < C; ++c) so[warp][lane * C + c] = o[c];
+  if (lane == 0) so[warp][D] = l;
+  __syncthreads();
+  if (s == 0 && q < gs) {
+    l = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) o[c] = 0.f;
+#pragma unroll
+    for (int w = 0; w < PER; ++w) {
+      l += so[warp + w][D];
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] += so[warp + w][lane * C + c];
+    }
+    const float f = l != 0.f ? 1.f / l : 0.f;
+    uint32_t* dst =
+        reinterpret_cast<uint32_t*>(a.out + (static_cast<int64_t>(info.y) * a.hq + g * gs + q) * D + lane * C);
+#pragma unroll
+    for (int c = 0; c < C; c += 2) dst[c / 2] = pack_bf16x2(o[c] * f, o[c + 1] * f);
+  }
+}
+
+// Query rows of a warp's tile: 8 where a KV head has at most 8 query heads, else 16
+// (a KV head of more than 16 is read once for every 16).
+static int pga_rows(int Hq, int Hkv) { return Hq / Hkv <= 8 ? 8 : 16; }
 
 }  // namespace decomoe
 
@@ -86,7 +558,9 @@ extern "C" {
 
 size_t decomoe_paged_attention_workspace_bytes(int64_t B, int Hq, int Hkv, int D) {
   if (B <= 0 || Hkv <= 0 || Hq < Hkv || D <= 0) return 0;
-  return 256;
+  // the pieces of every warp and of every block, one block per SM
+  const size_t rows = static_cast<size_t>(pga_rows(Hq, Hkv)) * (D + 4) * sizeof(float);
+  return static_cast<size_t>(sm_count()) * ((PGA_WARPS + 2) * rows + sizeof(int4));
 }
 
 int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t B, const void* k_pages, const void* v_pages,
@@ -140,10 +614,32 @@ int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t B, const vo
   a.hq = Hq;
   a.hkv = Hkv;
   a.shift = __builtin_ctz(static_cast<unsigned>(page_size));
+  const int rows = pga_rows(Hq, Hkv);
+  a.qt = (Hq / Hkv + rows - 1) / rows;
+  a.hv = Hkv * a.qt;
   a.sl2 = (scale > 0.f ? scale : 1.f / sqrtf(static_cast<float>(D))) * 1.4426950408889634f;
-  DM_CUDA_CHECK(launch_pdl(D == 128 ? k_paged_attention<128> : k_paged_attention<64>,
-                           dim3(static_cast<unsigned>(B), static_cast<unsigned>(Hq)), dim3(256), 0,
-                           reinterpret_cast<cudaStream_t>(stream), a));
+  const int keys = D == 128 ? PgaTile<128>::KEYS : PgaTile<64>::KEYS;
+  const int64_t most = B * ((max_pages * page_size + keys - 1) / keys) * a.hv;  // tiles, at most
+  DM_ARG_CHECK(most <= INT_MAX, "paged_attention: B * max_pages * page_size * heads is too large");
+  const int grid = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(sm_count(), (most + PGA_WARPS - 1) / PGA_WARPS)));
+  const size_t piece = static_cast<size_t>(rows) * (D + 4);
+  a.early = static_cast<float*>(ws);
+  a.part = a.early + static_cast<size_t>(grid) * PGA_WARPS * piece;
+  a.info = reinterpret_cast<int4*>(a.part + static_cast<size_t>(grid) * 2 * piece);
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const size_t smem = static_cast<size_t>(PGA_WARPS) * PGA_STAGES * PGA_STAGE + (static_cast<size_t>(B) + 1) * sizeof(int);
+  auto go = [&](auto main, auto join) -> int {
+    DM_CUDA_CHECK(cudaFuncSetAttribute(main, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    DM_CUDA_CHECK(launch_pdl(main, dim3(grid), dim3(PGA_THREADS), smem, s, a));
+    DM_CUDA_CHECK(launch_pdl(join, dim3(grid), dim3(32 * PGM_WARPS), 0, s, a));
+    return DECOMOE_OK;
+  };
+  if (D == 128)
+    DM_RET(rows == 8 ? go(k_paged_attention<128, 1>, k_paged_join<128, 1>)
+                     : go(k_paged_attention<128, 2>, k_paged_join<128, 2>));
+  else
+    DM_RET(rows == 8 ? go(k_paged_attention<64, 1>, k_paged_join<64, 1>)
+                     : go(k_paged_attention<64, 2>, k_paged_join<64, 2>));
   return DECOMOE_OK;
 }
 
