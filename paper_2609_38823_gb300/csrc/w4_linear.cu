@@ -6,20 +6,21 @@
 // The weights are read once and bound the call (half a byte per product of up to
 // 32 rows), so what matters is few instructions per weight and many bytes in
 // flight. Products run on the tensor cores (mma.m16n8k16, fp32 accumulate) with
-// 16 columns n as the rows of the product and 8 rows t as its columns. A weight
-// becomes an operand without a conversion: its four bits are put into the mantissa
-// of a 16-bit float of value 16 (bits 3 to 6 in bf16, 6 to 9 in fp16), which
-// makes it the exact number 16 + q, one shift and one three-input logic operation
-// for two weights. The offset of 24 leaves with 24 sum x, which the tensor
-// cores add up too, as the product of the same rows with ones; the difference is
-// at most six times what it is taken from, in fp32. Rows in bf16 take bf16
-// products, rows in e4m3 fp16 ones (an e4m3 value is exact in fp16), so that every
-// product is exact.
+// 16 columns n as the rows of the product and 8 rows t as its columns; rows in bf16
+// take bf16 products, rows in e4m3 fp16 ones (every e4m3 value is exact there), so
+// that every product is exact. Weights become operands without a conversion, by
+// their place among the bits of a 16-bit float, with an offset that leaves again with
+// the group's sum of x. The order of k inside a product is free as long as both
+// operands agree: lane l of a quad takes the l-th quarter of a group of a weight row
+// (one 16-byte load of a group of 128), a word of which holds four pairs (k, k + 4),
+// and picks the same pairs of x.
 //
-// The order of k inside a product is free as long as both operands agree: lane l of
-// a quad takes 16 / G' consecutive bytes of a group of a weight row (one 16-byte load
-// of a group of 128), a word of which holds four pairs (k, k + 4), and picks the
-// same pairs of x.
+// Two kernels. Up to 2^25 weights the call is a chain of latencies: one block per 16
+// columns, rows of x read as they lie (k_w4_direct). Above, the weights' stream counts:
+// rings of asynchronous copies per warp, x laid out once per block in shared memory
+// (k_w4_ring). Measured, bf16 rows, direct / ring, us: 5120 x 2048 T=1 4.3 / 4.9, T=8 4.7
+// / 6.1; 2048 x 4096 T=32 7.2 / 11.3; 9000 x 4096 T=1 7.8 / 7.0, T=8 10.7 / 8.8; 32001 x
+// 8192 T=1 47 / 33, T=8 56 / 36, T=32 188 / 90.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -28,7 +29,12 @@
 
 namespace decomoe {
 
-constexpr int W4_WARPS = 8;
+constexpr int W4_DIRECT_WARPS = 8;
+constexpr int W4_STAGES = 4;            // units of a warp's ring
+constexpr int W4_UNIT = 256;            // values of k of a unit (128 bytes of a weight row)
+constexpr int W4_STAGE = 16 * 128;      // bytes of a unit of 16 columns
+constexpr int W4_WARPS = 16;            // warps of a ring block, at most: 128 KB of rings
+constexpr size_t W4_SMEM = 226 * 1024;
 
 struct W4Args {
   const void* x;
@@ -38,29 +44,33 @@ struct W4Args {
   void* out;
   int64_t T, N, x_stride;
   int K, groups, out_f32;
+  int wm, wk;      // ring: column tiles and slices of k of a block, wm * wk warps
+  int chunk;       // ring: units of x staged at a time
+  int64_t tiles;   // tiles of 16 columns in all
 };
 
+// c += a b for 16 columns by 8 rows and 16 values of k; w4_mma0 has nothing to add to.
 template <bool E4M3>
 __device__ __forceinline__ void w4_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   if constexpr (E4M3)
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
   else
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-
-// Pair i (weights i and i + 4) of a word of eight, as two floats 16 + q.
 template <bool E4M3>
-__device__ __forceinline__ uint32_t w4_pair(uint32_t w, int i) {
-  constexpr uint32_t MASK = E4M3 ? 0x03c003c0u : 0x00780078u, SIXTEEN = E4M3 ? 0x4c004c00u : 0x41804180u;
-  const int sh = (E4M3 ? 6 : 3) - 4 * i;
-  const uint32_t s = sh >= 0 ? w << sh : w >> -sh;
-  return (s & MASK) | SIXTEEN;
+__device__ __forceinline__ void w4_mma0(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (E4M3)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // Eight consecutive values of a row of x as four pairs (k, k + 4).
@@ -89,27 +99,61 @@ __device__ __forceinline__ W4X w4_x(const uint2& v) {  // e4m3
   return r;
 }
 
-// One block per 16 MT columns and 8 NT rows; its warps take the groups g = warp,
-// warp + 8, ... and add up in warp order.
-template <bool E4M3, int GROUP, int MT, int NT>
-__global__ void __launch_bounds__(32 * W4_WARPS) k_w4_linear(W4Args a) {
+// The place of (row t, column n) among the accumulators [column tile][row tile][lane][4]
+// of a run of column tiles.
+template <int NT>
+__device__ __forceinline__ int w4_place(int t, int n) {
+  return ((n >> 4) * NT + (t >> 3)) * 128 + ((n & 7) * 4 + ((t & 7) >> 1)) * 4 + ((n >> 3) & 1) * 2 + (t & 1);
+}
+__device__ __forceinline__ void w4_put(const W4Args& a, int64_t t, int64_t n, float v) {
+  if (n >= a.N) return;
+  if (a.xs != nullptr) v *= a.xs[t];
+  if (a.out_f32) static_cast<float*>(a.out)[t * a.N + n] = v;
+  else static_cast<__nv_bfloat16*>(a.out)[t * a.N + n] = __float2bfloat16_rn(v);
+}
+
+// ------------------------------------------------------------------ up to 2^25 weights
+// Four bits put into the mantissa of a 16-bit float of value 16 (bits 3 to 6 in bf16,
+// 6 to 9 in fp16) make it the exact number 16 + q: a shift and a three-input logic
+// operation for two weights. 24 sum x leaves again, added up on the tensor cores too, as
+// the product of the rows with ones; the difference is at most six times smaller
+// than what it is taken from, in fp32.
+__device__ __forceinline__ uint32_t w4_const(uint32_t v) {  // a constant that stays in a register
+  uint32_t r;
+  asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// Pair i (weights i and i + 4) of a word of eight, as two floats 16 + q.
+template <bool E4M3>
+__device__ __forceinline__ uint32_t w4_pair(uint32_t w, int i, uint32_t mask, uint32_t sixteen) {
+  const int sh = (E4M3 ? 6 : 3) - 4 * i;
+  const uint32_t s = sh >= 0 ? w << sh : w >> -sh;
+  uint32_t r;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(s), "r"(mask), "r"(sixteen));  // (s & mask) | sixteen
+  return r;
+}
+
+// One block per 16 columns (blockIdx.x) and 8 NT rows (blockIdx.y); its warps take the
+// groups g = warp, warp + 8, ... and their sums are added in warp order.
+template <bool E4M3, int GROUP, int NT>
+__global__ void __launch_bounds__(32 * W4_DIRECT_WARPS) k_w4_direct(W4Args a) {
   constexpr int WORDS = GROUP / 32;  // words of a group of a weight row per lane
   using XV = std::conditional_t<E4M3, uint2, uint4>;
-  __shared__ float red[W4_WARPS][MT * NT][32][4];
+  __shared__ float red[W4_DIRECT_WARPS][NT * 128];
   pdl_enter();
+  const uint32_t mask = w4_const(E4M3 ? 0x03c003c0u : 0x00780078u);
+  const uint32_t sixteen = w4_const(E4M3 ? 0x4c004c00u : 0x41804180u);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane & 3, row = lane >> 2;
-  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * (16 * MT);
+  const int64_t n0 = static_cast<int64_t>(blockIdx.x) * 16;
   const int64_t t0 = static_cast<int64_t>(blockIdx.y) * (8 * NT);
-  const uint8_t* w[MT][2];
-  const __nv_bfloat16* ws[MT][2];
+  const uint8_t* w[2];
+  const __nv_bfloat16* ws[2];
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t n = min(n0 + m * 16 + i * 8 + row, a.N - 1);
-      w[m][i] = a.w + n * (a.K / 2) + quad * (4 * WORDS);
-      ws[m][i] = a.ws + n * a.groups;
-    }
+  for (int i = 0; i < 2; ++i) {
+    const int64_t n = min(n0 + i * 8 + row, a.N - 1);
+    w[i] = a.w + n * (a.K / 2) + quad * (4 * WORDS);
+    ws[i] = a.ws + n * a.groups;
+  }
   const uint8_t* x[NT];
   bool has[NT];
 #pragma unroll
@@ -118,29 +162,27 @@ __global__ void __launch_bounds__(32 * W4_WARPS) k_w4_linear(W4Args a) {
     x[j] = static_cast<const uint8_t*>(a.x) +
            ((has[j] ? t0 + j * 8 + row : 0) * a.x_stride + quad * (8 * WORDS)) * (E4M3 ? 1 : 2);
   }
-  float acc[MT][NT][4] = {};
+  float acc[NT][4] = {};
   const uint32_t one = E4M3 ? 0x3c003c00u : 0x3f803f80u;
   const uint32_t ones[4] = {one, one, one, one};
 #pragma unroll 2
-  for (int g = warp; g < a.groups; g += W4_WARPS) {
-    uint32_t q[MT][2][WORDS];
-    float s[MT][2];
+  for (int g = warp; g < a.groups; g += W4_DIRECT_WARPS) {
+    uint32_t q[2][WORDS];
+    float s[2];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const uint8_t* p = w[m][i] + static_cast<int64_t>(g) * (GROUP / 2);
-        if constexpr (WORDS == 4) {
-          const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
-          q[m][i][0] = v.x, q[m][i][1] = v.y, q[m][i][2] = v.z, q[m][i][3] = v.w;
-        } else if constexpr (WORDS == 2) {
-          const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-          q[m][i][0] = v.x, q[m][i][1] = v.y;
-        } else {
-          q[m][i][0] = __ldg(reinterpret_cast<const uint32_t*>(p));
-        }
-        s[m][i] = __bfloat162float(ws[m][i][g]);
+    for (int i = 0; i < 2; ++i) {
+      const uint8_t* p = w[i] + static_cast<int64_t>(g) * (GROUP / 2);
+      if constexpr (WORDS == 4) {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+        q[i][0] = v.x, q[i][1] = v.y, q[i][2] = v.z, q[i][3] = v.w;
+      } else if constexpr (WORDS == 2) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+        q[i][0] = v.x, q[i][1] = v.y;
+      } else {
+        q[i][0] = __ldg(reinterpret_cast<const uint32_t*>(p));
       }
+      s[i] = __bfloat162float(ws[i][g]);
+    }
     XV xv[NT][WORDS];
 #pragma unroll
     for (int j = 0; j < NT; ++j)
@@ -148,7 +190,7 @@ __global__ void __launch_bounds__(32 * W4_WARPS) k_w4_linear(W4Args a) {
       for (int u = 0; u < WORDS; ++u)
         xv[j][u] = has[j] ? __ldg(reinterpret_cast<const XV*>(x[j] + static_cast<int64_t>(g) * GROUP * (E4M3 ? 1 : 2)) + u)
                           : XV{};
-    float c[MT][NT][4] = {}, sum[NT][4] = {};
+    float c[NT][4] = {}, sum[NT][4] = {};
 #pragma unroll
     for (int u = 0; u < WORDS; ++u) {
       W4X xp[NT];
@@ -156,45 +198,425 @@ __global__ void __launch_bounds__(32 * W4_WARPS) k_w4_linear(W4Args a) {
       for (int j = 0; j < NT; ++j) xp[j] = w4_x(xv[j][u]);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
+        const uint32_t f[4] = {w4_pair<E4M3>(q[0][u], 2 * h, mask, sixteen), w4_pair<E4M3>(q[1][u], 2 * h, mask, sixteen),
+                               w4_pair<E4M3>(q[0][u], 2 * h + 1, mask, sixteen),
+                               w4_pair<E4M3>(q[1][u], 2 * h + 1, mask, sixteen)};
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          const uint32_t f[4] = {w4_pair<E4M3>(q[m][0][u], 2 * h), w4_pair<E4M3>(q[m][1][u], 2 * h),
-                                 w4_pair<E4M3>(q[m][0][u], 2 * h + 1), w4_pair<E4M3>(q[m][1][u], 2 * h + 1)};
-#pragma unroll
-          for (int j = 0; j < NT; ++j) w4_mma<E4M3>(c[m][j], f, xp[j].p[2 * h], xp[j].p[2 * h + 1]);
+        for (int j = 0; j < NT; ++j) {
+          w4_mma<E4M3>(c[j], f, xp[j].p[2 * h], xp[j].p[2 * h + 1]);
+          w4_mma<E4M3>(sum[j], ones, xp[j].p[2 * h], xp[j].p[2 * h + 1]);
         }
-#pragma unroll
-        for (int j = 0; j < NT; ++j) w4_mma<E4M3>(sum[j], ones, xp[j].p[2 * h], xp[j].p[2 * h + 1]);
       }
     }
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          acc[m][j][i] = fmaf(s[m][i >> 1], fmaf(-24.f, sum[j][i & 1], c[m][j][i]), acc[m][j][i]);
+      for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(s[i >> 1], fmaf(-24.f, sum[j][i & 1], c[j][i]), acc[j][i]);
   }
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int j = 0; j < NT; ++j)
-      *reinterpret_cast<float4*>(red[warp][m * NT + j][lane]) =
-          make_float4(acc[m][j][0], acc[m][j][1], acc[m][j][2], acc[m][j][3]);
+  for (int j = 0; j < NT; ++j)
+    *reinterpret_cast<float4*>(&red[warp][(j * 32 + lane) * 4]) = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
   __syncthreads();
-  // column n (consecutive threads) of row t; its place in the accumulator tiles
-  for (int i = threadIdx.x; i < 16 * MT * 8 * NT; i += 32 * W4_WARPS) {
-    const int nn = i % (16 * MT), tt = i / (16 * MT);
-    const int64_t n = n0 + nn, t = t0 + tt;
-    if (n >= a.N || t >= a.T) continue;
-    const int tile = (nn >> 4) * NT + (tt >> 3), l = (nn & 7) * 4 + ((tt & 7) >> 1), e = ((nn >> 3) & 1) * 2 + (tt & 1);
+  // a column (consecutive threads) of a row each
+  for (int i = threadIdx.x; i < 16 * 8 * NT; i += 32 * W4_DIRECT_WARPS) {
+    const int n = i & 15, t = i >> 4;
+    if (t0 + t >= a.T) continue;
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < W4_WARPS; ++k) v += red[k][tile][l][e];
-    if (a.xs != nullptr) v *= a.xs[t];
-    if (a.out_f32) static_cast<float*>(a.out)[t * a.N + n] = v;
-    else static_cast<__nv_bfloat16*>(a.out)[t * a.N + n] = __float2bfloat16_rn(v);
+    for (int k = 0; k < W4_DIRECT_WARPS; ++k) v += red[k][w4_place<NT>(t, n)];
+    w4_put(a, t0 + t, n0 + n, v);
   }
+}
+
+// ------------------------------------------------------------------ above 2^25 weights
+// The units that handle logic operations would be the bound with two of them for every
+// pair of weights. Four bits at the foot of a 16-bit float are the subnormal number
+// q times its smallest step (2^-133 in bf16, 2^-24 in fp16), the four bits above them
+// 16 q steps, both exact, so that a mask makes two operands and one shift serves four.
+// The values of x that meet the upper bits are divided by 16; in bf16 the rows are also
+// raised by 2^96 (less where a group holds values of 2^31 or more), which keeps the
+// products away from fp32's own subnormals, and the factor comes off each group's sum. The
+// offset leaves with 8 sum x, added up as the rows are laid out.
+__device__ __forceinline__ uint32_t w4_scale_bf16(uint32_t v, int e) {  // two bf16 times 2^e, exact where it does not overflow
+  const __nv_bfloat162 f = __bfloat162bfloat162(__ushort_as_bfloat16(static_cast<unsigned short>((127 + e) << 7)));
+  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v), f);
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t w4_sixteenth(uint32_t v) {  // of two fp16
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&v), __half2half2(__ushort_as_half(0x2c00)));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ void w4_cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// A float at the same place of the shared memory of block `rank` of the cluster.
+__device__ __forceinline__ float w4_ld_cluster(uint32_t addr, int rank) {
+  uint32_t at;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+  return v;
+}
+
+// A cluster of gridDim.x blocks (one or two) shares the columns of its launch column
+// (blockIdx.y), block `rank` of it takes the rank-th part of k, whose x it keeps in
+// shared memory for the 8 NT rows of its launch row (blockIdx.z): all of it or, where
+// that is too much, `chunk` units at a time. It walks over wm tiles of 16 columns at a
+// time, each on wk warps that take its units of k in turn. Every warp streams the
+// weights of its tiles through a ring of its own (16-byte asynchronous copies of
+// 128-byte pieces of 16 rows, on through the tile's end; no block-wide step but at a
+// tile's end). The sums are added over the warps of a block, then over the blocks of
+// the cluster through distributed shared memory, both in the order of k.
+// 32001 x 8192, T=1: 33 us, 4.2 TB/s; the same stream without any product 24.7 us.
+// Above 16 rows the tensor cores bound it (warp-level products, 1024 a cycle per SM).
+template <bool E4M3, int GROUP, int NT>
+__global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
+  constexpr int WORDS = GROUP / 32;            // words of a group of a weight row per lane
+  constexpr int GU = W4_UNIT / GROUP;          // groups of a unit
+  constexpr int SREG = GU == 8 ? 2 : 1;        // scales of a weight row per lane and unit
+  constexpr int TILE = NT * 128;               // floats of a warp's accumulators
+  constexpr int XE = E4M3 ? 1 : 2;             // bytes of a value of x
+  constexpr int XW = NT * 32;                  // 16-byte places of a word of a group of x
+  using XV = std::conditional_t<E4M3, uint2, uint4>;
+  extern __shared__ __align__(128) uint8_t w4_smem[];
+  const uint32_t xf_at = a.wm * a.wk * (W4_STAGES * W4_STAGE);  // x: [chunk groups][WORDS][NT][32 lanes] uint4
+  const uint32_t xo_at = xf_at + a.chunk * (GU * WORDS * XW * 16);  // [chunk groups][8 NT] float2: step of the sums, -8 sum x
+  uint4* xf = reinterpret_cast<uint4*>(w4_smem + xf_at);
+  float2* xoff = reinterpret_cast<float2*>(w4_smem + xo_at);
+  float* red = reinterpret_cast<float*>(xoff + a.chunk * (GU * 8 * NT));  // [warps][NT][32][4]
+  pdl_enter();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, row = lane >> 2;
+  const int slice = warp / a.wm, wm = warp - slice * a.wm;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.z) * (8 * NT);
+  const int rows = static_cast<int>(min(a.T - t0, static_cast<int64_t>(8 * NT)));
+  const int ks = static_cast<int>(gridDim.x), rank = static_cast<int>(blockIdx.x);
+  const int all_units = (a.K + W4_UNIT - 1) / W4_UNIT;
+  const int first = static_cast<int>(static_cast<int64_t>(rank) * all_units / ks);
+  const int units = static_cast<int>(static_cast<int64_t>(rank + 1) * all_units / ks) - first;
+  const int groups = min(units * GU, a.groups - first * GU);
+
+  // ---- weights: unit after unit of this warp's slice, tile after tile
+  const int steps = units > slice ? (units - slice + a.wk - 1) / a.wk : 0;
+  const int64_t tile_step = static_cast<int64_t>(gridDim.y) * a.wm;
+  const uint32_t kb = static_cast<uint32_t>(a.K / 2);
+  const uint32_t ring = warp * (W4_STAGES * W4_STAGE), ring_s = smem_u32(w4_smem) + ring;
+  // rows of 128 bytes; the 16-byte pieces of row r are exchanged by the reverse of r's
+  // low three bits, which spreads the reads of every group size over all banks
+  auto swz = [](int r) { return ((r & 1) << 2) | (r & 2) | ((r >> 2) & 1); };
+  int64_t ptile = static_cast<int64_t>(blockIdx.y) * a.wm + wm;
+  int pstep = 0, pslot = 0;
+  const uint8_t* psrc = nullptr;  // the tile's first row
+  uint32_t pat = 0, prow[4];      // place in a row; offsets of the rows that this lane copies
+  auto enter = [&]() {
+    const int64_t n0 = ptile * 16;
+    psrc = a.w + n0 * kb;
+    pat = static_cast<uint32_t>(first + slice) * 128u + (lane & 7) * 16u;
+    // rows past the last column read it again (their results go nowhere)
+    const int last = static_cast<int>(min(a.N - 1 - n0, int64_t{15}));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) prow[i] = static_cast<uint32_t>(min(i * 4 + (lane >> 3), last)) * kb;
+  };
+  const uint32_t pdst[2] = {(lane >> 3) * 128u + (((lane & 7) ^ swz(lane >> 3)) << 4),
+                            (lane >> 3) * 128u + (((lane & 7) ^ swz(4 + (lane >> 3))) << 4)};
+  if (ptile < a.tiles) enter();
+  auto issue = [&]() {
+    if (ptile < a.tiles && steps > 0) {
+      const bool in = pat < kb;  // the last unit of a row may be cut short: zeros
+      const uint8_t* src = psrc + (in ? pat : 0u);
+      const uint32_t dst = ring_s + pslot * W4_STAGE;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst + pdst[i & 1] + i * 512),
+                     "l"(src + prow[i]), "r"(in ? 16 : 0)
+                     : "memory");
+      pat += a.wk * 128u;
+      if (++pstep == steps) {
+        pstep = 0;
+        ptile += tile_step;
+        if (ptile < a.tiles) enter();
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    pslot = pslot + 1 == W4_STAGES ? 0 : pslot + 1;
+  };
+#pragma unroll
+  for (int i = 0; i < W4_STAGES - 1; ++i) issue();
+
+  // ---- x: units [u0, u0 + n) of this block's; a thread takes what one lane of a quad
+  // reads of a row of a group, the four of them in consecutive threads
+  auto stage = [&](int u0, int n) {
+    constexpr int U = 8 / WORDS;  // such pieces in flight
+    const int g0 = u0 * GU, pieces = min(n * GU, groups - g0) * 4 * rows;
+    // v / rows: the reciprocal rounded up is exact for v below 2^32 / rows
+    const uint32_t inverse = rows > 1 ? 0xffffffffu / static_cast<uint32_t>(rows) + 1 : 0;
+    const uint8_t* x0 = static_cast<const uint8_t*>(a.x) +
+                        (t0 * a.x_stride + (static_cast<int64_t>(first) * GU + g0) * GROUP) * XE;
+    const int64_t xrow = a.x_stride * XE;
+    for (int i0 = tid; i0 - tid < pieces; i0 += U * blockDim.x) {
+      XV v[U][WORDS];
+      int gs[U], rs[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * blockDim.x, gr = i >> 2;
+        gs[u] = rows > 1 ? static_cast<int>(__umulhi(static_cast<uint32_t>(gr), inverse)) : gr;
+        rs[u] = gr - gs[u] * rows;
+        const XV* src = reinterpret_cast<const XV*>(x0 + rs[u] * xrow + (gs[u] * GROUP + (i & 3) * (8 * WORDS)) * XE);
+#pragma unroll
+        for (int e = 0; e < WORDS; ++e) {
+          v[u][e] = XV{};
+          if (i < pieces) v[u][e] = __ldg(src + e);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = i0 + u * blockDim.x;
+        if (i - tid >= pieces) break;
+        W4X p[WORDS];
+        float sum = 0.f;
+        uint32_t top = 0;  // largest |x|, as bits
+#pragma unroll
+        for (int e = 0; e < WORDS; ++e) {
+          p[e] = w4_x(v[u][e]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if constexpr (E4M3) {
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p[e].p[k]));
+              sum += f.x + f.y;
+              p[e].p[k] = k & 1 ? w4_sixteenth(p[e].p[k]) : p[e].p[k];
+            } else {
+              sum += bf16_lo(p[e].p[k]) + bf16_hi(p[e].p[k]);
+              top = max(top, max(p[e].p[k] & 0x7fffu, (p[e].p[k] >> 16) & 0x7fffu));
+            }
+          }
+        }
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        float step = 16777216.f;  // 2^24
+        if constexpr (!E4M3) {
+          int up = 96;
+          if (__any_sync(0xffffffffu, top >= (158u << 7))) {
+            // |x| 2^up stays below 2^127 (what is not finite stays so); fp32 itself ends
+            // before sums of values of 2^121 do
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            up -= min(max(static_cast<int>(top >> 7) - 157, 0), 90);
+          }
+#pragma unroll
+          for (int e = 0; e < WORDS; ++e)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) p[e].p[k] = w4_scale_bf16(p[e].p[k], k & 1 ? up - 4 : up);
+          step = __uint_as_float(static_cast<uint32_t>(127 + 133 - up) << 23);  // 2^(133 - up)
+        }
+        if (i < pieces) {
+          const int at = gs[u] * (WORDS * XW) + (rs[u] >> 3) * 32 + (rs[u] & 7) * 4 + (i & 3);
+#pragma unroll
+          for (int e = 0; e < WORDS; ++e) xf[at + e * XW] = make_uint4(p[e].p[0], p[e].p[1], p[e].p[2], p[e].p[3]);
+          if ((i & 3) == 0) xoff[gs[u] * (8 * NT) + rs[u]] = make_float2(step, -8.f * sum);
+        }
+      }
+    }
+  };
+
+  // this lane's places in a word of x and in a unit's rows (byte offsets); rows of x
+  // that are not there read the first one, and their results go nowhere
+  uint32_t xl[NT], wl[GU];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) xl[j] = xf_at + (j * 8 + row < rows ? j * 32 + lane : quad) * 16;
+#pragma unroll
+  for (int gg = 0; gg < GU; ++gg)
+    wl[gg] = row * 128 + (((gg * WORDS + (quad * WORDS >> 2)) ^ swz(row)) << 4) + (quad * WORDS & 3) * 4;
+  const int ends = min(a.chunk, units);  // end of the first chunk
+  int c0 = -1;                           // first staged unit
+  int slot = 0;
+  for (int64_t tile0 = static_cast<int64_t>(blockIdx.y) * a.wm; tile0 < a.tiles; tile0 += tile_step) {
+    const bool live = tile0 + wm < a.tiles && steps > 0;
+    const int64_t n0 = (tile0 + wm) * 16;
+    const unsigned short* ws = reinterpret_cast<const unsigned short*>(a.ws) + n0 * a.groups + first * GU;
+    uint32_t so[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      so[i] = static_cast<uint32_t>(max(min(n0 + i * 8 + row, a.N - 1) - n0, int64_t{0})) * static_cast<uint32_t>(a.groups);
+    // bf16 scales of this step and the next: lane l of a quad holds groups l and l + 4 of a unit
+    uint32_t s[2][SREG] = {}, s1[2][SREG] = {};
+    auto scales = [&](uint32_t (&d)[2][SREG], int step) {
+#pragma unroll
+      for (int e = 0; e < SREG; ++e) {
+        const int g = min((slice + step * a.wk) * GU + (quad & (GU - 1)) + 4 * e, groups - 1);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) d[i][e] = __ldg(ws + (so[i] + g));
+      }
+    };
+    if (live) {
+      scales(s, 0);
+      scales(s1, 1);
+    }
+    if (c0 != 0) {
+      c0 = 0;
+      stage(0, ends);
+      __syncthreads();
+    }
+    float acc[NT][4] = {};
+    // chunk after chunk of k (mostly one); every warp goes through every chunk
+    for (int step = 0, end = ends;;) {
+      const int until = live ? min(steps, (end - slice + a.wk - 1) / a.wk) : 0;
+      uint32_t xg = static_cast<uint32_t>((slice + step * a.wk - c0) * GU);  // first group, from the chunk's
+#pragma unroll 1
+      for (; step < until; ++step, xg += a.wk * GU) {
+        issue();
+        uint32_t s2[2][SREG];
+        scales(s2, step + 2);
+        asm volatile("cp.async.wait_group %0;" ::"n"(W4_STAGES - 1) : "memory");
+        __syncwarp();
+        const uint32_t wq = ring + slot * W4_STAGE;
+        const int left = groups - (slice + step * a.wk) * GU;  // the last unit may be cut short
+#pragma unroll
+        for (int gg = 0; gg < GU; ++gg) {
+          if (gg > 0 && gg >= left) break;
+          uint32_t q[2][WORDS];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const uint32_t p = wq + wl[gg] + i * 8 * 128;
+            if constexpr (WORDS == 4) {
+              const uint4 v = *reinterpret_cast<const uint4*>(w4_smem + p);
+              q[i][0] = v.x, q[i][1] = v.y, q[i][2] = v.z, q[i][3] = v.w;
+            } else if constexpr (WORDS == 2) {
+              const uint2 v = *reinterpret_cast<const uint2*>(w4_smem + p);
+              q[i][0] = v.x, q[i][1] = v.y;
+            } else {
+              q[i][0] = *reinterpret_cast<const uint32_t*>(w4_smem + p);
+            }
+          }
+          float c[NT][4];
+          const uint32_t xb = (xg + gg) * (WORDS * XW * 16);
+#pragma unroll
+          for (int word = 0; word < WORDS; ++word) {
+            const uint32_t q0 = q[0][word], q1 = q[1][word], h0 = q0 >> 8, h1 = q1 >> 8;
+            const uint32_t f0[4] = {q0 & 0x000f000fu, q1 & 0x000f000fu, q0 & 0x00f000f0u, q1 & 0x00f000f0u};
+            const uint32_t f1[4] = {h0 & 0x000f000fu, h1 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x00f000f0u};
+#pragma unroll
+            for (int j = 0; j < NT; ++j) {
+              const uint4 xp = *reinterpret_cast<const uint4*>(w4_smem + (xl[j] + xb + word * (XW * 16)));
+              if (word == 0) w4_mma0<E4M3>(c[j], f0, xp.x, xp.y);
+              else w4_mma<E4M3>(c[j], f0, xp.x, xp.y);
+              w4_mma<E4M3>(c[j], f1, xp.z, xp.w);
+            }
+          }
+          float f[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            f[i] = __uint_as_float(__shfl_sync(0xffffffffu, s[i][gg >> 2], (lane & ~3) + (gg & 3)) << 16);
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            const float4 o = *reinterpret_cast<const float4*>(w4_smem + (xo_at + quad * 16 + (xg + gg) * (64 * NT) + j * 64));
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              acc[j][2 * i] = fmaf(f[i], fmaf(c[j][2 * i], o.x, o.y), acc[j][2 * i]);
+              acc[j][2 * i + 1] = fmaf(f[i], fmaf(c[j][2 * i + 1], o.z, o.w), acc[j][2 * i + 1]);
+            }
+          }
+        }
+        __syncwarp();
+        slot = slot + 1 == W4_STAGES ? 0 : slot + 1;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int e = 0; e < SREG; ++e) {
+            s[i][e] = s1[i][e];
+            s1[i][e] = s2[i][e];
+          }
+      }
+      if (end == units) break;
+      __syncthreads();
+      c0 = end;
+      end = min(end + a.chunk, units);
+      stage(c0, end - c0);
+      __syncthreads();
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+      *reinterpret_cast<float4*>(red + warp * TILE + (j * 32 + lane) * 4) =
+          make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
+    __syncthreads();
+    // a column (consecutive threads) of a row each
+    const int cols = 16 * a.wm;
+    auto of_block = [&](int at) {
+      float v = 0.f;
+      for (int k = 0; k < a.wk; ++k) v += red[k * a.wm * TILE + at];
+      return v;
+    };
+    if (ks == 1) {
+      for (int i = tid; i < cols * rows; i += blockDim.x) {
+        const int t = i / cols, n = i - t * cols;
+        w4_put(a, t0 + t, tile0 * 16 + n, of_block(w4_place<NT>(t, n)));
+      }
+      __syncthreads();
+    } else {
+      if (a.wk > 1)
+        for (int i = tid; i < a.wm * TILE; i += blockDim.x) red[i] = of_block(i);
+      w4_cluster_sync();
+      // each block takes the rank-th part of the (row, column) places
+      const int all = cols * rows, per = (all + ks - 1) / ks, i1 = min(all, (rank + 1) * per);
+      for (int i = rank * per + tid; i < i1; i += blockDim.x) {
+        const int t = i / cols, n = i - t * cols;
+        const uint32_t at = smem_u32(red + w4_place<NT>(t, n));
+        float v = 0.f;
+        for (int k = 0; k < ks; ++k) v += w4_ld_cluster(at, k);
+        w4_put(a, t0 + t, tile0 * 16 + n, v);
+      }
+      w4_cluster_sync();  // nobody leaves, or writes its sums again, before all have read them
+    }
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+template <bool E4M3, int GROUP, int NT>
+static int w4_launch(W4Args a, cudaStream_t s) {
+  a.tiles = (a.N + 15) / 16;
+  const unsigned z = static_cast<unsigned>((a.T + 8 * NT - 1) / (8 * NT));
+  if (a.N * a.K <= int64_t{1} << 25) {
+    DM_CUDA_CHECK(launch_pdl(k_w4_direct<E4M3, GROUP, NT>, dim3(static_cast<unsigned>(a.tiles), z),
+                             dim3(32 * W4_DIRECT_WARPS), 0, s, a));
+    return DECOMOE_OK;
+  }
+  const int units = (a.K + W4_UNIT - 1) / W4_UNIT;
+  const size_t per_unit = NT * 32 * 16 * (W4_UNIT / 32) + NT * 8 * (W4_UNIT / GROUP) * sizeof(float2);
+  const int64_t sms = sm_count();
+  // Two blocks share k where x is large beside the columns, so that each lays out half of it
+  // and twice as many columns use it: 9000 x 4096 T=32 24.6 -> 20.6 us, T=13 12.9 -> 11.9;
+  // not where the columns then no longer go in one pass (20000 x 2048 T=13 14.0 -> 17.4) nor
+  // where x is small (9000 x 4096 T=1 7.0 -> 8.1).
+  const int ks = units * per_unit > 100 * 1024 && a.tiles <= (sms / 2) * W4_WARPS && sms > 1 ? 2 : 1;
+  const int64_t places = sms / ks;
+  // as few passes over the column tiles as the warps of all blocks allow, the tiles
+  // spread over all blocks, and what is left of the warps over k
+  const int64_t passes = (a.tiles + places * W4_WARPS - 1) / (places * W4_WARPS);
+  a.wm = static_cast<int>((a.tiles + places * passes - 1) / (places * passes));
+  const int part = (units + ks - 1) / ks;
+  a.wk = std::max(1, std::min(W4_WARPS / a.wm, part));
+  const int warps = a.wm * a.wk;
+  const size_t fixed = static_cast<size_t>(warps) * (W4_STAGES * W4_STAGE + NT * 512);
+  a.chunk = static_cast<int>(std::min<size_t>(part, (W4_SMEM - fixed) / per_unit));
+  const size_t smem = fixed + a.chunk * per_unit;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(ks, static_cast<unsigned>(std::min(places, (a.tiles + a.wm - 1) / a.wm)), z);
+  cfg.blockDim = dim3(32 * warps);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed =
+      pdl_enabled(static_cast<int64_t>(cfg.gridDim.x) * cfg.gridDim.y * cfg.gridDim.z) ? 1 : 0;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = ks;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 2;
+  auto kern = k_w4_ring<E4M3, GROUP, NT>;
+  DM_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+  DM_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kern, a));
+  return DECOMOE_OK;
 }
 
 }  // namespace decomoe
@@ -209,6 +631,7 @@ extern "C" int decomoe_w4_linear(const void* x, int x_dtype, int64_t x_stride, c
   DM_ARG_CHECK(out_dtype == DECOMOE_BF16 || out_dtype == DECOMOE_F32, "w4_linear: out must be bf16 or f32");
   DM_ARG_CHECK(group == 32 || group == 64 || group == 128, "w4_linear: group must be 32, 64 or 128");
   DM_ARG_CHECK(T >= 0 && K > 0 && K % group == 0 && N >= 1 && N <= INT_MAX, "w4_linear: bad sizes (K a multiple of group)");
+  DM_ARG_CHECK(K <= 1 << 26, "w4_linear: K above 2^26");
   DM_ARG_CHECK(T <= 65535 * 8, "w4_linear: T above %d", 65535 * 8);
   if (T == 0) return DECOMOE_OK;
   DM_ARG_CHECK(x && w && w_scale && out, "w4_linear: null pointer");
@@ -231,17 +654,12 @@ extern "C" int decomoe_w4_linear(const void* x, int x_dtype, int64_t x_stride, c
   a.groups = K / group;
   a.out_f32 = out_dtype == DECOMOE_F32;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  auto go = [&](auto kern, int cols, int rows) -> int {
-    const dim3 grid(static_cast<unsigned>((N + cols - 1) / cols), static_cast<unsigned>((T + rows - 1) / rows));
-    DM_CUDA_CHECK(launch_pdl(kern, grid, dim3(32 * W4_WARPS), 0, s, a));
-    return DECOMOE_OK;
-  };
   auto by_rows = [&](auto e4m3, auto grp) -> int {
     constexpr bool E = decltype(e4m3)::value;
     constexpr int G = decltype(grp)::value;
-    if (T <= 8) return go(k_w4_linear<E, G, 1, 1>, 16, 8);
-    if (T <= 16) return go(k_w4_linear<E, G, 1, 2>, 16, 16);
-    return go(k_w4_linear<E, G, 1, 4>, 16, 32);
+    if (T <= 8) return w4_launch<E, G, 1>(a, s);
+    if (T <= 16) return w4_launch<E, G, 2>(a, s);
+    return w4_launch<E, G, 4>(a, s);
   };
   auto by_group = [&](auto e4m3) -> int {
     switch (group) {

@@ -202,6 +202,76 @@ def test_w4_rows_of_wider_ones():
     _check_w4(20, 9, 128, 32, BF16, pad=8)
 
 
+def _check_w4_large(T, N, K, group, kind, seed=0, out_dtype=F32, spread=None):
+    """As _check_w4 for matrices of which 64-bit copies are made on the GPU, a
+    block of columns at a time."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    w = torch.randint(0, 256, (N, K // 2), generator=g, device=DEV, dtype=torch.uint8)
+    ws = (torch.rand(N, K // group, generator=g, device=DEV) * 0.02 - 0.005).to(BF16)
+    x = torch.randn(T, K, generator=g, device=DEV)
+    if spread is not None:
+        x = x * spread(x)
+    xs = None
+    if kind == E4M3:
+        a = x.abs().amax(1, keepdim=True)
+        xs = (a[:, 0] / 448).float()
+        x = x * 448 / a
+    x = x.to(kind)
+    out = torch.full((T, N), 5.0, dtype=out_dtype, device=DEV)
+    dm.decomoe_w4_linear(x, w, ws, out, x_scale=xs)
+    again = torch.empty_like(out)
+    dm.decomoe_w4_linear(x, w, ws, again, x_scale=xs)
+    assert torch.equal(out, again)
+    x64 = x.double() * (1.0 if xs is None else xs.double()[:, None])
+    u = 2.0 ** -8 if out_dtype == BF16 else 2.0 ** -23
+    for n in range(0, N, 4096):
+        b = w[n:n + 4096].int()
+        q = torch.stack([b % 16, b // 16], -1).flatten(1).double() - 8
+        s = ws[n:n + 4096].double().repeat_interleave(group, 1)
+        ref, mag = x64 @ (q * s).t(), x64.abs() @ s.abs().t() * 16
+        err = (out[:, n:n + 4096].double() - ref).abs()
+        assert (err <= u * ref.abs() + 2.0 ** -18 * mag).all(), (n, float((err / mag).max()))
+
+
+@pytest.mark.parametrize("kind", [BF16, E4M3])
+@pytest.mark.parametrize("T,N,K,group", [
+    (1, 20000, 2048, 128), (3, 40001, 1024, 64), (8, 4111, 8224, 32), (9, 9000, 4096, 128), (16, 20001, 2112, 64),
+    (17, 4500, 8192, 64), (32, 4500, 8192, 128), (33, 5000, 8000, 32), (32, 2100, 16384, 32), (5, 1100, 32768, 128),
+    (2, 130000, 512, 128), (20, 80000, 512, 64), (12, 300, 131072, 64)])
+def test_w4_large_matrices(kind, T, N, K, group):
+    # the kernel that large matrices take: one pass and several over the columns, rows
+    # cut inside a unit of k, x staged whole and in parts, on one block and on two
+    _check_w4_large(T, N, K, group, kind, seed=T + N)
+
+
+@pytest.mark.parametrize("N,K", [(500, 1024), (20000, 2048)])
+def test_w4_values_of_every_size(N, K):
+    # groups of values around 2^-40, 1, 2^40 and 2^100 side by side in a row, rows of one size
+    def spread(x):
+        e = torch.tensor([0, 40, -40, 100, 31, 35], device=DEV)
+        f = 2.0 ** e[(torch.arange(K, device=DEV) // 64) % 6].float()
+        f = f.expand_as(x).clone()
+        f[1], f[2], f[3] = 2.0 ** 100, 2.0 ** -60, 1.0
+        return f
+
+    _check_w4_large(6, N, K, 64, BF16, spread=spread)
+    _check_w4_large(6, N, K, 64, BF16, spread=spread, out_dtype=BF16)
+
+
+def test_w4_large_matrix_keeps_non_finite_values_in_their_row():
+    N, K = 20000, 2048
+    w = torch.randint(0, 256, (N, K // 2), device=DEV, dtype=torch.uint8)
+    ws = torch.full((N, K // 64), 0.01, dtype=BF16, device=DEV)
+    x = torch.randn(9, K, device=DEV).to(BF16)
+    out = [torch.empty(9, N, dtype=F32, device=DEV) for _ in range(2)]
+    dm.decomoe_w4_linear(x, w, ws, out[0])
+    x[4, 100], x[7, 5] = float("nan"), float("inf")
+    dm.decomoe_w4_linear(x, w, ws, out[1])
+    keep = [0, 1, 2, 3, 5, 6, 8]
+    assert torch.isnan(out[1][4]).all() and not torch.isfinite(out[1][7]).any()
+    assert torch.equal(out[0][keep], out[1][keep])
+
+
 def test_w4_values_that_are_not_finite_stay_in_their_row():
     x, w, ws, _ = _w4(9, 40, 512, 64, BF16)
     out = [torch.empty(9, 40, dtype=F32, device=DEV) for _ in range(2)]
