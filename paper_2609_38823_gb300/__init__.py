@@ -614,39 +614,22 @@ def decomoe_moe_layer(x, w_r, bias, w_gate_up, w_down, k, out, ws, K_fixed=0, p=
     return Ku.value, (Ks.value if Ks.value >= 0 else None)
 
 
-def _need_i32(name, *ts):
-    """Contiguous int32 device vectors or matrices (index arrays; None passes)."""
-    for t in ts:
-        if t is not None and not (t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()):
-            raise ValueError(f"{name}: index arrays must be contiguous int32 device tensors")
+# The calls of a decode step go through the _marshal extension (csrc/marshal.cpp),
+# which checks the tensors and calls the same C ABI: in Python those checks cost
+# more than the launches.
+_step_calls = None
 
 
-def _rows(name, t, tail):
-    """The row stride (elements) of a device tensor [N, *tail] whose rows are
-    contiguous; the rows themselves may lie apart (a slice of wider rows)."""
-    if not t.is_cuda or tuple(t.shape[1:]) != tail:
-        raise ValueError(f"{name}: a device tensor [N, {', '.join(map(str, tail))}] expected, got {tuple(t.shape)}")
-    width = math.prod(tail)
-    if t.is_contiguous():
-        return width
-    inner = 1
-    for size, stride in zip(reversed(tail), reversed(t.stride()[1:])):
-        if size != 1 and stride != inner:
-            raise ValueError(f"{name}: rows must be contiguous")
-        inner *= size
-    return t.stride(0) if t.shape[0] > 1 else width
-
-
-def _pool(name, k_pages, v_pages):
-    """(num_pages, page_size, Hkv, D, page stride in elements) of a key and a
-    value pool [num_pages, page_size, Hkv, D] whose pages are contiguous."""
-    if k_pages.dim() != 4 or v_pages.shape != k_pages.shape or v_pages.dtype != k_pages.dtype:
-        raise ValueError(f"{name}: two pools [num_pages, page_size, Hkv, D] of one shape and type expected")
-    P, ps, hkv, d = k_pages.shape
-    stride = _rows(name, k_pages, (ps, hkv, d))
-    if _rows(name, v_pages, (ps, hkv, d)) != stride:
-        raise ValueError(f"{name}: the two pools must have the same page stride")
-    return P, ps, hkv, d, stride
+def _calls():
+    global _step_calls
+    if _step_calls is None:
+        lib()
+        try:
+            from . import _marshal
+        except ImportError as e:
+            raise ImportError(f"the _marshal extension cannot be loaded ({e}): build it with __graft_entry__.build()") from e
+        _step_calls = _marshal
+    return _step_calls
 
 
 def decomoe_paged_plan(cached, fresh, page_size, free_pages, block_table, seq_len, row_start, slot_map, positions=None,
@@ -655,35 +638,19 @@ def decomoe_paged_plan(cached, fresh, page_size, free_pages, block_table, seq_le
     requests' lengths: cached, fresh, seq_len [B], block_table [B, max_pages],
     row_start [B + 1], slot_map and positions [N], free_pages [n_free],
     free_head and free_head_out [1], all int32 on the device."""
-    _need_i32("paged_plan", cached, fresh, free_pages, block_table, seq_len, row_start, slot_map, positions, free_head,
-              free_head_out, status)
-    B, N = cached.shape[0], slot_map.shape[0]
-    if (fresh.shape[0] != B or seq_len.shape[0] != B or row_start.shape[0] != B + 1 or block_table.dim() != 2
-            or block_table.shape[0] != B or (positions is not None and positions.shape[0] != N)):
-        raise ValueError("paged_plan: cached, fresh, seq_len [B], row_start [B + 1], block_table [B, max_pages], "
-                         "slot_map and positions [N] expected")
-    _check("decomoe_paged_plan",
-           lib().decomoe_paged_plan(_ptr(cached), _ptr(fresh), B, page_size, _ptr(free_pages), free_pages.shape[0],
-                                    _ptr(free_head), _ptr(free_head_out), _ptr(block_table), block_table.shape[1],
-                                    _ptr(seq_len), _ptr(row_start), _ptr(slot_map), _ptr(positions), N, _ptr(status),
-                                    _stream(stream)))
+    code = _calls().paged_plan(cached, fresh, page_size, free_pages, block_table, seq_len, row_start, slot_map, positions,
+                               free_head, free_head_out, status, None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_paged_plan", code)
 
 
 def decomoe_paged_append(k_new, v_new, slot_map, k_pages, v_pages, status=None, stream=None):
     """New key and value rows [N, Hkv, D] (rows may be slices of wider ones)
     into their slots of the pools [num_pages, page_size, Hkv, D]."""
-    _need_i32("paged_append", slot_map, status)
-    P, ps, hkv, d, page_stride = _pool("paged_append", k_pages, v_pages)
-    ks, vs = _rows("paged_append", k_new, (hkv, d)), _rows("paged_append", v_new, (hkv, d))
-    N = slot_map.shape[0]
-    if k_new.shape[0] != N or v_new.shape[0] != N:
-        raise ValueError("paged_append: k_new, v_new [N, Hkv, D] and slot_map [N] expected")
-    if k_new.dtype != k_pages.dtype or v_new.dtype != k_pages.dtype:
-        raise TypeError("paged_append: rows and pools must have one type")
-    _check("decomoe_paged_append",
-           lib().decomoe_paged_append(_ptr(k_new), ks, _ptr(v_new), vs, N, hkv * d, _dt(k_pages), _ptr(slot_map),
-                                      _ptr(k_pages), _ptr(v_pages), P, ps, page_stride, _ptr(status),
-                                      _stream(stream)))
+    code = _calls().paged_append(k_new, v_new, slot_map, k_pages, v_pages, status,
+                                 None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_paged_append", code)
 
 
 def decomoe_paged_attention_workspace_bytes(B, Hq, Hkv, D):
@@ -695,70 +662,29 @@ def decomoe_paged_attention(q, k_pages, v_pages, block_table, seq_len, out, ws, 
     """One new token per request over its pages: q [B, Hq, D] (requests may be
     slices of wider rows), out [B, Hq, D], block_table [B, max_pages], seq_len
     [B]; rows [hide_begin[b], hide_begin[b] + hide_count[b]) are left out."""
-    _need_i32("paged_attention", block_table, seq_len, hide_begin, hide_count, status)
-    _need_cuda(out, ws)
-    P, ps, hkv, d, page_stride = _pool("paged_attention", k_pages, v_pages)
-    B, hq = q.shape[0], q.shape[1]
-    q_stride = _rows("paged_attention", q, (hq, d))
-    if (out.shape != q.shape or seq_len.shape[0] != B or block_table.dim() != 2 or block_table.shape[0] != B
-            or any(h is not None and h.shape[0] != B for h in (hide_begin, hide_count))):
-        raise ValueError("paged_attention: q, out [B, Hq, D], block_table [B, max_pages], seq_len, hide_begin and "
-                         "hide_count [B] expected")
-    if any(t.dtype != torch.bfloat16 for t in (q, k_pages, out)):
-        raise TypeError("paged_attention: q, pools and out must be bf16")
-    _check("decomoe_paged_attention",
-           lib().decomoe_paged_attention(_ptr(q), q_stride, B, _ptr(k_pages), _ptr(v_pages), P, ps, page_stride,
-                                         _ptr(block_table), block_table.shape[1], _ptr(seq_len), _ptr(hide_begin),
-                                         _ptr(hide_count), hq, hkv, d, scale, _ptr(out), _ptr(ws),
-                                         ws.numel() * ws.element_size(), _ptr(status), _stream(stream)))
+    code = _calls().paged_attention(q, k_pages, v_pages, block_table, seq_len, out, ws, hide_begin, hide_count, scale,
+                                    status, None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_paged_attention", code)
 
 
 def decomoe_add_rmsnorm_q8(x, residual, weight, sum_out=None, y=None, y8=None, y8_scale=None, eps=1e-6, stream=None):
     """s = x + residual, v = s / rms(s) * weight: s to sum_out, v to y, and v in
     8 bits to y8 (e4m3) with one scale per row in y8_scale (fp32). residual,
     weight and each output may be None."""
-    _need_cuda(x, residual, weight, sum_out, y, y8, y8_scale)
-    T, d = x.shape
-    dt = x.dtype
-    for t in (residual, sum_out, y):
-        if t is not None and (t.shape != x.shape or t.dtype != dt):
-            raise ValueError("add_rmsnorm_q8: residual, sum_out and y must have x's shape and type")
-    if weight is not None and (weight.shape != (d,) or weight.dtype != dt):
-        raise ValueError("add_rmsnorm_q8: weight [d] of x's type expected")
-    if y8 is not None and (y8.shape != x.shape or y8.dtype != torch.float8_e4m3fn):
-        raise ValueError("add_rmsnorm_q8: y8 [T, d] float8_e4m3fn expected")
-    if y8_scale is not None and (y8_scale.numel() != T or y8_scale.dtype != torch.float32):
-        raise ValueError("add_rmsnorm_q8: y8_scale [T] float32 expected")
-    _check("decomoe_add_rmsnorm_q8",
-           lib().decomoe_add_rmsnorm_q8(_ptr(x), _ptr(residual), _ptr(weight), T, d, eps, _dt(x), _ptr(sum_out),
-                                        _ptr(y), _ptr(y8), _ptr(y8_scale), _stream(stream)))
+    code = _calls().add_rmsnorm_q8(x, residual, weight, sum_out, y, y8, y8_scale, eps,
+                                   None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_add_rmsnorm_q8", code)
 
 
 def decomoe_w4_linear(x, w, w_scale, out, x_scale=None, stream=None):
     """out [T, N] = x [T, K] times 4-bit weights w [N, K / 2] (uint8, even k in
     the low bits, value q - 8) with bf16 group scales w_scale [N, K / group].
     x: bf16, or e4m3 with x_scale [T] fp32 (rows may be slices of wider ones)."""
-    _need_cuda(w, w_scale, out, x_scale)
-    T, K = x.shape
-    N = w.shape[0]
-    x_stride = _rows("w4_linear", x, (K,))
-    if w.dtype != torch.uint8 or w.shape != (N, K // 2) or w_scale.dtype != torch.bfloat16 or w_scale.dim() != 2 or (
-            w_scale.shape[0] != N):
-        raise ValueError("w4_linear: w [N, K / 2] uint8 and w_scale [N, K / group] bf16 expected")
-    if out.shape != (T, N):
-        raise ValueError("w4_linear: out [T, N] expected")
-    groups = w_scale.shape[1]
-    if groups == 0 or K % groups or K % 2:
-        raise ValueError("w4_linear: K must be groups * group")
-    if x.dtype == torch.float8_e4m3fn:
-        x_dtype = DECOMOE_E4M3
-        if x_scale is None or x_scale.dtype != torch.float32 or x_scale.numel() != T:
-            raise ValueError("w4_linear: e4m3 rows need x_scale [T] float32")
-    else:
-        x_dtype = _dt(x)
-    _check("decomoe_w4_linear",
-           lib().decomoe_w4_linear(_ptr(x), x_dtype, x_stride, _ptr(x_scale), T, K, _ptr(w), _ptr(w_scale),
-                                   K // groups, N, _ptr(out), _dt(out), _stream(stream)))
+    code = _calls().w4_linear(x, w, w_scale, out, x_scale, None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_w4_linear", code)
 
 
 def decomoe_read_status(status, stream=None) -> int:

@@ -1,25 +1,31 @@
-"""Build libdecomoe.so in-tree with nvcc for sm_103a.
+"""Build libdecomoe.so in-tree with nvcc for sm_103a, and the _marshal extension.
 
 Each CUDA translation unit compiles in parallel (one -gencode), the plain-C
-prefix selection with gcc, and nvcc links the shared library next to this file.
+prefix selection with gcc, the Python extension that marshals the decode step's
+calls with g++ against torch's headers, and the two shared libraries are linked
+next to this file.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libdecomoe.so")
+EXT = os.path.join(HERE, "_marshal.so")
 
 CU_SOURCES = ["api.cu", "route.cu", "dispatch.cu", "expert_gemm.cu", "combine_compact.cu", "calib_gate.cu", "layer.cu", "decode_layer.cu", "attention.cu",
               "paged.cu", "paged_attention.cu", "add_norm.cu", "w4_linear.cu"]
 C_SOURCES = ["prefix.c"]
+EXT_SOURCE = "marshal.cpp"
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 
@@ -40,11 +46,11 @@ def _run(cmd):
 def build(verbose: bool = False, ptxas_info: bool = False, force: bool = False) -> str:
     os.makedirs(BUILD, exist_ok=True)
     nvcc = nvcc_path()
-    srcs = [os.path.join(CSRC, s) for s in CU_SOURCES + C_SOURCES]
+    srcs = [os.path.join(CSRC, s) for s in CU_SOURCES + C_SOURCES + [EXT_SOURCE]]
     hdrs = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith(".cuh")]
     hdrs.append(os.path.join(ROOT, "include", "decomoe.h"))
-    if not force and os.path.exists(LIB):
-        lib_t = os.path.getmtime(LIB)
+    if not force and os.path.exists(LIB) and os.path.exists(EXT):
+        lib_t = min(os.path.getmtime(LIB), os.path.getmtime(EXT))
         if all(os.path.getmtime(p) < lib_t for p in srcs + hdrs + [__file__]):
             return LIB
     common = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC,-fvisibility=hidden",
@@ -60,6 +66,13 @@ def build(verbose: bool = False, ptxas_info: bool = False, force: bool = False) 
         cc = shutil.which("gcc") or "cc"
         jobs.append(([cc, "-O2", "-std=c11", "-fPIC", "-fvisibility=hidden", "-Wall",
                       "-I" + os.path.join(ROOT, "include"), "-c", os.path.join(CSRC, s), "-o", obj], obj))
+    torch_dir = list(importlib.util.find_spec("torch").submodule_search_locations)[0]
+    cuda = os.path.dirname(os.path.dirname(nvcc))
+    ext_obj = os.path.join(BUILD, "marshal.o")
+    cxx = shutil.which("g++") or "c++"
+    jobs.append(([cxx, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-I" + os.path.join(torch_dir, "include"),
+                  "-I" + sysconfig.get_paths()["include"], "-I" + os.path.join(cuda, "include"), "-c",
+                  os.path.join(CSRC, EXT_SOURCE), "-o", ext_obj], ext_obj))
     outs = []
     with cf.ThreadPoolExecutor(max_workers=min(len(jobs), os.cpu_count() or 4)) as ex:
         for out in ex.map(lambda j: _run(j[0]), jobs):
@@ -69,8 +82,12 @@ def build(verbose: bool = False, ptxas_info: bool = False, force: bool = False) 
             if o.strip():
                 sys.stdout.write(o)
     tmp = LIB + ".tmp"
-    _run([nvcc, *ARCH, "-shared", "-o", tmp, *[j[1] for j in jobs], "-lcudart"])
+    _run([nvcc, *ARCH, "-shared", "-o", tmp, *[j[1] for j in jobs if j[1] != ext_obj], "-lcudart"])
     os.replace(tmp, LIB)
+    tmp = EXT + ".tmp"
+    _run([cxx, "-shared", "-o", tmp, ext_obj, "-L" + HERE, "-ldecomoe", "-L" + os.path.join(torch_dir, "lib"),
+          "-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10", "-Wl,-rpath,$ORIGIN"])
+    os.replace(tmp, EXT)
     return LIB
 
 
