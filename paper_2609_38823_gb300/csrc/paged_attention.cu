@@ -28,6 +28,7 @@ constexpr int PGA_WARPS = 8;
 constexpr int PGA_THREADS = 32 * PGA_WARPS;
 constexpr int PGA_STAGES = 3;
 constexpr int PGA_STAGE = 8192;  // bytes of one tile: keys, then values
+constexpr int PGA_EXTRA = 3;     // what a (request, KV head) pair costs beside its tiles, in tiles
 
 template <int D>
 struct PgaTile {
@@ -48,6 +49,7 @@ struct PagedArgs {
   int64_t q_stride, page_stride, num_pages, max_pages;
   int B, hq, hkv, shift;
   int qt, hv;    // query tiles per KV head, (KV head, query tile) pairs
+  int extra;     // what a pair costs beside its tiles, in tiles
   float sl2;     // scale * log2(e)
 };
 
@@ -71,15 +73,30 @@ __device__ __forceinline__ PgaReq pga_request(const PagedArgs& a, int b, bool* b
   return r;
 }
 
-// The first tile of warp i's share, of `total` tiles over `workers` warps: equal
-// shares, or one tile each where there are fewer tiles than warps.
-__device__ __forceinline__ int pga_share(int64_t total, int workers, int i) {
-  return static_cast<int>(total >= workers ? i * total / workers : min(static_cast<int64_t>(i), total));
-}
-// The warp whose share holds tile t.
-__device__ __forceinline__ int pga_holder(int64_t total, int workers, int t) {
-  return static_cast<int>(total >= workers ? ((static_cast<int64_t>(t) + 1) * workers - 1) / total : t);
-}
+// How the tiles are shared out. A pair costs `extra` more than its tiles (its
+// lengths, queries and result go over latencies that its tiles' copies do not hide),
+// so warps get equal shares of tiles + extra: places of a line on which every pair
+// takes tiles + extra of them, the first `extra` belonging to its first tile.
+struct PgaPlan {
+  const int* pre;  // [B + 1] tiles per head tile before a request
+  const int* nz;   // [B + 1] requests that see something before a request
+  int B, hv, extra;
+  int total;       // places in all
+  int per, more;   // places of a warp, and how many warps take one more
+  __device__ __forceinline__ int places(int b) const {  // before request b
+    return (pre[b] + nz[b] * extra) * hv;
+  }
+  __device__ __forceinline__ void divide(int workers) {
+    total = places(B);
+    per = total / workers;
+    more = total - per * workers;
+  }
+  __device__ __forceinline__ int place(int i) const { return i * per + min(i, more); }  // the first one of warp i
+  __device__ __forceinline__ int holder(int p) const {  // the warp whose share holds place p
+    const int full = more * (per + 1);
+    return p < full ? p / (per + 1) : more + (p - full) / per;
+  }
+};
 
 __device__ __forceinline__ float pga_ex2(float x) {
   float y;
@@ -122,19 +139,20 @@ struct PgaWalk {
     r = pga_request(a, b, &bad);
     tiles = (r.seen + PgaTile<D>::KEYS - 1) / PgaTile<D>::KEYS;
   }
-  __device__ __forceinline__ void seek(const PagedArgs& a, const int* pre, int tile) {
-    int lo = 0, hi = a.B;  // the last request with pre * hv <= tile: it is not empty
-    const int at = tile / a.hv;
+  // To the first tile at or after place p (p < total); its number over all pairs.
+  __device__ __forceinline__ int seek(const PgaPlan& plan, int p) {
+    int lo = 0, hi = plan.B;  // the last request with places <= p: it is not empty
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (pre[mid] <= at) lo = mid;
+      if (plan.places(mid) <= p) lo = mid;
       else hi = mid;
     }
     b = lo;
-    enter(a);
-    const int in = tile - pre[b] * a.hv;
-    h = in / tiles;
-    t = in - h * tiles;
+    tiles = plan.pre[b + 1] - plan.pre[b];
+    const int in = p - plan.places(b), each = tiles + plan.extra;
+    h = in / each;
+    t = max(in - h * each - plan.extra, 0);
+    return plan.pre[b] * plan.hv + h * tiles + t;
   }
   // To the next tile; in the last pair it stays past the end (nobody looks).
   __device__ __forceinline__ void next(const PagedArgs& a, const int* pre) {
@@ -155,10 +173,11 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
   constexpr int SUB = T::KEYS / 16;
   constexpr int ROWS = 8 * NT;
   extern __shared__ __align__(1024) uint8_t pga_smem[];
-  __shared__ int scan_w[PGA_WARPS];
+  __shared__ int scan_w[2][PGA_WARPS];
   __shared__ uint32_t seen_mask[PGA_WARPS][PGA_STAGES];
   __shared__ int3 meta[PGA_WARPS];  // last piece goes on (1: begun in the share, 2: before it), its request and head tile
-  int* pre = reinterpret_cast<int*>(pga_smem + PGA_WARPS * PGA_STAGES * PGA_STAGE);  // [B + 1] tiles per head before a request
+  int* pre = reinterpret_cast<int*>(pga_smem + PGA_WARPS * PGA_STAGES * PGA_STAGE);
+  int* nz = pre + a.B + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_enter();
 
@@ -167,30 +186,42 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
     const int per = (a.B + PGA_THREADS - 1) / PGA_THREADS;
     const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
     bool bad = false;
-    int sum = 0;
+    int sum = 0, some = 0;
     for (int b = b0; b < b1; ++b) {
       const int n = (pga_request(a, b, &bad).seen + T::KEYS - 1) / T::KEYS;
       pre[b + 1] = n;
       sum += n;
+      some += n > 0;
     }
     if (bad && blockIdx.x == 0) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
-    int inc = sum;
+    int inc = sum, inn = some;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int u = __shfl_up_sync(0xffffffffu, inc, o);
-      if (lane >= o) inc += u;
+      const int u = __shfl_up_sync(0xffffffffu, inc, o), v = __shfl_up_sync(0xffffffffu, inn, o);
+      if (lane >= o) {
+        inc += u;
+        inn += v;
+      }
     }
-    if (lane == 31) scan_w[warp] = inc;
+    if (lane == 31) {
+      scan_w[0][warp] = inc;
+      scan_w[1][warp] = inn;
+    }
     __syncthreads();
-    int at = inc - sum;
+    int at = inc - sum, an = inn - some;
 #pragma unroll
     for (int w = 0; w < PGA_WARPS; ++w)
-      if (w < warp) at += scan_w[w];
+      if (w < warp) {
+        at += scan_w[0][w];
+        an += scan_w[1][w];
+      }
     for (int b = b0; b < b1; ++b) {
+      an += pre[b + 1] > 0;
       at += pre[b + 1];
       pre[b + 1] = at;
+      nz[b + 1] = an;
     }
-    if (tid == 0) pre[0] = 0;
+    if (tid == 0) pre[0] = nz[0] = 0;
     __syncthreads();
   }
   // requests that see nothing
@@ -199,9 +230,19 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
       uint4* o = reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(b) * a.hq * D);
       for (int i = tid; i < a.hq * D / 8; i += PGA_THREADS) o[i] = make_uint4(0, 0, 0, 0);
     }
-  const int64_t total = static_cast<int64_t>(pre[a.B]) * a.hv;
-  const int workers = gridDim.x * PGA_WARPS, me = blockIdx.x * PGA_WARPS + warp;
-  const int r0 = pga_share(total, workers, me), r1 = pga_share(total, workers, me + 1);
+  PgaPlan plan;
+  plan.pre = pre;
+  plan.nz = nz;
+  plan.B = a.B;
+  plan.hv = a.hv;
+  plan.extra = pre[a.B] * a.hv > static_cast<int>(gridDim.x) * PGA_WARPS ? a.extra : 0;
+  plan.divide(static_cast<int>(gridDim.x) * PGA_WARPS);
+  const int me = blockIdx.x * PGA_WARPS + warp;
+  // lane 0 seeks the start of this warp's share, lane 1 that of the next one's
+  PgaWalk<D> look;
+  const int from = plan.place(me + (lane & 1));
+  const int first = from < plan.total ? look.seek(plan, from) : pre[a.B] * a.hv;
+  const int r0 = __shfl_sync(0xffffffffu, first, 0), r1 = __shfl_sync(0xffffffffu, first, 1);
   const int gs = a.hq / a.hkv;
 
   uint8_t* ring = pga_smem + warp * PGA_STAGES * PGA_STAGE;
@@ -212,9 +253,11 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
 
   if (r0 < r1) {
     // ---- lookup, copy and use, each at its own tile
-    PgaWalk<D> look, use;
-    look.seek(a, pre, r0);
-    use = look;
+    look.b = __shfl_sync(0xffffffffu, look.b, 0);
+    look.h = __shfl_sync(0xffffffffu, look.h, 0);
+    look.t = __shfl_sync(0xffffffffu, look.t, 0);
+    look.enter(a);
+    PgaWalk<D> use = look;
     const int64_t row_elems = static_cast<int64_t>(a.hkv) * D;
     const int in_page = (1 << a.shift) - 1;
     int page = -1, off = 0, head = 0;
@@ -249,17 +292,6 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
     };
     const int n = r1 - r0;
     lookup();
-#pragma unroll
-    for (int s = 0; s < PGA_STAGES - 1; ++s) {
-      if (s < n) {
-        issue(s);
-        if (s + 1 < n) {
-          look.next(a, pre);
-          lookup();
-        }
-      }
-      asm volatile("cp.async.commit_group;" ::: "memory");
-    }
 
     uint32_t qf[NT][KS][2];
     float o[KS][NT][4], m[NT][2], l[NT][2];
@@ -305,18 +337,23 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
           }
         }
     };
-    begin_piece();
     bool began = use.t > 0;  // the piece's pair began in an earlier share
-    int slot = 0;
-    for (int i = 0; i < n; ++i) {
+    int slot = 0, fill = 0;
+    // the first steps only fill the ring (one copy of the code: a short share runs it cold)
+    for (int i = 1 - PGA_STAGES; i < n; ++i) {
       if (i + PGA_STAGES - 1 < n) {
-        issue(slot == 0 ? PGA_STAGES - 1 : slot - 1);
+        issue(fill);
+        fill = fill + 1 == PGA_STAGES ? 0 : fill + 1;
         if (i + PGA_STAGES < n) {
           look.next(a, pre);
           lookup();
         }
       }
       asm volatile("cp.async.commit_group;" ::: "memory");
+      if (i < 0) {
+        if (i == -1) begin_piece();
+        continue;
+      }
       asm volatile("cp.async.wait_group %0;" ::"n"(PGA_STAGES - 1) : "memory");
       __syncwarp();
       const uint32_t ks = ring_s + slot * PGA_STAGE, vs = ks + PGA_STAGE / 2;
@@ -429,64 +466,95 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
   }
   __syncthreads();
 
-  // ---- the block's pieces joined in key order, a warp per row: the last piece of a
-  // warp, the whole shares of the next ones, and the first piece of the one in which
-  // the pair ends. What began before the block or goes on after it leaves joined.
-  int4 info = make_int4(0, 0, 0, 0);
-  for (int w0 = 0; w0 < PGA_WARPS; ++w0) {
-    const int3 first = meta[w0];
-    if (first.x == 0 || (first.x == 2 && w0 > 0)) continue;
-    int w1 = w0 + 1;
-    while (w1 < PGA_WARPS && meta[w1].x == 2) ++w1;
-    const bool open_begin = first.x == 2, open_end = w1 == PGA_WARPS;
-    const int b = first.y, h = first.z, g = h / a.qt;
-    if (open_end && !open_begin) info = make_int4(1, b, h, 0);
-    for (int r = warp; r < ROWS; r += PGA_WARPS) {
-      const int q = (h - g * a.qt) * ROWS + r;
-      if (q >= gs) continue;
-      auto piece = [&](int i) -> const float* {
-        const int w = w0 + i;
-        return (w == w1 ? a.early + static_cast<int64_t>(blockIdx.x * PGA_WARPS + w) * ROWS * T::ROW
-                        : reinterpret_cast<const float*>(pga_smem + w * PGA_STAGES * PGA_STAGE)) +
-               r * T::ROW;
-      };
-      constexpr int C = D / 32;
-      const int n = (open_end ? w1 : w1 + 1) - w0;
-      float m = -INFINITY;
-      for (int i = 0; i < n; ++i) m = fmaxf(m, piece(i)[D]);
-      const float ref = m == -INFINITY ? 0.f : m;
-      float l = 0.f, o[C] = {};
-      for (int i = 0; i < n; ++i) {
-        const float* p = piece(i);
-        const float f = pga_ex2(p[D] - ref);
-        l = fmaf(p[D + 1], f, l);
+  // ---- the block's pieces joined in key order, a warp per row, in one walk over the
+  // warps: the last piece of a warp that goes on, the whole shares of the next ones, and
+  // the first piece of the one in which the pair ends. What began before the block or goes
+  // on after it leaves joined. All pieces are loaded ahead of the walk.
+  constexpr int C = D / 32;
+  int kind[PGA_WARPS];  // of a warp's last piece: 0 ends there, 1 begun in its share and goes on, 2 its whole share
 #pragma unroll
-        for (int c = 0; c < C; ++c) o[c] = fmaf(p[lane * C + c], f, o[c]);
+  for (int w = 0; w < PGA_WARPS; ++w) kind[w] = meta[w].x;
+#pragma unroll 1
+  for (int r = warp; r < ROWS; r += PGA_WARPS) {
+    float last[PGA_WARPS][C], early[PGA_WARPS][C];
+    float2 last_ml[PGA_WARPS], early_ml[PGA_WARPS];
+#pragma unroll
+    for (int w = 0; w < PGA_WARPS; ++w) {
+      if (kind[w] != 0) {
+        const float* p = reinterpret_cast<const float*>(pga_smem + w * PGA_STAGES * PGA_STAGE) + r * T::ROW;
+        last_ml[w] = *reinterpret_cast<const float2*>(p + D);
+#pragma unroll
+        for (int c = 0; c < C; ++c) last[w][c] = p[lane * C + c];
       }
+      if (w > 0 && kind[w - 1] != 0 && kind[w] != 2) {
+        const float* p = a.early + (static_cast<int64_t>(blockIdx.x * PGA_WARPS + w) * ROWS + r) * T::ROW;
+        early_ml[w] = *reinterpret_cast<const float2*>(p + D);
+#pragma unroll
+        for (int c = 0; c < C; ++c) early[w][c] = p[lane * C + c];
+      }
+    }
+    if (tid == 0) {
+      // a pair that begins here and ends in a later block
+      int4 info = make_int4(0, 0, 0, 0);
+      if (kind[PGA_WARPS - 1] != 0) {
+        int w0 = PGA_WARPS - 1;
+        while (w0 > 0 && kind[w0] == 2) --w0;
+        if (meta[w0].x == 1) {
+          info = make_int4(1, meta[w0].y, meta[w0].z, 0);
+          const int tiles = pre[info.y + 1] - pre[info.y];
+          const int end = plan.places(info.y) + (info.z + 1) * (tiles + plan.extra) - 1;
+          info.w = plan.holder(end) / PGA_WARPS;
+        }
+      }
+      a.info[blockIdx.x] = info;
+    }
+    float m = 0.f, l = 0.f, o[C];
+    int w0 = 0;  // where the chain began
+    auto add = [&](const float2& ml, const float (&v)[C]) {
+      const float to = fmaxf(m, ml.x), ref = to == -INFINITY ? 0.f : to;
+      const float f = pga_ex2(m - ref), e = pga_ex2(ml.x - ref);
+      m = to;
+      l = l * f + ml.y * e;
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] = o[c] * f + v[c] * e;
+    };
+    auto leave = [&](bool open_begin, bool open_end) {
       if (open_begin || open_end) {
         float* dst = part + ((open_begin ? 0 : ROWS) + r) * T::ROW;
 #pragma unroll
         for (int c = 0; c < C; ++c) dst[lane * C + c] = o[c];
-        if (lane == 0) {
-          dst[D] = m;
-          dst[D + 1] = l;
-        }
+        if (lane == 0) *reinterpret_cast<float2*>(dst + D) = make_float2(m, l);
       } else {
-        const float f = l != 0.f ? 1.f / l : 0.f;
+        const int b = meta[w0].y, h = meta[w0].z, g = a.qt == 1 ? h : h / a.qt, q = (h - g * a.qt) * ROWS + r;
+        if (q >= gs) return;
+        const float inv = l != 0.f ? 1.f / l : 0.f;
         uint32_t* dst =
             reinterpret_cast<uint32_t*>(a.out + (static_cast<int64_t>(b) * a.hq + g * gs + q) * D + lane * C);
 #pragma unroll
-        for (int c = 0; c < C; c += 2) dst[c / 2] = pack_bf16x2(o[c] * f, o[c + 1] * f);
+        for (int c = 0; c < C; c += 2) dst[c / 2] = pack_bf16x2(o[c] * inv, o[c + 1] * inv);
+      }
+    };
+    bool on = false;  // a chain goes on into warp w
+#pragma unroll
+    for (int w = 0; w < PGA_WARPS; ++w) {
+      if (on) {
+        if (kind[w] == 2) {
+          add(last_ml[w], last[w]);
+          continue;
+        }
+        add(early_ml[w], early[w]);
+        leave(w0 == 0 && kind[0] == 2, false);
+      }
+      on = kind[w] != 0;
+      if (on) {
+        w0 = w;
+        m = last_ml[w].x;
+        l = last_ml[w].y;
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = last[w][c];
       }
     }
-  }
-  if (tid == 0) {
-    if (info.x != 0) {
-      const int tiles = pre[info.y + 1] - pre[info.y];
-      const int last = pre[info.y] * a.hv + (info.z + 1) * tiles - 1;
-      info.w = pga_holder(total, workers, last) / PGA_WARPS;
-    }
-    a.info[blockIdx.x] = info;
+    if (on) leave(w0 == 0 && kind[0] == 2, true);
   }
 }
 
@@ -500,29 +568,43 @@ __global__ void __launch_bounds__(32 * PGM_WARPS) k_paged_join(PagedArgs a) {
   constexpr int ROWS = 8 * NT, PER = PGM_WARPS / ROWS, C = D / 32;
   __shared__ float so[PGM_WARPS][D + 2];
   pdl_enter();
-  const int4 info = a.info[blockIdx.x];
-  if (info.x == 0) return;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r = warp / PER, s = warp % PER;
-  const int gs = a.hq / a.hkv, g = info.z / a.qt, q = (info.z - g * a.qt) * ROWS + r;
-  const int n = info.w - static_cast<int>(blockIdx.x) + 1;
-  const int i0 = s * n / PER, i1 = (s + 1) * n / PER;
   auto piece = [&](int i) {
     return a.part + ((static_cast<int64_t>(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + r) * T::ROW;
   };
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 32) m = fmaxf(m, piece(i)[D]);
+  // the first 32 maxima and sums come with the pair's description, whether they are its or not
+  float2 ml = blockIdx.x + lane < gridDim.x ? *reinterpret_cast<const float2*>(piece(lane) + D) : make_float2(0.f, 0.f);
+  const int4 info = a.info[blockIdx.x];
+  if (info.x == 0) return;
+  const int gs = a.hq / a.hkv, g = info.z / a.qt, q = (info.z - g * a.qt) * ROWS + r;
+  const int n = info.w - static_cast<int>(blockIdx.x) + 1;
+  float m = lane < n ? ml.x : -INFINITY;
+  for (int i = lane + 32; i < n; i += 32) m = fmaxf(m, piece(i)[D]);
 #pragma unroll
   for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
   const float ref = m == -INFINITY ? 0.f : m;
   float l = 0.f, o[C] = {};
-#pragma unroll 8
-  for (int i = i0; i < i1; ++i) {
-    const float* p = piece(i);
-    const float f = pga_ex2(p[D] - ref);
-    l = fmaf(p[D + 1], f, l);
+  // pieces s, s + PER, ...: the loads of eight in flight together
+  for (int i0 = s; i0 < n; i0 += 8 * PER) {
+    float v[8][C];
 #pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = fmaf(p[lane * C + c], f, o[c]);
+    for (int k = 0; k < 8; ++k) {
+      const int i = i0 + k * PER;
+#pragma unroll
+      for (int c = 0; c < C; ++c) v[k][c] = i < n ? piece(i)[lane * C + c] : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int i = i0 + k * PER;
+      if (i >= n) break;
+      const float2 pm = i < 32 ? make_float2(__shfl_sync(0xffffffffu, ml.x, i), __shfl_sync(0xffffffffu, ml.y, i))
+                               : *reinterpret_cast<const float2*>(piece(i) + D);
+      const float f = pga_ex2(pm.x - ref);
+      l = fmaf(pm.y, f, l);
+#pragma unroll
+      for (int c = 0; c < C; ++c) o[c] = fmaf(v[k][c], f, o[c]);
+    }
   }
 #pragma unroll
   for (int c = 0; c < C; ++c) so[warp][lane * C + c] = o[c];
@@ -620,14 +702,15 @@ int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t B, const vo
   a.sl2 = (scale > 0.f ? scale : 1.f / sqrtf(static_cast<float>(D))) * 1.4426950408889634f;
   const int keys = D == 128 ? PgaTile<128>::KEYS : PgaTile<64>::KEYS;
   const int64_t most = B * ((max_pages * page_size + keys - 1) / keys) * a.hv;  // tiles, at most
-  DM_ARG_CHECK(most <= INT_MAX, "paged_attention: B * max_pages * page_size * heads is too large");
+  DM_ARG_CHECK(most + PGA_EXTRA * B * a.hv <= INT_MAX, "paged_attention: B * max_pages * page_size * heads is too large");
   const int grid = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(sm_count(), (most + PGA_WARPS - 1) / PGA_WARPS)));
   const size_t piece = static_cast<size_t>(rows) * (D + 4);
   a.early = static_cast<float*>(ws);
   a.part = a.early + static_cast<size_t>(grid) * PGA_WARPS * piece;
   a.info = reinterpret_cast<int4*>(a.part + static_cast<size_t>(grid) * 2 * piece);
+  a.extra = PGA_EXTRA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const size_t smem = static_cast<size_t>(PGA_WARPS) * PGA_STAGES * PGA_STAGE + (static_cast<size_t>(B) + 1) * sizeof(int);
+  const size_t smem = static_cast<size_t>(PGA_WARPS) * PGA_STAGES * PGA_STAGE + 2 * (static_cast<size_t>(B) + 1) * sizeof(int);
   auto go = [&](auto main, auto join) -> int {
     DM_CUDA_CHECK(cudaFuncSetAttribute(main, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
     DM_CUDA_CHECK(launch_pdl(main, dim3(grid), dim3(PGA_THREADS), smem, s, a));
