@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(32 * AN_WARPS) k_add_rmsnorm(AddNormArgs a, in
   constexpr int KEEP = NV > 0 ? NV : 1;
   __shared__ float red_s[2][AN_WARPS];
   __shared__ uint32_t red_m[2][AN_WARPS];
-  pdl_enter();
+  pdl_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int per_block = (blockDim.x >> 5) / warps;  // rows at a time: 1 where warps > 1
   const int in_row = threadIdx.x - (warp / warps) * warps * 32, step = warps * 32;
@@ -171,6 +171,7 @@ __global__ void __launch_bounds__(32 * AN_WARPS) k_add_rmsnorm(AddNormArgs a, in
     }
     if (a.scale != nullptr && in_row == 0) a.scale[t] = m / AN_MAX;
   }
+  pdl_trigger();
 }
 
 }  // namespace decomoe
@@ -217,8 +218,8 @@ extern "C" int decomoe_add_rmsnorm_q8(const void* x, const void* residual, const
   const int64_t want = warps > 1 ? T : (T + block - 1) / block;
   const int grid = static_cast<int>(std::min<int64_t>(want, static_cast<int64_t>(sm_count()) * 16));
   auto go = [&](auto kern) {
-    return launch_pdl(kern, dim3(grid), dim3(static_cast<unsigned>(32 * block)), 0, reinterpret_cast<cudaStream_t>(stream), a,
-                      warps);
+    return launch_pdl_late(kern, dim3(grid), dim3(static_cast<unsigned>(32 * block)), 0,
+                           reinterpret_cast<cudaStream_t>(stream), a, warps);
   };
   auto pick = [&](auto bf16) {
     constexpr bool B = decltype(bf16)::value;

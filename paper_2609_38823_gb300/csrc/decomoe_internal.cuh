@@ -85,6 +85,25 @@ inline cudaError_t launch_pdl(void (*kern)(KArgs...), dim3 grid, dim3 block, siz
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
+// The same whatever the grid's size, for kernels that call pdl_trigger() only when
+// they are done with their loads: the next kernel's blocks then come in as this one's
+// leave, instead of taking the places of those of its blocks that have not started.
+template <typename... KArgs, typename... Args>
+inline cudaError_t launch_pdl_late(void (*kern)(KArgs...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                                   Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = block;
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled(1) ? 1 : 0;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
+}
+
 // Internal entry points shared between translation units.
 // TMA map of a 2-D bf16 tensor [outer, inner] row-major; box = box_outer rows x
 // box_inner columns (64 -> 128-byte swizzle, 32 -> 64-byte swizzle), zero fill

@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(256)
     k_paged_append(const uint4* __restrict__ kn, int64_t ks, const uint4* __restrict__ vn, int64_t vs, int64_t N,
                    int vec, const int32_t* __restrict__ slot_map, uint4* __restrict__ kp, uint4* __restrict__ vp,
                    int64_t slots, int shift, int64_t page_vecs, int32_t* status) {
-  pdl_enter();
+  pdl_wait();
   const int64_t all = 2 * N * vec, step = static_cast<int64_t>(gridDim.x) * blockDim.x;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += step) {
     const int64_t row2 = i / vec;
@@ -170,6 +170,7 @@ __global__ void __launch_bounds__(256)
     if (row2 & 1) vp[at] = vn[r * vs + c];
     else kp[at] = kn[r * ks + c];
   }
+  pdl_trigger();
 }
 
 static bool ranges_overlap(const void* p, size_t n, const void* q, size_t m) {
@@ -247,7 +248,7 @@ int decomoe_paged_append(const void* k_new, int64_t k_row_stride, const void* v_
   const int vec = static_cast<int>(width * e / 16);
   const int64_t all = 2 * N * vec;
   const int grid = static_cast<int>(std::min<int64_t>((all + 255) / 256, static_cast<int64_t>(sm_count()) * 16));
-  DM_CUDA_CHECK(launch_pdl(k_paged_append, dim3(grid), dim3(256), 0, reinterpret_cast<cudaStream_t>(stream),
+  DM_CUDA_CHECK(launch_pdl_late(k_paged_append, dim3(grid), dim3(256), 0, reinterpret_cast<cudaStream_t>(stream),
                            static_cast<const uint4*>(k_new), k_row_stride * e / 16, static_cast<const uint4*>(v_new),
                            v_row_stride * e / 16, N, vec, slot_map, static_cast<uint4*>(k_pages),
                            static_cast<uint4*>(v_pages), num_pages * page_size,

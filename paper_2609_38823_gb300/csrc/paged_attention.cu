@@ -561,70 +561,85 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
 // Pairs that end in a later block than they begin in: block k joins the pair that
 // begins in block k of the launch before. A row's pieces are shared by several
 // warps, each with its loads in flight together, whose sums are then added in order.
-constexpr int PGM_WARPS = 32;
+// While the launch before is still running the blocks of this one, already on their
+// SMs, go through the same code once on whatever the workspace holds and store nothing:
+// the second time its instructions are there (loads past L1, which keeps nothing of the
+// first time).
+constexpr int PGM_WARPS = 16;
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * PGM_WARPS) k_paged_join(PagedArgs a) {
   using T = PgaTile<D>;
   constexpr int ROWS = 8 * NT, PER = PGM_WARPS / ROWS, C = D / 32;
   __shared__ float so[PGM_WARPS][D + 2];
-  pdl_enter();
+  pdl_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int r = warp / PER, s = warp % PER;
   auto piece = [&](int i) {
     return a.part + ((static_cast<int64_t>(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + r) * T::ROW;
   };
-  // the first 32 maxima and sums come with the pair's description, whether they are its or not
-  float2 ml = blockIdx.x + lane < gridDim.x ? *reinterpret_cast<const float2*>(piece(lane) + D) : make_float2(0.f, 0.f);
-  const int4 info = a.info[blockIdx.x];
-  if (info.x == 0) return;
-  const int gs = a.hq / a.hkv, g = info.z / a.qt, q = (info.z - g * a.qt) * ROWS + r;
-  const int n = info.w - static_cast<int>(blockIdx.x) + 1;
-  float m = lane < n ? ml.x : -INFINITY;
-  for (int i = lane + 32; i < n; i += 32) m = fmaxf(m, piece(i)[D]);
+#pragma unroll 1
+  for (int pass = 0; pass < 2; ++pass) {
+    if (pass == 1) pdl_wait();
+    // the first 32 maxima and sums come with the pair's description, whether they are its or not
+    const float2 ml = blockIdx.x + lane < gridDim.x ? __ldcg(reinterpret_cast<const float2*>(piece(lane) + D))
+                                                    : make_float2(0.f, 0.f);
+    int4 info = __ldcg(a.info + blockIdx.x);
+    if (pass == 0) info = make_int4(1, 0, 0, min(blockIdx.x + 1, gridDim.x - 1));
+    if (info.x == 0) return;
+    const int gs = a.hq / a.hkv, g = a.qt == 1 ? info.z : info.z / a.qt, q = (info.z - g * a.qt) * ROWS + r;
+    const int n = info.w - static_cast<int>(blockIdx.x) + 1;
+    float m = lane < n ? ml.x : -INFINITY;
+    for (int i = lane + 32; i < n; i += 32) m = fmaxf(m, __ldcg(piece(i) + D));
 #pragma unroll
-  for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f, o[C] = {};
-  // pieces s, s + PER, ...: the loads of eight in flight together
-  for (int i0 = s; i0 < n; i0 += 8 * PER) {
-    float v[8][C];
+    for (int w = 16; w > 0; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f, o[C] = {};
+    // pieces s, s + PER, ...: the loads of sixteen in flight together
+#pragma unroll 1
+    for (int i0 = s; i0 < n; i0 += 16 * PER) {
+      float v[16][C];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int i = i0 + k * PER;
+      for (int k = 0; k < 16; ++k) {
+        const int i = i0 + k * PER;
 #pragma unroll
-      for (int c = 0; c < C; ++c) v[k][c] = i < n ? piece(i)[lane * C + c] : 0.f;
+        for (int c = 0; c < C; ++c) v[k][c] = i < n ? __ldcg(piece(i) + lane * C + c) : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const int i = i0 + k * PER;
+        if (i >= n) break;
+        const float2 pm = i < 32 ? make_float2(__shfl_sync(0xffffffffu, ml.x, i), __shfl_sync(0xffffffffu, ml.y, i))
+                                 : __ldcg(reinterpret_cast<const float2*>(piece(i) + D));
+        const float f = pga_ex2(pm.x - ref);
+        l = fmaf(pm.y, f, l);
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] = fmaf(v[k][c], f, o[c]);
+      }
     }
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const int i = i0 + k * PER;
-      if (i >= n) break;
-      const float2 pm = i < 32 ? make_float2(__shfl_sync(0xffffffffu, ml.x, i), __shfl_sync(0xffffffffu, ml.y, i))
-                               : *reinterpret_cast<const float2*>(piece(i) + D);
-      const float f = pga_ex2(pm.x - ref);
-      l = fmaf(pm.y, f, l);
+    for (int c = 0; c < C; ++c) so[warp][lane * C + c] = o[c];
+    if (lane == 0) so[warp][D] = l;
+    __syncthreads();
+    if (s == 0 && q < gs) {
+      l = 0.f;
 #pragma unroll
-      for (int c = 0; c < C; ++c) o[c] = fmaf(v[k][c], f, o[c]);
+      for (int c = 0; c < C; ++c) o[c] = 0.f;
+#pragma unroll
+      for (int w = 0; w < PER; ++w) {
+        l += so[warp + w][D];
+#pragma unroll
+        for (int c = 0; c < C; ++c) o[c] += so[warp + w][lane * C + c];
+      }
+      const float f = l != 0.f ? 1.f / l : 0.f;
+      uint32_t* dst =
+          reinterpret_cast<uint32_t*>(a.out + (static_cast<int64_t>(info.y) * a.hq + g * gs + q) * D + lane * C);
+#pragma unroll
+      for (int c = 0; c < C; c += 2) {
+        const uint32_t two = pack_bf16x2(o[c] * f, o[c + 1] * f);
+        if (pass == 1) dst[c / 2] = two;
+      }
     }
-  }
-#pragma unroll
-  for (int c = 0; c < C; ++c) so[warp][lane * C + c] = o[c];
-  if (lane == 0) so[warp][D] = l;
-  __syncthreads();
-  if (s == 0 && q < gs) {
-    l = 0.f;
-#pragma unroll
-    for (int c = 0; c < C; ++c) o[c] = 0.f;
-#pragma unroll
-    for (int w = 0; w < PER; ++w) {
-      l += so[warp + w][D];
-#pragma unroll
-      for (int c = 0; c < C; ++c) o[c] += so[warp + w][lane * C + c];
-    }
-    const float f = l != 0.f ? 1.f / l : 0.f;
-    uint32_t* dst =
-        reinterpret_cast<uint32_t*>(a.out + (static_cast<int64_t>(info.y) * a.hq + g * gs + q) * D + lane * C);
-#pragma unroll
-    for (int c = 0; c < C; c += 2) dst[c / 2] = pack_bf16x2(o[c] * f, o[c + 1] * f);
+    __syncthreads();
   }
 }
 

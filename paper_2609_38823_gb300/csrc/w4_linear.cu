@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(32 * W4_DIRECT_WARPS) k_w4_direct(W4Args a) {
   constexpr int WORDS = GROUP / 32;  // words of a group of a weight row per lane
   using XV = std::conditional_t<E4M3, uint2, uint4>;
   __shared__ float red[W4_DIRECT_WARPS][NT * 128];
-  pdl_enter();
+  pdl_wait();
   const uint32_t mask = w4_const(E4M3 ? 0x03c003c0u : 0x00780078u);
   const uint32_t sixteen = w4_const(E4M3 ? 0x4c004c00u : 0x41804180u);
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, quad = lane & 3, row = lane >> 2;
@@ -213,6 +213,7 @@ __global__ void __launch_bounds__(32 * W4_DIRECT_WARPS) k_w4_direct(W4Args a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(s[i >> 1], fmaf(-24.f, sum[j][i & 1], c[j][i]), acc[j][i]);
   }
+  pdl_trigger();
 #pragma unroll
   for (int j = 0; j < NT; ++j)
     *reinterpret_cast<float4*>(&red[warp][(j * 32 + lane) * 4]) = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
@@ -575,7 +576,7 @@ static int w4_launch(W4Args a, cudaStream_t s) {
   a.tiles = (a.N + 15) / 16;
   const unsigned z = static_cast<unsigned>((a.T + 8 * NT - 1) / (8 * NT));
   if (a.N * a.K <= int64_t{1} << 25) {
-    DM_CUDA_CHECK(launch_pdl(k_w4_direct<E4M3, GROUP, NT>, dim3(static_cast<unsigned>(a.tiles), z),
+    DM_CUDA_CHECK(launch_pdl_late(k_w4_direct<E4M3, GROUP, NT>, dim3(static_cast<unsigned>(a.tiles), z),
                              dim3(32 * W4_DIRECT_WARPS), 0, s, a));
     return DECOMOE_OK;
   }
