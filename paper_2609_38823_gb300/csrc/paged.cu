@@ -149,26 +149,41 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_plan(PlanArgs a) {
 }
 
 // ------------------------------------------------------------------ append
-// One thread per 16 bytes of a key or value row: a plain scatter, bound by
-// bandwidth where there are many rows and by one round trip where there are few.
+// A plain scatter, bound by bandwidth where there are many rows and by one round trip
+// where there are few. 1 << LANES threads take a row of keys and the same of values,
+// with up to eight 16-byte loads of each thread in flight. 16384 rows of 1 KB twice: 12.0
+// us, 5.6 TB/s read and written; a thread per 16 bytes that divides to find its row 14.2.
+constexpr int APPEND_VECS = 4;  // of a thread and pool in flight
 __global__ void __launch_bounds__(256)
     k_paged_append(const uint4* __restrict__ kn, int64_t ks, const uint4* __restrict__ vn, int64_t vs, int64_t N,
-                   int vec, const int32_t* __restrict__ slot_map, uint4* __restrict__ kp, uint4* __restrict__ vp,
-                   int64_t slots, int shift, int64_t page_vecs, int32_t* status) {
+                   int vec, int lanes, const int32_t* __restrict__ slot_map, uint4* __restrict__ kp,
+                   uint4* __restrict__ vp, int64_t slots, int shift, int64_t page_vecs, int32_t* status) {
   pdl_wait();
-  const int64_t all = 2 * N * vec, step = static_cast<int64_t>(gridDim.x) * blockDim.x;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < all; i += step) {
-    const int64_t row2 = i / vec;
-    const int c = static_cast<int>(i - row2 * vec);
-    const int64_t r = row2 >> 1;
+  const int64_t r = (static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x) >> lanes;
+  const int c0 = threadIdx.x & ((1 << lanes) - 1), step = 1 << lanes;
+  if (r < N) {
     const int64_t s = slot_map[r];
-    if (s < 0 || s >= slots) {
-      if (s != -1) report_status(status, DECOMOE_ERR_BAD_INPUT);
-      continue;
+    if (s >= 0 && s < slots) {
+      const uint4 *k = kn + r * ks, *v = vn + r * vs;
+      const int64_t at = (s >> shift) * page_vecs + (s & ((int64_t{1} << shift) - 1)) * vec;
+      for (int c = c0; c < vec; c += APPEND_VECS * step) {
+        uint4 a[APPEND_VECS], b[APPEND_VECS];
+#pragma unroll
+        for (int i = 0; i < APPEND_VECS; ++i)
+          if (c + i * step < vec) {
+            a[i] = k[c + i * step];
+            b[i] = v[c + i * step];
+          }
+#pragma unroll
+        for (int i = 0; i < APPEND_VECS; ++i)
+          if (c + i * step < vec) {
+            kp[at + c + i * step] = a[i];
+            vp[at + c + i * step] = b[i];
+          }
+      }
+    } else if (s != -1 && c0 == 0) {
+      report_status(status, DECOMOE_ERR_BAD_INPUT);
     }
-    const int64_t at = (s >> shift) * page_vecs + (s & ((int64_t{1} << shift) - 1)) * vec + c;
-    if (row2 & 1) vp[at] = vn[r * vs + c];
-    else kp[at] = kn[r * ks + c];
   }
   pdl_trigger();
 }
@@ -246,13 +261,15 @@ int decomoe_paged_append(const void* k_new, int64_t k_row_stride, const void* v_
                    aligned16(v_pages),
                "paged_append: rows and strides must be 16-byte multiples, pointers 16-byte aligned");
   const int vec = static_cast<int>(width * e / 16);
-  const int64_t all = 2 * N * vec;
-  const int grid = static_cast<int>(std::min<int64_t>((all + 255) / 256, static_cast<int64_t>(sm_count()) * 16));
-  DM_CUDA_CHECK(launch_pdl_late(k_paged_append, dim3(grid), dim3(256), 0, reinterpret_cast<cudaStream_t>(stream),
-                           static_cast<const uint4*>(k_new), k_row_stride * e / 16, static_cast<const uint4*>(v_new),
-                           v_row_stride * e / 16, N, vec, slot_map, static_cast<uint4*>(k_pages),
-                           static_cast<uint4*>(v_pages), num_pages * page_size,
-                           __builtin_ctz(static_cast<unsigned>(page_size)), page_stride * e / 16, status_dev));
+  int lanes = 0;  // the least power of two that covers a row, at most a warp
+  while (lanes < 5 && (1 << lanes) < vec) ++lanes;
+  const int64_t grid = ((N << lanes) + 255) / 256;
+  DM_CUDA_CHECK(launch_pdl_late(k_paged_append, dim3(static_cast<unsigned>(grid)), dim3(256), 0,
+                                reinterpret_cast<cudaStream_t>(stream), static_cast<const uint4*>(k_new),
+                                k_row_stride * e / 16, static_cast<const uint4*>(v_new), v_row_stride * e / 16, N, vec,
+                                lanes, slot_map, static_cast<uint4*>(k_pages), static_cast<uint4*>(v_pages),
+                                num_pages * page_size, __builtin_ctz(static_cast<unsigned>(page_size)),
+                                page_stride * e / 16, status_dev));
   return DECOMOE_OK;
 }
 
