@@ -16,11 +16,12 @@
 // and picks the same pairs of x.
 //
 // Two kernels. Up to 2^25 weights the call is a chain of latencies: one block per 16
-// columns, rows of x read as they lie (k_w4_direct). Above, the weights' stream counts:
+// columns, rows of x read as they lie (k_w4_direct). Above (and for more than 16 rows by
+// many columns), the weights' stream counts:
 // rings of asynchronous copies per warp, x laid out once per block in shared memory
 // (k_w4_ring). Measured, bf16 rows, direct / ring, us: 5120 x 2048 T=1 4.3 / 4.9, T=8 4.7
 // / 6.1; 2048 x 4096 T=32 7.2 / 11.3; 9000 x 4096 T=1 7.8 / 7.0, T=8 10.7 / 8.8; 32001 x
-// 8192 T=1 47 / 32, T=8 56 / 36, T=32 188 / 85.
+// 8192 T=1 47 / 32, T=8 56 / 36, T=32 188 / 85; 12000 x 2048 T=8 6.8 / 7.4.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -112,7 +113,7 @@ __device__ __forceinline__ void w4_put(const W4Args& a, int64_t t, int64_t n, fl
   else static_cast<__nv_bfloat16*>(a.out)[t * a.N + n] = __float2bfloat16_rn(v);
 }
 
-// ------------------------------------------------------------------ up to 2^25 weights
+// ------------------------------------------------------------------ smaller matrices
 // Four bits put into the mantissa of a 16-bit float of value 16 (bits 3 to 6 in bf16,
 // 6 to 9 in fp16) make it the exact number 16 + q: a shift and a three-input logic
 // operation for two weights. 24 sum x leaves again, added up on the tensor cores too, as
@@ -229,7 +230,7 @@ __global__ void __launch_bounds__(32 * W4_DIRECT_WARPS) k_w4_direct(W4Args a) {
   }
 }
 
-// ------------------------------------------------------------------ above 2^25 weights
+// ------------------------------------------------------------------ larger matrices
 // The units that handle logic operations would be the bound with two of them for every
 // pair of weights. Four bits at the foot of a 16-bit float are the subnormal number
 // q times its smallest step (2^-133 in bf16, 2^-24 in fp16), the four bits above them
@@ -575,7 +576,10 @@ template <bool E4M3, int GROUP, int NT>
 static int w4_launch(W4Args a, cudaStream_t s) {
   a.tiles = (a.N + 15) / 16;
   const unsigned z = static_cast<unsigned>((a.T + 8 * NT - 1) / (8 * NT));
-  if (a.N * a.K <= int64_t{1} << 25) {
+  // (Above 16 rows x weighs as much as the weights where there are many columns, whatever
+  // their length: T=24, 29478 x 512 direct 19.2 / ring 12.1 us, 8000 x 2048 13.7 / 11.7; fewer
+  // columns 2000 x 8192 12.2 / 19.0.)
+  if (a.N * a.K <= int64_t{1} << 25 && (NT < 4 || a.N < 48 * static_cast<int64_t>(sm_count()))) {
     DM_CUDA_CHECK(launch_pdl_late(k_w4_direct<E4M3, GROUP, NT>, dim3(static_cast<unsigned>(a.tiles), z),
                              dim3(32 * W4_DIRECT_WARPS), 0, s, a));
     return DECOMOE_OK;
