@@ -120,7 +120,7 @@ __device__ __forceinline__ uint32_t pga_transpose(uint32_t v) {
   return r;
 }
 __device__ __forceinline__ void pga_mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile(
+  asm(
       "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -301,24 +301,32 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
       head = look.h / a.qt;
       if (want) page = a.table[look.b * a.max_pages + (p >> a.shift)];
     };
+    // places in a tile, the 16-byte pieces of row r exchanged by r's low three bits: of what
+    // this lane copies, and of its row of the operands of the two products
+    const uint32_t copy_at = (lane >> 2) * (2 * D) + (((lane & 3) ^ (lane >> 2)) << 4);
+    const uint32_t k_at = (lane & 15) * (2 * D) + (((lane >> 4) ^ (lane & 7)) << 4);
+    const uint32_t v_at = (((lane >> 4) << 3) + (lane & 7)) * (2 * D) + ((((lane >> 3) & 1) ^ (lane & 7)) << 4);
     auto issue = [&](int slot) {
       const bool there = want && page >= 0 && page < a.num_pages;
       if (want && !there) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
       const uint32_t mask = __ballot_sync(0xffffffffu, there);
       if (lane == 0) seen_mask[warp][slot] = mask;
+      // four lanes to a row, 64 bytes of eight rows at a time
+      constexpr int SETS = T::KEYS / 8, GROUPS = T::VECS / 4;
       const int64_t base = there ? page * a.page_stride + off * row_elems + static_cast<int64_t>(head) * D : -1;
-      constexpr int PER = 32 / T::VECS;  // rows per copy instruction
-      const int c = lane % T::VECS;
       const uint32_t stage = ring_s + slot * PGA_STAGE;
 #pragma unroll
-      for (int i = 0; i < T::KEYS / PER; ++i) {
-        const int row = i * PER + lane / T::VECS;
-        const int64_t at = __shfl_sync(0xffffffffu, base, row);
+      for (int i = 0; i < SETS; ++i) {
+        const int64_t at = __shfl_sync(0xffffffffu, base, i * 8 + (lane >> 2));
         const bool ok = at >= 0;
-        const int64_t e = ok ? at + c * 8 : 0;
-        const uint32_t dst = stage + row * (2 * D) + ((c ^ (row & 7)) << 4);
-        pga_copy(dst, a.k + e, ok);
-        pga_copy(dst + PGA_STAGE / 2, a.v + e, ok);
+        const int64_t e = (ok ? at : 0) + (lane & 3) * 8;
+        const __nv_bfloat16 *k = a.k + e, *v = a.v + e;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+          const uint32_t dst = stage + i * (8 * 2 * D) + (copy_at ^ (g << 6));
+          pga_copy(dst, k + g * 32, ok);
+          pga_copy(dst + PGA_STAGE / 2, v + g * 32, ok);
+        }
       }
     };
     const int n = r1 - r0;
@@ -391,14 +399,13 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
       const uint32_t mask = seen_mask[warp][slot];
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
-        float sc[NT][4] = {};
+        float sc[NT][4] = {}, odd[NT][4] = {};  // even and odd steps: two chains of products
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-          const int row = u * 16 + (lane & 15), c = 2 * s + (lane >> 4);
           uint32_t f[4];
-          pga_ldsm(ks + row * (2 * D) + ((c ^ (row & 7)) << 4), f);
+          pga_ldsm(ks + u * (16 * 2 * D) + (k_at ^ (s << 5)), f);
 #pragma unroll
-          for (int x = 0; x < NT; ++x) pga_mma(sc[x], f, qf[x][s][0], qf[x][s][1]);
+          for (int x = 0; x < NT; ++x) pga_mma(s & 1 ? odd[x] : sc[x], f, qf[x][s][0], qf[x][s][1]);
         }
         const bool lo = (mask >> (u * 16 + (lane >> 2))) & 1u, hi = (mask >> (u * 16 + 8 + (lane >> 2))) & 1u;
         uint32_t p[NT][2];
@@ -407,8 +414,8 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
           float mx[2];
 #pragma unroll
           for (int i2 = 0; i2 < 2; ++i2) {
-            sc[x][i2] = lo ? sc[x][i2] * a.sl2 : -INFINITY;
-            sc[x][i2 + 2] = hi ? sc[x][i2 + 2] * a.sl2 : -INFINITY;
+            sc[x][i2] = lo ? (sc[x][i2] + odd[x][i2]) * a.sl2 : -INFINITY;
+            sc[x][i2 + 2] = hi ? (sc[x][i2 + 2] + odd[x][i2 + 2]) * a.sl2 : -INFINITY;
             mx[i2] = fmaxf(sc[x][i2], sc[x][i2 + 2]);
           }
 #pragma unroll
@@ -444,9 +451,8 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
         }
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-          const int row = u * 16 + ((lane >> 4) << 3) + (lane & 7), c = 2 * s + ((lane >> 3) & 1);
           uint32_t f[4];
-          pga_ldsm_t(vs + row * (2 * D) + ((c ^ (row & 7)) << 4), f);
+          pga_ldsm_t(vs + u * (16 * 2 * D) + (v_at ^ (s << 5)), f);
 #pragma unroll
           for (int x = 0; x < NT; ++x) pga_mma(o[s][x], f, p[x][0], p[x][1]);
         }
