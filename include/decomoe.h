@@ -686,9 +686,12 @@ DECOMOE_API int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t
  * or DECOMOE_E4M3 with x_scale [T] fp32, one factor per row (as
  * decomoe_add_rmsnorm_q8 leaves them). out: [T, N] contiguous, out_dtype
  * DECOMOE_BF16 or DECOMOE_F32. Products are exact, sums of a group and over the
- * groups fp32, scales applied to whole group sums, one rounding at the end. For
- * decode sizes (the weights are read once per 32 rows); any T >= 0 and N >= 1
- * are right. x and w 16-byte aligned, x_stride a multiple of 16 bytes.
+ * groups fp32, scales applied to whole group sums, one rounding at the end. A row
+ * with a value that is not finite gives values that are not finite (NaN where the
+ * formula has an infinity), in that row alone; bf16 values of 2^121 and more may
+ * overflow in a group's sum. For decode sizes (the weights are read once per 32
+ * rows); any T up to 524280 and N >= 1 are right. K <= 2^26. x and w 16-byte aligned,
+ * x_stride a multiple of 16 bytes.
  * ------------------------------------------------------------------------ */
 DECOMOE_API int decomoe_add_rmsnorm_q8(const void* x, const void* residual, const void* weight, int64_t T, int d,
                                        float eps, int dtype, void* sum_out, void* y, void* y8, float* y8_scale,

@@ -23,7 +23,14 @@ namespace decomoe {
 // features by 8 queries, so that the 8 query heads of a KV head fill a tile (16
 // rows by 8 keys would leave half of each product empty). The accumulator of the
 // first becomes the operand of the second by two 8x8 transposes (movmatrix), and
-// a query's maximum, sum and outputs all lie in the same lanes.
+// a query's maximum, sum and outputs all lie in the same lanes. Scores, maxima, sums and
+// outputs are fp32; the weights are rounded to bf16 as operands of the second product
+// (the values are bf16, and the two must be of one type): 2^-9 of a weight at most,
+// relative errors of 0.0022 after the output's own rounding, which alone gives 0.0017.
+//
+// Bound: the stream of keys and values. 96 requests of 2000 to 16385 rows (545 MB) 95 us:
+// 6.2 TB/s but for the 3 us before the first tile and the 4 us of the joins. One request of
+// 2049 rows 8.6 us, all of it latency.
 constexpr int PGA_WARPS = 8;
 constexpr int PGA_THREADS = 32 * PGA_WARPS;
 constexpr int PGA_STAGES = 3;

@@ -74,6 +74,24 @@ class PagedCache:
         self.cached.copy_(self.seq_len)
         self.head.copy_(self.head_next)
 
+    def release(self, request: int) -> None:
+        """The request is over: its pages go back to the list (those of a hidden block
+        that were given back before must be -1 in the table). Reads its length on the
+        host, between steps."""
+        n = -(-int(self.cached[request]) // self.page_size)
+        pages = self.table[request, :n]
+        pages = pages[pages >= 0]
+        head = int(self.head) - pages.numel()
+        if head < 0:
+            raise ValueError("more pages released than were given out")
+        self.free[head:head + pages.numel()] = pages
+        self.head.fill_(head)
+        self.table[request] = -1
+        self.cached[request] = 0
+        self.seq_len[request] = 0
+        self.hide_begin[request] = 0
+        self.hide_count[:, request] = 0
+
     def hide(self, request: int, begin: int, count: int, from_layer: int) -> None:
         """Leave rows [begin, begin + count) of a request out of the attention of
         every layer from `from_layer` on (its visual block after the exit)."""

@@ -146,3 +146,25 @@ def test_quantize_w4():
     # half a step of 1/7 of the group's largest value; the scale itself rounded to 8 bits
     top = w.view(10, 4, 64).abs().amax(-1).repeat_interleave(64, 1).double().numpy()
     assert (np.abs(got - w.double().numpy()) <= top * (0.5 / 7 + 2.0 ** -8) + 1e-12).all() and (got[3, :64] == 0).all()
+
+
+def test_pages_of_finished_requests_are_given_out_again():
+    cache = PagedCache(L, 3, pages=30, page_size=8, max_pages=12, hkv=HKV, d=D)
+    lens = [40, 17, 64]
+    _prompt(cache, lens, 1)
+    first = [set(cache.table[b][cache.table[b] >= 0].tolist()) for b in range(3)]
+    assert [len(p) for p in first] == [5, 3, 8]
+    cache.hide(2, 4, 10, from_layer=0)
+    cache.release(2)
+    cache.release(0)
+    assert cache.cached.tolist() == [0, 17, 0] and int(cache.head) == 3 and int(cache.hide_count.sum()) == 0
+    slots = torch.empty(95, dtype=torch.int32, device=DEV)
+    cache.plan(torch.tensor([95, 0, 0], dtype=torch.int32, device=DEV), slots)
+    cache.advance()
+    assert dm.decomoe_read_status(cache.status) == dm.DECOMOE_OK
+    again = set(cache.table[0][cache.table[0] >= 0].tolist())
+    assert len(again) == 12 and not again & first[1] and first[0] | first[2] > again - set(range(16, 30))
+    assert len(set(slots.tolist())) == 95
+    with pytest.raises(ValueError):
+        cache.head.zero_()
+        cache.release(0)

@@ -230,6 +230,14 @@ def test_attention_ragged_batches():
     _check([1] * 700, 8, 8, 64, 8, seed=4)
 
 
+def test_attention_most_requests():
+    # as many requests as a call takes: some long, many short, every fifth empty
+    r = np.random.default_rng(8)
+    lens = [0 if b % 5 == 0 else int(r.integers(1, 30)) for b in range(4096)]
+    lens[77], lens[4000] = 3000, 900
+    _check(lens, 2, 1, 64, 16, seed=9)
+
+
 def test_attention_empty_requests():
     for lens in ([0], [0, 0, 0], [0, 5, 0], [0] * 200):
         out, _ = _check(lens, 8, 2, 128, 16, seed=1)
@@ -401,6 +409,48 @@ def test_steps_in_a_captured_graph():
             k, v = (f64(torch.stack([r[j] for r in held[b]])) for j in (0, 1))
             assert_close_out(f64(out[b]), O.attention(f64(q[b:b + 1]), k, v)[0], 2 * BF16_REL_L2, 2 * BF16_MAX_ABS)
     assert dm.decomoe_read_status(status) == dm.DECOMOE_OK
+
+
+def test_programmatic_launches_change_no_bits():
+    """Plan, append, attention, norm and 4-bit products in a row, with and without
+    programmatic launches, several times over changing inputs."""
+    lens = [300, 41, 0, 1200]
+    q, kp, vp, dk, dv, table, dq = _case(lens, 8, 2, 128, 16, 12)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    w = torch.randint(0, 256, (8 * 128, 128), generator=g, device=DEV, dtype=torch.uint8)
+    w_big = torch.randint(0, 256, (20000, 1024), generator=g, device=DEV, dtype=torch.uint8)
+    ws, ws_big = (torch.full((n, k // 128), 0.01, dtype=torch.bfloat16, device=DEV) for n, k in ((8 * 128, 256), (20000, 2048)))
+    runs = []
+    for on in (True, False, True):
+        dm.decomoe_set_pdl(on)
+        try:
+            k, v = dk.clone(), dv.clone()
+            h = torch.randn(4, 256, generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).to(torch.bfloat16)
+            x8, sc = torch.empty(4, 256, dtype=torch.float8_e4m3fn, device=DEV), torch.empty(4, device=DEV)
+            qq, out = torch.empty(4, 8, 128, dtype=torch.bfloat16, device=DEV), torch.empty(4, 8, 128, dtype=torch.bfloat16, device=DEV)
+            big = torch.empty(4, 20000, dtype=torch.bfloat16, device=DEV)
+            aws = dm.workspace(dm.decomoe_paged_attention_workspace_bytes(4, 8, 2, 128), DEV)
+            cached, fresh = _i32([n - 1 if n else 0 for n in lens]), _i32([1 if n else 0 for n in lens])
+            n_len, start, slots = _i32([0] * 4), _i32([0] * 5), _i32([0] * 4)
+            t = table.to(DEV)
+            got = []
+            for i in range(5):
+                dm.decomoe_add_rmsnorm_q8(h, None, None, y8=x8, y8_scale=sc)
+                dm.decomoe_w4_linear(x8, w, ws, qq.view(4, -1), x_scale=sc)
+                dm.decomoe_paged_plan(cached, fresh, 16, _i32([0]), t, n_len, start, slots)
+                dm.decomoe_paged_append(qq[:, :2], qq[:, 2:4], slots, k, v)
+                dm.decomoe_paged_attention(qq, k, v, t, n_len, out, aws)
+                dm.decomoe_w4_linear(out.view(4, -1)[:, :256], w, ws, qq.view(4, -1))
+                dm.decomoe_w4_linear(torch.cat([out.view(4, -1)] * 2, 1), w_big, ws_big, big)
+                dm.decomoe_add_rmsnorm_q8(qq.view(4, -1)[:, :256].contiguous(), h, None, h)
+                got += [out.clone(), big.clone(), h.clone()]
+            torch.cuda.synchronize()
+            runs.append(got)
+        finally:
+            dm.decomoe_set_pdl(True)
+    for other in runs[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], other))
+    assert all(torch.isfinite(t.float()).all() for t in runs[0])
 
 
 def test_refusals():
