@@ -30,8 +30,7 @@
 
 namespace decomoe {
 
-constexpr int W4_DIRECT_WARPS = 8;
-__host__ __device__ constexpr int w4_stages(int NT) { return NT == 4 ? 3 : 4; }  // units of a warp's ring
+__host__ __device__ constexpr int w4_stages(int NT) { return NT > 2 ? 3 : 4; }  // units of a warp's ring
 constexpr int W4_UNIT = 256;            // values of k of a unit (128 bytes of a weight row)
 constexpr int W4_STAGE = 16 * 128;      // bytes of a unit of 16 columns
 constexpr int W4_WARPS = 16;            // warps of a ring block, at most
@@ -135,12 +134,12 @@ __device__ __forceinline__ uint32_t w4_pair(uint32_t w, int i, uint32_t mask, ui
 }
 
 // One block per 16 columns (blockIdx.x) and 8 NT rows (blockIdx.y); its warps take the
-// groups g = warp, warp + 8, ... and their sums are added in warp order.
-template <bool E4M3, int GROUP, int NT>
-__global__ void __launch_bounds__(32 * W4_DIRECT_WARPS) k_w4_direct(W4Args a) {
+// groups g = warp, warp + WARPS, ... and their sums are added in warp order.
+template <bool E4M3, int GROUP, int NT, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) k_w4_direct(W4Args a) {
   constexpr int WORDS = GROUP / 32;  // words of a group of a weight row per lane
   using XV = std::conditional_t<E4M3, uint2, uint4>;
-  __shared__ float red[W4_DIRECT_WARPS][NT * 128];
+  __shared__ float red[WARPS][NT * 128];
   pdl_wait();
   const uint32_t mask = w4_const(E4M3 ? 0x03c003c0u : 0x00780078u);
   const uint32_t sixteen = w4_const(E4M3 ? 0x4c004c00u : 0x41804180u);
@@ -167,7 +166,7 @@ __global__ void __launch_bounds__(32 * W4_DIRECT_WARPS) k_w4_direct(W4Args a) {
   const uint32_t one = E4M3 ? 0x3c003c00u : 0x3f803f80u;
   const uint32_t ones[4] = {one, one, one, one};
 #pragma unroll 2
-  for (int g = warp; g < a.groups; g += W4_DIRECT_WARPS) {
+  for (int g = warp; g < a.groups; g += WARPS) {
     uint32_t q[2][WORDS];
     float s[2];
 #pragma unroll
@@ -220,12 +219,12 @@ __global__ void __launch_bounds__(32 * W4_DIRECT_WARPS) k_w4_direct(W4Args a) {
     *reinterpret_cast<float4*>(&red[warp][(j * 32 + lane) * 4]) = make_float4(acc[j][0], acc[j][1], acc[j][2], acc[j][3]);
   __syncthreads();
   // a column (consecutive threads) of a row each
-  for (int i = threadIdx.x; i < 16 * 8 * NT; i += 32 * W4_DIRECT_WARPS) {
+  for (int i = threadIdx.x; i < 16 * 8 * NT; i += 32 * WARPS) {
     const int n = i & 15, t = i >> 4;
     if (t0 + t >= a.T) continue;
     float v = 0.f;
 #pragma unroll
-    for (int k = 0; k < W4_DIRECT_WARPS; ++k) v += red[k][w4_place<NT>(t, n)];
+    for (int k = 0; k < WARPS; ++k) v += red[k][w4_place<NT>(t, n)];
     w4_put(a, t0 + t, n0 + n, v);
   }
 }
@@ -579,9 +578,15 @@ static int w4_launch(W4Args a, cudaStream_t s) {
   // (Above 16 rows x weighs as much as the weights where there are many columns, whatever
   // their length: T=24, 29478 x 512 direct 19.2 / ring 12.1 us, 8000 x 2048 13.7 / 11.7; fewer
   // columns 2000 x 8192 12.2 / 19.0.)
-  if (a.N * a.K <= int64_t{1} << 25 && (NT < 4 || a.N < 48 * static_cast<int64_t>(sm_count()))) {
-    DM_CUDA_CHECK(launch_pdl_late(k_w4_direct<E4M3, GROUP, NT>, dim3(static_cast<unsigned>(a.tiles), z),
-                             dim3(32 * W4_DIRECT_WARPS), 0, s, a));
+  if (a.N * a.K <= int64_t{1} << 25 && (NT < 3 || a.N < 48 * static_cast<int64_t>(sm_count()))) {
+    const dim3 grid(static_cast<unsigned>(a.tiles), z);
+    // Sixteen warps a block where every block has an SM to itself and every warp at least
+    // two groups: 2048 x 4096 T=1 4.2 -> 3.3 us, T=17 6.9 -> 5.6; not where blocks share SMs
+    // (5120 x 2048 T=1 3.4, with sixteen 4.9) or k is short (700 x 1920 T=17 3.7, 4.1).
+    if (a.tiles <= sm_count() && a.groups >= 32)
+      DM_CUDA_CHECK(launch_pdl_late(k_w4_direct<E4M3, GROUP, NT, 16>, grid, dim3(512), 0, s, a));
+    else
+      DM_CUDA_CHECK(launch_pdl_late(k_w4_direct<E4M3, GROUP, NT, 8>, grid, dim3(256), 0, s, a));
     return DECOMOE_OK;
   }
   const int units = (a.K + W4_UNIT - 1) / W4_UNIT;
@@ -664,6 +669,7 @@ extern "C" int decomoe_w4_linear(const void* x, int x_dtype, int64_t x_stride, c
     constexpr int G = decltype(grp)::value;
     if (T <= 8) return w4_launch<E, G, 1>(a, s);
     if (T <= 16) return w4_launch<E, G, 2>(a, s);
+    if (T <= 24) return w4_launch<E, G, 3>(a, s);
     return w4_launch<E, G, 4>(a, s);
   };
   auto by_group = [&](auto e4m3) -> int {
