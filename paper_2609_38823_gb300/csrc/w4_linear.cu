@@ -21,7 +21,7 @@
 // rings of asynchronous copies per warp, x laid out once per block in shared memory
 // (k_w4_ring). Measured, bf16 rows, direct / ring, us: 5120 x 2048 T=1 4.3 / 4.9, T=8 4.7
 // / 6.1; 2048 x 4096 T=32 7.2 / 11.3; 9000 x 4096 T=1 7.8 / 7.0, T=8 10.7 / 8.8; 32001 x
-// 8192 T=1 47 / 32, T=8 56 / 36, T=32 188 / 85; 12000 x 2048 T=8 6.8 / 7.4.
+// 8192 T=1 47 / 30, T=8 56 / 35, T=32 188 / 85; 12000 x 2048 T=8 6.8 / 7.4.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -30,7 +30,7 @@
 
 namespace decomoe {
 
-__host__ __device__ constexpr int w4_stages(int NT) { return NT > 2 ? 3 : 4; }  // units of a warp's ring
+constexpr int W4_STAGES = 3;            // units of a warp's ring (with four less of x is staged at a time: 36 us for 35)
 constexpr int W4_UNIT = 256;            // values of k of a unit (128 bytes of a weight row)
 constexpr int W4_STAGE = 16 * 128;      // bytes of a unit of 16 columns
 constexpr int W4_WARPS = 16;            // warps of a ring block, at most
@@ -269,7 +269,7 @@ __device__ __forceinline__ float w4_ld_cluster(uint32_t addr, int rank) {
 // 128-byte pieces of 16 rows, on through the tile's end; no block-wide step but at a
 // tile's end). The sums are added over the warps of a block, then over the blocks of
 // the cluster through distributed shared memory, both in the order of k.
-// 32001 x 8192, T=1: 32 us, 4.3 TB/s; T=8 36 us; the same stream without any product 24.7 us.
+// 32001 x 8192, T=1: 30 us, 4.6 TB/s; T=8 35 us; the same stream without any product 24.7 us.
 // At T=32 (85 us) the reads of x from shared memory bound it: every warp reads all of x for
 // 16 columns.
 template <bool E4M3, int GROUP, int NT>
@@ -277,13 +277,12 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
   constexpr int WORDS = GROUP / 32;            // words of a group of a weight row per lane
   constexpr int GU = W4_UNIT / GROUP;          // groups of a unit
   constexpr int SREG = GU == 8 ? 2 : 1;        // scales of a weight row per lane and unit
-  constexpr int STAGES = w4_stages(NT);
   constexpr int TILE = NT * 128;               // floats of a warp's accumulators
   constexpr int XE = E4M3 ? 1 : 2;             // bytes of a value of x
   constexpr int XW = NT * 32;                  // 16-byte places of a word of a group of x
   using XV = std::conditional_t<E4M3, uint2, uint4>;
   extern __shared__ __align__(128) uint8_t w4_smem[];
-  const uint32_t xf_at = a.wm * a.wk * (STAGES * W4_STAGE);  // x: [chunk groups][WORDS][NT][32 lanes] uint4
+  const uint32_t xf_at = a.wm * a.wk * (W4_STAGES * W4_STAGE);  // x: [chunk groups][WORDS][NT][32 lanes] uint4
   const uint32_t xo_at = xf_at + a.chunk * (GU * WORDS * XW * 16);  // [chunk groups][8 NT] float2: step of the sums, -8 sum x
   uint4* xf = reinterpret_cast<uint4*>(w4_smem + xf_at);
   float2* xoff = reinterpret_cast<float2*>(w4_smem + xo_at);
@@ -303,7 +302,7 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
   const int steps = units > slice ? (units - slice + a.wk - 1) / a.wk : 0;
   const int64_t tile_step = static_cast<int64_t>(gridDim.y) * a.wm;
   const uint32_t kb = static_cast<uint32_t>(a.K / 2);
-  const uint32_t ring = warp * (STAGES * W4_STAGE), ring_s = smem_u32(w4_smem) + ring;
+  const uint32_t ring = warp * (W4_STAGES * W4_STAGE), ring_s = smem_u32(w4_smem) + ring;
   // rows of 128 bytes; the 16-byte pieces of row r are exchanged by the reverse of r's
   // low three bits, which spreads the reads of every group size over all banks
   auto swz = [](int r) { return ((r & 1) << 2) | (r & 2) | ((r >> 2) & 1); };
@@ -341,10 +340,10 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    pslot = pslot + 1 == STAGES ? 0 : pslot + 1;
+    pslot = pslot + 1 == W4_STAGES ? 0 : pslot + 1;
   };
 #pragma unroll
-  for (int i = 0; i < STAGES - 1; ++i) issue();
+  for (int i = 0; i < W4_STAGES - 1; ++i) issue();
 
   // ---- x: units [u0, u0 + n) of this block's; a thread takes what one lane of a quad
   // reads of a row of a group, the four of them in consecutive threads
@@ -468,7 +467,7 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
       uint32_t xg = static_cast<uint32_t>((slice + step * a.wk - c0) * GU);  // first group, from the chunk's
       auto unit = [&](uint32_t (&s)[2][SREG]) {
         issue();
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+        asm volatile("cp.async.wait_group %0;" ::"n"(W4_STAGES - 1) : "memory");
         __syncwarp();
         const uint32_t wq = ring + slot * W4_STAGE;
         const int left = groups - (slice + step * a.wk) * GU;  // the last unit may be cut short
@@ -519,7 +518,7 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
           }
         }
         __syncwarp();
-        slot = slot + 1 == STAGES ? 0 : slot + 1;
+        slot = slot + 1 == W4_STAGES ? 0 : slot + 1;
         scales(s, step + 2);
       };
 #pragma unroll 1
@@ -605,7 +604,7 @@ static int w4_launch(W4Args a, cudaStream_t s) {
   const int part = (units + ks - 1) / ks;
   a.wk = std::max(1, std::min(W4_WARPS / a.wm, part));
   const int warps = a.wm * a.wk;
-  const size_t fixed = static_cast<size_t>(warps) * (w4_stages(NT) * W4_STAGE + NT * 512);
+  const size_t fixed = static_cast<size_t>(warps) * (W4_STAGES * W4_STAGE + NT * 512);
   a.chunk = static_cast<int>(std::min<size_t>(part, (W4_SMEM - fixed) / per_unit));
   const size_t smem = fixed + a.chunk * per_unit;
   cudaLaunchConfig_t cfg = {};
