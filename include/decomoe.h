@@ -637,8 +637,9 @@ DECOMOE_API int decomoe_attention(const void* q, int64_t n, const void* k_cache,
  * give what the formula gives, in their own request and KV head; rows past the
  * length or hidden never reach a result.
  * D is 64 or 128, Hq a multiple of Hkv, pointers and strides multiples of 16
- * bytes. A length beyond max_pages * page_size is cut there, and a page outside
- * the pool counts as hidden; both mark DECOMOE_ERR_BAD_INPUT.
+ * bytes, max_pages * page_size <= 2^31 - 32. A length beyond max_pages * page_size
+ * is cut there, and a page outside the pool counts as hidden; both mark
+ * DECOMOE_ERR_BAD_INPUT. A negative hide_begin or hide_count counts as 0.
  * The visible rows of all requests are divided evenly over the SMs; a request
  * cut by that leaves partial rows in the workspace, which a second small launch
  * joins in key order. Deterministic: the same call gives the same bits, but the

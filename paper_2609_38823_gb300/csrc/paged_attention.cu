@@ -715,8 +715,9 @@ int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t B, const vo
                "paged_attention: page_size must be a power of two");
   DM_ARG_CHECK(num_pages >= 0 && num_pages <= INT_MAX / page_size,
                "paged_attention: num_pages * page_size must be below 2^31");
-  DM_ARG_CHECK(max_pages >= 0 && max_pages <= INT_MAX / page_size,
-               "paged_attention: max_pages * page_size must be below 2^31");
+  // a length rounded up to a tile of (at most) 32 keys is counted in 32 bits
+  DM_ARG_CHECK(max_pages >= 0 && max_pages <= (INT_MAX - 31) / page_size,
+               "paged_attention: max_pages * page_size must be at most 2^31 - 32");
   DM_ARG_CHECK(page_stride >= static_cast<int64_t>(page_size) * Hkv * D && page_stride % 8 == 0,
                "paged_attention: page_stride must be at least page_size * Hkv * D and a multiple of 8");
   DM_ARG_CHECK(q_stride >= static_cast<int64_t>(Hq) * D && q_stride % 8 == 0,

@@ -69,6 +69,14 @@ def test_attention_arguments():
     assert L.decomoe_paged_attention_workspace_bytes(4, 48, 4, 128) > L.decomoe_paged_attention_workspace_bytes(4, 32, 4, 128)
 
 
+@pytest.mark.parametrize("ps,max_pages", [(16, 2 ** 27 - 1), (1, 2 ** 31 - 1), (1, 2 ** 31 - 31)])
+def test_attention_refuses_a_table_whose_last_tile_passes_32_bits(ps, max_pages):
+    """A length of max_pages * page_size, rounded up to a tile of 32 keys, has to fit 32 bits."""
+    args = (P, 64, 1, P, P, 8, ps, ps * 64, P, max_pages, P, None, None, 1, 1, 64, 0.0, P, P, 1 << 30, None, None)
+    assert dm.lib().decomoe_paged_attention(*args) == dm.DECOMOE_ERR_INVALID_ARG
+    assert b"max_pages" in dm.lib().decomoe_last_error()
+
+
 def test_dense_arguments():
     L = dm.lib()
 
