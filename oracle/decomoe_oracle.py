@@ -536,7 +536,8 @@ def paged_attention(q, k_pages, v_pages, table, seq_len, hide_begin=None, hide_c
     ps, Hkv = k_pages.shape[1], k_pages.shape[2]
     out = np.zeros((B, Hq, D), F64)
     for b in range(B):
-        h0, h1 = (0, 0) if hide_begin is None else (int(hide_begin[b]), int(hide_begin[b]) + max(int(hide_count[b]), 0))
+        h0 = 0 if hide_begin is None else max(int(hide_begin[b]), 0)
+        h1 = h0 + (0 if hide_count is None else max(int(hide_count[b]), 0))
         rows = [j for j in range(int(seq_len[b])) if not h0 <= j < h1]
         if not rows:
             continue
