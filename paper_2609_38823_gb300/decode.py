@@ -39,7 +39,11 @@ def quantize_w4(w: torch.Tensor, group: int = 128):
 
 class PagedCache:
     """Keys and values of `layers` layers for up to `requests` requests in
-    `pages` pages of `page_size` rows, bf16. `max_pages` bounds a request."""
+    `pages` pages of `page_size` rows, bf16. `max_pages` bounds a request.
+
+    `active` [requests] says which slots a decode step adds a row to (1) and which it
+    leaves alone (0: no request, or one that waits). All do at the start; a released slot
+    does not until rows are planned for it again."""
 
     def __init__(self, layers: int, requests: int, pages: int, page_size: int, max_pages: int, hkv: int, d: int,
                  device="cuda"):
@@ -52,6 +56,7 @@ class PagedCache:
         self.head, self.head_next = torch.zeros(1, **i32), torch.zeros(1, **i32)
         self.cached, self.seq_len = torch.zeros(requests, **i32), torch.zeros(requests, **i32)
         self.row_start = torch.zeros(requests + 1, **i32)
+        self.active = torch.ones(requests, **i32)
         self.hide_begin = torch.zeros(requests, **i32)
         self.hide_count = torch.zeros(layers, requests, **i32)
         self.status = torch.zeros(1, **i32)
@@ -64,8 +69,14 @@ class PagedCache:
 
     def plan(self, fresh: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
         """Pages, slots [N] and positions [N] of the rows that this step adds
-        (fresh [requests]); seq_len then counts them. Repeating it before
-        ``advance`` changes nothing."""
+        (fresh [requests]); seq_len then counts them. Rows are numbered request after
+        request, over those that add some. Repeating it before ``advance`` changes
+        nothing."""
+        self.active.logical_or_(fresh > 0)
+        self.plan_rows(fresh, slots, positions)
+
+    def plan_rows(self, fresh: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
+        """``plan`` without a look at `active`: what a decode step calls."""
         decomoe_paged_plan(self.cached, fresh, self.page_size, self.free, self.table, self.seq_len, self.row_start, slots,
                            positions, free_head=self.head, free_head_out=self.head_next, status=self.status)
 
@@ -89,6 +100,7 @@ class PagedCache:
         self.table[request] = -1
         self.cached[request] = 0
         self.seq_len[request] = 0
+        self.active[request] = 0
         self.hide_begin[request] = 0
         self.hide_count[:, request] = 0
 
@@ -111,7 +123,10 @@ class DecodeLayer:
 
 
 class DecodeStep:
-    """One new token for each of B requests through all layers."""
+    """One new token for each of B requests through all layers. `fresh` [B] (the
+    cache's `active`) says which of them have one: a slot of 0 adds no row and takes no
+    page, its slot and position are -1, and what its row of the hidden states holds is carried
+    through the layers without a meaning."""
 
     def __init__(self, layers: Sequence[DecodeLayer], cache: PagedCache, B: int, hq: int, k: int, eps: float = 1e-6,
                  rotate: Optional[Callable[[torch.Tensor, torch.Tensor, torch.Tensor], None]] = None):
@@ -122,8 +137,11 @@ class DecodeStep:
         m = layers[0].w_down.shape[2]
         dev = cache.pool.device
         bf = dict(dtype=torch.bfloat16, device=dev)
-        self.fresh = torch.ones(B, dtype=torch.int32, device=dev)
-        self.slots, self.positions = (torch.empty(B, dtype=torch.int32, device=dev) for _ in range(2))
+        self.fresh = cache.active
+        # slots and positions as the plan numbers rows (live requests alone), and by request
+        self.rows, self.idle = torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B, dtype=torch.bool, device=dev)
+        self.packed, self.placed = (torch.empty(2, B, dtype=torch.int32, device=dev) for _ in range(2))
+        self.slots, self.positions = self.placed
         self.x8 = torch.empty(B, d, dtype=torch.float8_e4m3fn, device=dev)
         self.x8_scale = torch.empty(B, dtype=torch.float32, device=dev)
         self.qkv = torch.empty(B, hq + 2 * hkv, D, **bf)
@@ -139,7 +157,12 @@ class DecodeStep:
         last layer. trace(l, step, h_in, h_out), if given, is called after each
         layer's launches are queued (the buffers are reused by later layers)."""
         c = self.cache
-        c.plan(self.fresh, self.slots, self.positions)
+        # one row at most for each request, so that row_start[b] <= b stays inside the rows
+        torch.clamp(self.fresh, 0, 1, out=self.rows)
+        c.plan_rows(self.rows, *self.packed)
+        torch.index_select(self.packed, 1, c.row_start[:-1], out=self.placed)
+        torch.eq(self.rows, 0, out=self.idle)
+        self.placed.masked_fill_(self.idle, -1)
         h = h0
         for l, w in enumerate(self.layers):
             out = self.h[l & 1]
