@@ -6,11 +6,11 @@
 // The weights are read once and bound the call (half a byte per product of up to
 // 32 rows), so what matters is few instructions per weight and many bytes in
 // flight. Products run on the tensor cores (mma.m16n8k16, fp32 accumulate) with
-// 16 columns n as the rows of the product and 8 rows t as its columns; rows in bf16
-// take bf16 products, rows in e4m3 fp16 ones (every e4m3 value is exact there), so
-// that every product is exact. Weights become operands without a conversion, by
-// their place among the bits of a 16-bit float, with an offset that leaves again with
-// the group's sum of x. The order of k inside a product is free as long as both
+// 16 columns n as the rows of the product and 8 rows t as its columns, on bf16 or fp16
+// operands that hold the values of x and of the weights as they are, so that every
+// product is exact. Weights become operands without a conversion, by their place among the
+// bits of a 16-bit float, and less their offset: in the larger kernel at once, in the
+// smaller one with the group's sum of x. The order of k inside a product is free as long as both
 // operands agree: lane l of a quad takes the l-th quarter of a group of a weight row
 // (one 16-byte load of a group of 128), a word of which holds four pairs (k, k + 4),
 // and picks the same pairs of x.
@@ -20,8 +20,8 @@
 // many columns), the weights' stream counts:
 // rings of asynchronous copies per warp, x laid out once per block in shared memory
 // (k_w4_ring). Measured, bf16 rows, direct / ring, us: 5120 x 2048 T=1 4.3 / 4.9, T=8 4.7
-// / 6.1; 2048 x 4096 T=32 7.2 / 11.3; 9000 x 4096 T=1 7.8 / 7.0, T=8 10.7 / 8.8; 32001 x
-// 8192 T=1 47 / 30, T=8 56 / 35, T=32 188 / 85; 12000 x 2048 T=8 6.8 / 7.4.
+// / 6.1; 2048 x 4096 T=32 7.2 / 11.3; 9000 x 4096 T=1 7.8 / 7.0, T=8 10.7 / 8.3; 32001 x
+// 8192 T=1 47 / 31, T=8 56 / 35, T=32 188 / 79; 12000 x 2048 T=8 6.8 / 6.8.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -30,7 +30,7 @@
 
 namespace decomoe {
 
-constexpr int W4_STAGES = 3;            // units of a warp's ring (with four less of x is staged at a time: 36 us for 35)
+constexpr int W4_STAGES = 3;            // units of a warp's ring (with four less of x is staged at a time: T=32 82 us for 79)
 constexpr int W4_UNIT = 256;            // values of k of a unit (128 bytes of a weight row)
 constexpr int W4_STAGE = 16 * 128;      // bytes of a unit of 16 columns
 constexpr int W4_WARPS = 16;            // warps of a ring block, at most
@@ -61,16 +61,10 @@ __device__ __forceinline__ void w4_mma(float (&c)[4], const uint32_t (&a)[4], ui
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-template <bool E4M3>
-__device__ __forceinline__ void w4_mma0(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  if constexpr (E4M3)
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
-        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-  else
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
-        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+__device__ __forceinline__ void w4_mma0(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {  // bf16
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
 // Eight consecutive values of a row of x as four pairs (k, k + 4).
@@ -231,20 +225,27 @@ __global__ void __launch_bounds__(32 * WARPS) k_w4_direct(W4Args a) {
 
 // ------------------------------------------------------------------ larger matrices
 // The units that handle logic operations would be the bound with two of them for every
-// pair of weights. Four bits at the foot of a 16-bit float are the subnormal number
-// q times its smallest step (2^-133 in bf16, 2^-24 in fp16), the four bits above them
-// 16 q steps, both exact, so that a mask makes two operands and one shift serves four.
-// The values of x that meet the upper bits are divided by 16; in bf16 the rows are also
-// raised by 2^96 (less where a group holds values of 2^31 or more), which keeps the
-// products away from fp32's own subnormals, and the factor comes off each group's sum. The
-// offset leaves with 8 sum x, added up as the rows are laid out.
-__device__ __forceinline__ uint32_t w4_scale_bf16(uint32_t v, int e) {  // two bf16 times 2^e, exact where it does not overflow
-  const __nv_bfloat162 f = __bfloat162bfloat162(__ushort_as_bfloat16(static_cast<unsigned short>((127 + e) << 7)));
-  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v), f);
+// pair of weights. Four bits at the foot of a bf16 number are the subnormal number
+// q 2^-133, the four bits above them 16 q 2^-133, both exact, and one multiply-add of two
+// numbers makes (q - 8) / 64 of either, so that a mask and a multiply-add give two operands
+// and one shift serves a word of eight. The rows are laid out times 64, rows in e4m3 as
+// bf16, which holds their values too; every step is exact.
+constexpr float W4_RAISE = 64.f;
+__device__ __forceinline__ uint32_t w4_raise(uint32_t v) {  // two bf16, exact below 2^122 (infinite from there)
+  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v), __float2bfloat162_rn(W4_RAISE));
   return *reinterpret_cast<const uint32_t*>(&r);
 }
-__device__ __forceinline__ uint32_t w4_sixteenth(uint32_t v) {  // of two fp16
-  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&v), __half2half2(__ushort_as_half(0x2c00)));
+__device__ __forceinline__ uint32_t w4_raise_fp16(uint32_t v) {  // two fp16 that were e4m3, to bf16
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
+  return pack_bf16x2(f.x * W4_RAISE, f.y * W4_RAISE);
+}
+// The lowest four bits (UP: the next four) of either half of w as weights over 64.
+template <bool UP>
+__device__ __forceinline__ uint32_t w4_weights(uint32_t w) {
+  const uint32_t bits = w & (UP ? 0x00f000f0u : 0x000f000fu);
+  const __nv_bfloat162 f = __bfloat162bfloat162(__ushort_as_bfloat16(UP ? 0x7d00 : 0x7f00));  // 2^123, 2^127
+  const __nv_bfloat162 o = __bfloat162bfloat162(__ushort_as_bfloat16(0xbe00));                // -2^-3
+  const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162*>(&bits), f, o);
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 __device__ __forceinline__ void w4_cluster_sync() {
@@ -269,8 +270,8 @@ __device__ __forceinline__ float w4_ld_cluster(uint32_t addr, int rank) {
 // 128-byte pieces of 16 rows, on through the tile's end; no block-wide step but at a
 // tile's end). The sums are added over the warps of a block, then over the blocks of
 // the cluster through distributed shared memory, both in the order of k.
-// 32001 x 8192, T=1: 30 us, 4.6 TB/s; T=8 35 us; the same stream without any product 24.7 us.
-// At T=32 (85 us) the reads of x from shared memory bound it: every warp reads all of x for
+// 32001 x 8192, T=1: 31 us, 4.4 TB/s; T=8 35 us; the same stream without any product 24.7 us.
+// At T=32 (79 us) the reads of x from shared memory bound it: every warp reads all of x for
 // 16 columns.
 template <bool E4M3, int GROUP, int NT>
 __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
@@ -283,10 +284,8 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
   using XV = std::conditional_t<E4M3, uint2, uint4>;
   extern __shared__ __align__(128) uint8_t w4_smem[];
   const uint32_t xf_at = a.wm * a.wk * (W4_STAGES * W4_STAGE);  // x: [chunk groups][WORDS][NT][32 lanes] uint4
-  const uint32_t xo_at = xf_at + a.chunk * (GU * WORDS * XW * 16);  // [chunk groups][8 NT] float2: step of the sums, -8 sum x
   uint4* xf = reinterpret_cast<uint4*>(w4_smem + xf_at);
-  float2* xoff = reinterpret_cast<float2*>(w4_smem + xo_at);
-  float* red = reinterpret_cast<float*>(xoff + a.chunk * (GU * 8 * NT));  // [warps][NT][32][4]
+  float* red = reinterpret_cast<float*>(xf + a.chunk * (GU * WORDS * XW));  // [warps][NT][32][4]
   pdl_enter();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, quad = lane & 3, row = lane >> 2;
   const int slice = warp / a.wm, wm = warp - slice * a.wm;
@@ -373,48 +372,14 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int i = i0 + u * blockDim.x;
-        if (i - tid >= pieces) break;
-        W4X p[WORDS];
-        float sum = 0.f;
-        uint32_t top = 0;  // largest |x|, as bits
+        if (i >= pieces) break;
+        const int at = gs[u] * (WORDS * XW) + (rs[u] >> 3) * 32 + (rs[u] & 7) * 4 + (i & 3);
 #pragma unroll
         for (int e = 0; e < WORDS; ++e) {
-          p[e] = w4_x(v[u][e]);
+          W4X p = w4_x(v[u][e]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if constexpr (E4M3) {
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&p[e].p[k]));
-              sum += f.x + f.y;
-              p[e].p[k] = k & 1 ? w4_sixteenth(p[e].p[k]) : p[e].p[k];
-            } else {
-              sum += bf16_lo(p[e].p[k]) + bf16_hi(p[e].p[k]);
-              top = max(top, max(p[e].p[k] & 0x7fffu, (p[e].p[k] >> 16) & 0x7fffu));
-            }
-          }
-        }
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        float step = 16777216.f;  // 2^24
-        if constexpr (!E4M3) {
-          int up = 96;
-          if (__any_sync(0xffffffffu, top >= (158u << 7))) {
-            // |x| 2^up stays below 2^127 (what is not finite stays so); fp32 itself ends
-            // before sums of values of 2^121 do
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            up -= min(max(static_cast<int>(top >> 7) - 157, 0), 90);
-          }
-#pragma unroll
-          for (int e = 0; e < WORDS; ++e)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) p[e].p[k] = w4_scale_bf16(p[e].p[k], k & 1 ? up - 4 : up);
-          step = __uint_as_float(static_cast<uint32_t>(127 + 133 - up) << 23);  // 2^(133 - up)
-        }
-        if (i < pieces) {
-          const int at = gs[u] * (WORDS * XW) + (rs[u] >> 3) * 32 + (rs[u] & 7) * 4 + (i & 3);
-#pragma unroll
-          for (int e = 0; e < WORDS; ++e) xf[at + e * XW] = make_uint4(p[e].p[0], p[e].p[1], p[e].p[2], p[e].p[3]);
-          if ((i & 3) == 0) xoff[gs[u] * (8 * NT) + rs[u]] = make_float2(step, -8.f * sum);
+          for (int k = 0; k < 4; ++k) p.p[k] = E4M3 ? w4_raise_fp16(p.p[k]) : w4_raise(p.p[k]);
+          xf[at + e * XW] = make_uint4(p.p[0], p.p[1], p.p[2], p.p[3]);
         }
       }
     }
@@ -493,14 +458,14 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
 #pragma unroll
           for (int word = 0; word < WORDS; ++word) {
             const uint32_t q0 = q[0][word], q1 = q[1][word], h0 = q0 >> 8, h1 = q1 >> 8;
-            const uint32_t f0[4] = {q0 & 0x000f000fu, q1 & 0x000f000fu, q0 & 0x00f000f0u, q1 & 0x00f000f0u};
-            const uint32_t f1[4] = {h0 & 0x000f000fu, h1 & 0x000f000fu, h0 & 0x00f000f0u, h1 & 0x00f000f0u};
+            const uint32_t f0[4] = {w4_weights<false>(q0), w4_weights<false>(q1), w4_weights<true>(q0), w4_weights<true>(q1)};
+            const uint32_t f1[4] = {w4_weights<false>(h0), w4_weights<false>(h1), w4_weights<true>(h0), w4_weights<true>(h1)};
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
               const uint4 xp = *reinterpret_cast<const uint4*>(w4_smem + (xl[j] + xb + word * (XW * 16)));
-              if (word == 0) w4_mma0<E4M3>(c[j], f0, xp.x, xp.y);
-              else w4_mma<E4M3>(c[j], f0, xp.x, xp.y);
-              w4_mma<E4M3>(c[j], f1, xp.z, xp.w);
+              if (word == 0) w4_mma0(c[j], f0, xp.x, xp.y);
+              else w4_mma<false>(c[j], f0, xp.x, xp.y);
+              w4_mma<false>(c[j], f1, xp.z, xp.w);
             }
           }
           float f[2];
@@ -508,14 +473,9 @@ __global__ void __launch_bounds__(32 * W4_WARPS, 1) k_w4_ring(W4Args a) {
           for (int i = 0; i < 2; ++i)
             f[i] = __uint_as_float(__shfl_sync(0xffffffffu, s[i][gg >> 2], (lane & ~3) + (gg & 3)) << 16);
 #pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            const float4 o = *reinterpret_cast<const float4*>(w4_smem + (xo_at + quad * 16 + (xg + gg) * (64 * NT) + j * 64));
+          for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              acc[j][2 * i] = fmaf(f[i], fmaf(c[j][2 * i], o.x, o.y), acc[j][2 * i]);
-              acc[j][2 * i + 1] = fmaf(f[i], fmaf(c[j][2 * i + 1], o.z, o.w), acc[j][2 * i + 1]);
-            }
-          }
+            for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(f[i >> 1], c[j][i], acc[j][i]);
         }
         __syncwarp();
         slot = slot + 1 == W4_STAGES ? 0 : slot + 1;
@@ -589,7 +549,7 @@ static int w4_launch(W4Args a, cudaStream_t s) {
     return DECOMOE_OK;
   }
   const int units = (a.K + W4_UNIT - 1) / W4_UNIT;
-  const size_t per_unit = NT * 32 * 16 * (W4_UNIT / 32) + NT * 8 * (W4_UNIT / GROUP) * sizeof(float2);
+  const size_t per_unit = NT * 32 * 16 * (W4_UNIT / 32);
   const int64_t sms = sm_count();
   // Two blocks share k where x is large beside the columns, so that each lays out half of it
   // and twice as many columns use it: 9000 x 4096 T=32 24.6 -> 20.6 us, T=13 12.9 -> 11.9;

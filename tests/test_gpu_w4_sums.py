@@ -1,0 +1,67 @@
+"""Sums of the products with 4-bit weights against 64 bits, bounded by the formula's own
+terms |x (q - 8) scale|: rows near the foot of bf16's range. Sizes of either kernel."""
+import pytest
+import torch
+
+import paper_2609_38823_gb300 as dm
+
+pytestmark = pytest.mark.gpu
+DEV = torch.device("cuda")
+BF16, F32 = torch.bfloat16, torch.float32
+SMALL, LARGE = (300, 1024), (17000, 2048)  # N, K
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    import __graft_entry__
+
+    __graft_entry__.build()
+    dm.lib()
+
+
+def _weights(N, K, group, seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    w = torch.randint(0, 256, (N, K // 2), generator=g, device=DEV, dtype=torch.uint8)
+    return w, (torch.rand(N, K // group, generator=g, device=DEV) * 0.02 - 0.005).to(BF16)
+
+
+def _check(x, w, ws, xs=None):
+    """A product is exact; a group's at most eight matrix products of 16 terms each lose at most 2^-22
+    of the magnitudes added so far (fp32, alignment included), 2^-19 of all terms, the sums over groups and warps
+    less than that again at these sizes: 2^-18 of the terms. Below fp32's normal numbers
+    each of fewer than K roundings loses at most 2^-149. Then the output's own rounding."""
+    T, K = x.shape
+    N, groups = ws.shape
+    out = torch.full((T, N), 5.0, dtype=F32, device=DEV)
+    dm.decomoe_w4_linear(x, w, ws, out, x_scale=xs)
+    x64 = x.double() * (1.0 if xs is None else xs.double()[:, None])
+    for n in range(0, N, 4096):
+        b = w[n:n + 4096].int()
+        full = (torch.stack([b % 16, b // 16], -1).flatten(1).double() - 8) * ws[n:n + 4096].double().repeat_interleave(K // groups, 1)
+        ref, terms = x64 @ full.t(), x64.abs() @ full.abs().t()
+        err = (out[:, n:n + 4096].double() - ref).abs()
+        bound = 2.0 ** -23 * ref.abs() + 2.0 ** -18 * terms + K * 2.0 ** -149
+        assert (err <= bound).all(), (n, float((err / bound).max()))
+    return out
+
+
+@pytest.mark.parametrize("N,K", [SMALL, LARGE])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("T", [1, 8, 11, 24, 30])
+def test_small_rows(N, K, group, T):
+    w, ws = _weights(N, K, group, T)
+    g = torch.Generator(device=DEV).manual_seed(T)
+    x = torch.randn(T, K, generator=g, device=DEV)
+    for e in (-95, -110, -122):
+        _check((x * 2.0 ** e).to(BF16), w, ws)
+
+
+@pytest.mark.parametrize("N,K", [SMALL, LARGE])
+def test_rows_of_every_size_side_by_side(N, K):
+    w, ws = _weights(N, K, 64, 5)
+    e = torch.tensor([0, -60, -95, -110, -122, 60, 100, 115], device=DEV)
+    x = torch.randn(8, K, device=DEV) * 2.0 ** e.double()[:, None]
+    _check(x.to(BF16), w, ws)
+    # and group by group
+    f = 2.0 ** e[(torch.arange(K, device=DEV) // 64) % 8].double()
+    _check((torch.randn(3, K, device=DEV) * f).to(BF16), w, ws)
