@@ -686,11 +686,12 @@ DECOMOE_API int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t
  * x: [T, K] rows x_stride elements apart, x_dtype DECOMOE_BF16 (x_scale NULL)
  * or DECOMOE_E4M3 with x_scale [T] fp32, one factor per row (as
  * decomoe_add_rmsnorm_q8 leaves them). out: [T, N] contiguous, out_dtype
- * DECOMOE_BF16 or DECOMOE_F32. Products are exact, sums of a group and over the
- * groups fp32, scales applied to whole group sums, one rounding at the end. A row
- * with a value that is not finite gives values that are not finite (NaN where the
- * formula has an infinity), in that row alone; bf16 values of 2^121 and more may
- * overflow in a group's sum. For decode sizes (the weights are read once per 32
+ * DECOMOE_BF16 or DECOMOE_F32. Products x (q - 8) are exact (a weight of zero adds
+ * nothing, however large its x), sums of a group and over the groups fp32, scales
+ * applied to whole group sums, one rounding at the end: what the sums lose goes by
+ * the sum of |x (q - 8) scale|. A row with a value that is not finite gives values that
+ * are not finite, in that row alone; bf16 values of 2^121 and more may overflow in a
+ * group's sum. For decode sizes (the weights are read once per 32
  * rows); any T up to 524280 and N >= 1 are right. K <= 2^26. x and w 16-byte aligned,
  * x_stride a multiple of 16 bytes.
  * ------------------------------------------------------------------------ */

@@ -9,19 +9,18 @@
 // 16 columns n as the rows of the product and 8 rows t as its columns, on bf16 or fp16
 // operands that hold the values of x and of the weights as they are, so that every
 // product is exact. Weights become operands without a conversion, by their place among the
-// bits of a 16-bit float, and less their offset: in the larger kernel at once, in the
-// smaller one with the group's sum of x. The order of k inside a product is free as long as both
+// bits of a 16-bit float, and less their offset at once. The order of k inside a product is free as long as both
 // operands agree: lane l of a quad takes the l-th quarter of a group of a weight row
 // (one 16-byte load of a group of 128), a word of which holds four pairs (k, k + 4),
 // and picks the same pairs of x.
 //
 // Two kernels. Up to 2^25 weights the call is a chain of latencies: one block per 16
-// columns, rows of x read as they lie (k_w4_direct). Above (and for more than 16 rows by
+// columns, rows of x read as they lie (k_w4_direct). Above (and for more than 8 or 16 rows by
 // many columns), the weights' stream counts:
 // rings of asynchronous copies per warp, x laid out once per block in shared memory
-// (k_w4_ring). Measured, bf16 rows, direct / ring, us: 5120 x 2048 T=1 4.3 / 4.9, T=8 4.7
-// / 6.1; 2048 x 4096 T=32 7.2 / 11.3; 9000 x 4096 T=1 7.8 / 7.0, T=8 10.7 / 8.3; 32001 x
-// 8192 T=1 47 / 31, T=8 56 / 35, T=32 188 / 79; 12000 x 2048 T=8 6.8 / 6.8.
+// (k_w4_ring). Measured, bf16 rows, direct / ring, us: 5120 x 2048 T=1 3.2 / 4.9, T=8 3.9
+// / 5.5; 2048 x 4096 T=32 6.5 / 10.3; 12000 x 2048 T=8 7.4 / 6.8; 9000 x 4096 T=1 5.9 / 7.0,
+// T=8 7.9 / 8.3, T=13 16.2 / 11.3; 32001 x 8192 T=1 38 / 31, T=8 56 / 35, T=32 181 / 79.
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -108,29 +107,39 @@ __device__ __forceinline__ void w4_put(const W4Args& a, int64_t t, int64_t n, fl
 
 // ------------------------------------------------------------------ smaller matrices
 // Four bits put into the mantissa of a 16-bit float of value 16 (bits 3 to 6 in bf16,
-// 6 to 9 in fp16) make it the exact number 16 + q: a shift and a three-input logic
-// operation for two weights. 24 sum x leaves again, added up on the tensor cores too, as
-// the product of the rows with ones; the difference is at most six times smaller
-// than what it is taken from, in fp32.
+// 6 to 9 in fp16) make it the exact number 16 + q, and less 24 the exact weight q - 8: a shift,
+// a three-input logic operation and an addition for two weights. (An offset left in the
+// weights, to be taken off a group's sum, would leave there the rounding of large
+// values of x that meet the code of zero.)
 __device__ __forceinline__ uint32_t w4_const(uint32_t v) {  // a constant that stays in a register
   uint32_t r;
   asm volatile("mov.b32 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-// Pair i (weights i and i + 4) of a word of eight, as two floats 16 + q.
+// Pair i (weights i and i + 4) of a word of eight, as two floats q - 8.
 template <bool E4M3>
 __device__ __forceinline__ uint32_t w4_pair(uint32_t w, int i, uint32_t mask, uint32_t sixteen) {
   const int sh = (E4M3 ? 6 : 3) - 4 * i;
   const uint32_t s = sh >= 0 ? w << sh : w >> -sh;
   uint32_t r;
   asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(r) : "r"(s), "r"(mask), "r"(sixteen));  // (s & mask) | sixteen
-  return r;
+  if constexpr (E4M3) {
+    const __half2 d = __hadd2(*reinterpret_cast<const __half2*>(&r), __half2half2(__ushort_as_half(0xce00)));  // -24
+    return *reinterpret_cast<const uint32_t*>(&d);
+  } else {
+    const __nv_bfloat162 d = __hadd2(*reinterpret_cast<const __nv_bfloat162*>(&r),
+                                     __bfloat162bfloat162(__ushort_as_bfloat16(0xc1c0)));  // -24
+    return *reinterpret_cast<const uint32_t*>(&d);
+  }
 }
 
 // One block per 16 columns (blockIdx.x) and 8 NT rows (blockIdx.y); its warps take the
-// groups g = warp, warp + WARPS, ... and their sums are added in warp order.
+// groups g = warp, warp + WARPS, ... and their sums are added in warp order. (Groups of 32 are
+// little work each: asked for one block per SM, the compiler keeps more of their loads in
+// flight. 4149 x 4960 T=1 6.3 -> 4.9 us, T=32 15.9 -> 9.9; with larger groups fewer blocks
+// then fit an SM, 5000 x 4096 by 128 T=1 4.6 -> 5.1, T=8 6.4 -> 7.4.)
 template <bool E4M3, int GROUP, int NT, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS) k_w4_direct(W4Args a) {
+__global__ void __launch_bounds__(32 * WARPS, GROUP == 32 ? 1 : 0) k_w4_direct(W4Args a) {
   constexpr int WORDS = GROUP / 32;  // words of a group of a weight row per lane
   using XV = std::conditional_t<E4M3, uint2, uint4>;
   __shared__ float red[WARPS][NT * 128];
@@ -157,8 +166,6 @@ __global__ void __launch_bounds__(32 * WARPS) k_w4_direct(W4Args a) {
            ((has[j] ? t0 + j * 8 + row : 0) * a.x_stride + quad * (8 * WORDS)) * (E4M3 ? 1 : 2);
   }
   float acc[NT][4] = {};
-  const uint32_t one = E4M3 ? 0x3c003c00u : 0x3f803f80u;
-  const uint32_t ones[4] = {one, one, one, one};
 #pragma unroll 2
   for (int g = warp; g < a.groups; g += WARPS) {
     uint32_t q[2][WORDS];
@@ -184,7 +191,7 @@ __global__ void __launch_bounds__(32 * WARPS) k_w4_direct(W4Args a) {
       for (int u = 0; u < WORDS; ++u)
         xv[j][u] = has[j] ? __ldg(reinterpret_cast<const XV*>(x[j] + static_cast<int64_t>(g) * GROUP * (E4M3 ? 1 : 2)) + u)
                           : XV{};
-    float c[NT][4] = {}, sum[NT][4] = {};
+    float c[NT][4] = {};
 #pragma unroll
     for (int u = 0; u < WORDS; ++u) {
       W4X xp[NT];
@@ -196,16 +203,13 @@ __global__ void __launch_bounds__(32 * WARPS) k_w4_direct(W4Args a) {
                                w4_pair<E4M3>(q[0][u], 2 * h + 1, mask, sixteen),
                                w4_pair<E4M3>(q[1][u], 2 * h + 1, mask, sixteen)};
 #pragma unroll
-        for (int j = 0; j < NT; ++j) {
-          w4_mma<E4M3>(c[j], f, xp[j].p[2 * h], xp[j].p[2 * h + 1]);
-          w4_mma<E4M3>(sum[j], ones, xp[j].p[2 * h], xp[j].p[2 * h + 1]);
-        }
+        for (int j = 0; j < NT; ++j) w4_mma<E4M3>(c[j], f, xp[j].p[2 * h], xp[j].p[2 * h + 1]);
       }
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(s[i >> 1], fmaf(-24.f, sum[j][i & 1], c[j][i]), acc[j][i]);
+      for (int i = 0; i < 4; ++i) acc[j][i] = fmaf(s[i >> 1], c[j][i], acc[j][i]);
   }
   pdl_trigger();
 #pragma unroll
@@ -534,14 +538,15 @@ template <bool E4M3, int GROUP, int NT>
 static int w4_launch(W4Args a, cudaStream_t s) {
   a.tiles = (a.N + 15) / 16;
   const unsigned z = static_cast<unsigned>((a.T + 8 * NT - 1) / (8 * NT));
-  // (Above 16 rows x weighs as much as the weights where there are many columns, whatever
-  // their length: T=24, 29478 x 512 direct 19.2 / ring 12.1 us, 8000 x 2048 13.7 / 11.7; fewer
-  // columns 2000 x 8192 12.2 / 19.0.)
-  if (a.N * a.K <= int64_t{1} << 25 && (NT < 3 || a.N < 48 * static_cast<int64_t>(sm_count()))) {
+  // (With more rows x weighs as much as the weights where there are many columns, whatever
+  // their length: direct / ring, bf16 T=24 29478 x 512 12.9 / 10.2 us, 8000 x 2048 10.3 / 9.6, T=13
+  // 9.0 / 7.3; fewer columns 2000 x 8192 T=24 10.0 / 12.8. Rows in e4m3 weigh half of it: T=13
+  // 8000 x 2048 6.2 / 7.2.)
+  if (a.N * a.K <= int64_t{1} << 25 && (NT < (E4M3 ? 3 : 2) || a.N < 48 * static_cast<int64_t>(sm_count()))) {
     const dim3 grid(static_cast<unsigned>(a.tiles), z);
     // Sixteen warps a block where every block has an SM to itself and every warp at least
-    // two groups: 2048 x 4096 T=1 4.2 -> 3.3 us, T=17 6.9 -> 5.6; not where blocks share SMs
-    // (5120 x 2048 T=1 3.4, with sixteen 4.9) or k is short (700 x 1920 T=17 3.7, 4.1).
+    // two groups: 2048 x 4096 T=1 4.3 -> 3.3 us, T=17 7.4 -> 5.1; not where blocks share SMs
+    // (5120 x 2048 T=1 3.1, with sixteen 3.7) or k is short (700 x 1920 T=32 4.2, 4.8).
     if (a.tiles <= sm_count() && a.groups >= 32)
       DM_CUDA_CHECK(launch_pdl_late(k_w4_direct<E4M3, GROUP, NT, 16>, grid, dim3(512), 0, s, a));
     else
@@ -552,9 +557,9 @@ static int w4_launch(W4Args a, cudaStream_t s) {
   const size_t per_unit = NT * 32 * 16 * (W4_UNIT / 32);
   const int64_t sms = sm_count();
   // Two blocks share k where x is large beside the columns, so that each lays out half of it
-  // and twice as many columns use it: 9000 x 4096 T=32 24.6 -> 20.6 us, T=13 12.9 -> 11.9;
-  // not where the columns then no longer go in one pass (20000 x 2048 T=13 14.0 -> 17.4) nor
-  // where x is small (9000 x 4096 T=1 7.0 -> 8.1).
+  // and twice as many columns use it: 9000 x 4096 T=32 19.6 -> 17.9 us, T=13 11.7 -> 11.2;
+  // not where the columns then no longer go in one pass (20000 x 2048 T=13 13.0 -> 16.7) nor
+  // where x is small (9000 x 4096 T=1 7.0 -> 8.0).
   const int ks = units * per_unit > 100 * 1024 && a.tiles <= (sms / 2) * W4_WARPS && sms > 1 ? 2 : 1;
   const int64_t places = sms / ks;
   // as few passes over the column tiles as the warps of all blocks allow, the tiles

@@ -1,5 +1,6 @@
 """Sums of the products with 4-bit weights against 64 bits, bounded by the formula's own
-terms |x (q - 8) scale|: rows near the foot of bf16's range. Sizes of either kernel."""
+terms |x (q - 8) scale|: rows near the foot of bf16's range, and large values that
+meet the code of zero, which add nothing. Sizes of either kernel."""
 import pytest
 import torch
 
@@ -7,7 +8,7 @@ import paper_2609_38823_gb300 as dm
 
 pytestmark = pytest.mark.gpu
 DEV = torch.device("cuda")
-BF16, F32 = torch.bfloat16, torch.float32
+BF16, F32, E4M3 = torch.bfloat16, torch.float32, torch.float8_e4m3fn
 SMALL, LARGE = (300, 1024), (17000, 2048)  # N, K
 
 
@@ -65,3 +66,26 @@ def test_rows_of_every_size_side_by_side(N, K):
     # and group by group
     f = 2.0 ** e[(torch.arange(K, device=DEV) // 64) % 8].double()
     _check((torch.randn(3, K, device=DEV) * f).to(BF16), w, ws)
+
+
+@pytest.mark.parametrize("kind", [BF16, E4M3])
+@pytest.mark.parametrize("N,K", [SMALL, LARGE])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("T", [1, 12, 20, 32])
+def test_large_values_on_the_code_of_zero(kind, N, K, group, T):
+    w, ws = _weights(N, K, group, T)
+    g = torch.Generator(device=DEV).manual_seed(T + 1)
+    x = torch.randn(T, K, generator=g, device=DEV)
+    # one value of a group 2^14 times its neighbours (e4m3: 448 beside values of 1/64), its weights all zero
+    at = torch.arange(0, K, group, device=DEV) + torch.randint(0, group, (K // group,), generator=g, device=DEV)
+    x = x / 64 if kind == E4M3 else x
+    x[:, at] = 448.0 if kind == E4M3 else 2.0 ** 14
+    low, byte = at % 2 == 0, at // 2
+    w[:, byte] = torch.where(low, (w[:, byte] & 0xF0) | 8, (w[:, byte] & 0x0F) | 0x80)
+    xs = torch.rand(T, generator=g, device=DEV) + 0.5 if kind == E4M3 else None
+    out = _check(x.to(kind), w, ws, xs)
+    # without them: not a bit changes
+    x[:, at] = 0
+    again = torch.empty_like(out)
+    dm.decomoe_w4_linear(x.to(kind), w, ws, again, x_scale=xs)
+    assert torch.equal(out, again)
