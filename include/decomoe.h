@@ -615,6 +615,11 @@ DECOMOE_API int decomoe_attention(const void* q, int64_t n, const void* k_cache,
  * left out. seq_len must not overlap cached or fresh, nor free_head_out free_head.
  * positions may be NULL. One launch, no host synchronisation.
  *
+ * decomoe_paged_plan_step: the same for a decode step, in which request b has row b:
+ * it adds one row where fresh[b] is 1 and none where it is 0 (no request, or one that
+ * waits), and slot_map and positions [B] are by request, -1 where none is added.
+ * More than one row counts as one and marks DECOMOE_ERR_BAD_INPUT.
+ *
  * decomoe_paged_append: the step's new rows into their slots, keys and values
  * in one launch. k_new, v_new: [N, width] dtype (bf16 or f32), rows
  * k_row_stride and v_row_stride elements apart (the rows of a fused projection
@@ -653,6 +658,11 @@ DECOMOE_API int decomoe_paged_plan(const int32_t* cached, const int32_t* fresh, 
                                    int32_t* free_head_out, int32_t* block_table, int64_t max_pages,
                                    int32_t* seq_len, int32_t* row_start, int32_t* slot_map, int32_t* positions,
                                    int64_t N, int32_t* status_dev, decomoe_stream_t stream);
+DECOMOE_API int decomoe_paged_plan_step(const int32_t* cached, const int32_t* fresh, int64_t B, int page_size,
+                                        const int32_t* free_pages, int64_t n_free, const int32_t* free_head,
+                                        int32_t* free_head_out, int32_t* block_table, int64_t max_pages,
+                                        int32_t* seq_len, int32_t* slot_map, int32_t* positions, int32_t* status_dev,
+                                        decomoe_stream_t stream);
 DECOMOE_API int decomoe_paged_append(const void* k_new, int64_t k_row_stride, const void* v_new, int64_t v_row_stride,
                                      int64_t N, int width, int dtype, const int32_t* slot_map, void* k_pages,
                                      void* v_pages, int64_t num_pages, int page_size, int64_t page_stride,

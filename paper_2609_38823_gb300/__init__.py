@@ -94,6 +94,7 @@ SIGNATURES = {
                                     _P, _P, _S, _P, _P]),
     "decomoe_moe_layer_workspace_layout": (_I, [_L, _I, _I, _I, _I, _I, _P]),
     "decomoe_paged_plan": (_I, [_P, _P, _L, _I, _P, _L, _P, _P, _P, _L, _P, _P, _P, _P, _L, _P, _P]),
+    "decomoe_paged_plan_step": (_I, [_P, _P, _L, _I, _P, _L, _P, _P, _P, _L, _P, _P, _P, _P, _P]),
     "decomoe_paged_append": (_I, [_P, _L, _P, _L, _L, _I, _I, _P, _P, _P, _L, _I, _L, _P, _P]),
     "decomoe_paged_attention_workspace_bytes": (_S, [_L, _I, _I, _I]),
     "decomoe_paged_attention": (_I, [_P, _L, _L, _P, _P, _L, _I, _L, _P, _L, _P, _P, _P, _I, _I, _I, _F, _P, _P, _S,
@@ -642,6 +643,16 @@ def decomoe_paged_plan(cached, fresh, page_size, free_pages, block_table, seq_le
                                free_head, free_head_out, status, None if stream is None else stream.cuda_stream)
     if code:
         _check("decomoe_paged_plan", code)
+
+
+def decomoe_paged_plan_step(cached, fresh, page_size, free_pages, block_table, seq_len, slot_map, positions=None,
+                            free_head=None, free_head_out=None, status=None, stream=None):
+    """decomoe_paged_plan for a decode step: one row where fresh[b] is 1, none where it
+    is 0, and slot_map and positions [B] are by request (-1 where none is added)."""
+    code = _calls().paged_plan_step(cached, fresh, page_size, free_pages, block_table, seq_len, slot_map, positions,
+                                    free_head, free_head_out, status, None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_paged_plan_step", code)
 
 
 def decomoe_paged_append(k_new, v_new, slot_map, k_pages, v_pages, status=None, stream=None):

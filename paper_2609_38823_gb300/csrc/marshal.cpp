@@ -129,6 +129,26 @@ int paged_plan(PyObject* const* a) {
                             ptr<int32_t>(status), stream(a[12]));
 }
 
+// cached, fresh, page_size, free_pages, block_table, seq_len, slot_map, positions,
+// free_head, free_head_out, status, stream
+int paged_plan_step(PyObject* const* a) {
+  const char* n = "paged_plan_step";
+  const at::Tensor *cached = index(a[0], n), *fresh = index(a[1], n), *pages = index(a[3], n), *table = index(a[4], n),
+                   *len = index(a[5], n), *slots = index(a[6], n), *pos = index(a[7], n, true), *head = index(a[8], n, true),
+                   *head_out = index(a[9], n, true), *status = index(a[10], n, true);
+  const int64_t B = cached->numel();
+  need(cached->dim() == 1 && pages->dim() == 1 && shaped(fresh, {B}) && shaped(len, {B}) && shaped(slots, {B}) &&
+           table->dim() == 2 && table->size(0) == B && (pos == nullptr || shaped(pos, {B})) &&
+           (head == nullptr || head->numel() == 1) && (head_out == nullptr || head_out->numel() == 1) &&
+           (status == nullptr || status->numel() >= 1),
+       "paged_plan_step: cached, fresh, seq_len, slot_map and positions [B], block_table [B, max_pages], free_pages [n], "
+       "free_head and free_head_out [1] expected");
+  return decomoe_paged_plan_step(ptr<int32_t>(cached), ptr<int32_t>(fresh), B, to_int(a[2]), ptr<int32_t>(pages),
+                                 pages->numel(), ptr<int32_t>(head), ptr<int32_t>(head_out), ptr<int32_t>(table),
+                                 table->size(1), ptr<int32_t>(len), ptr<int32_t>(slots), ptr<int32_t>(pos),
+                                 ptr<int32_t>(status), stream(a[11]));
+}
+
 // k_new, v_new, slot_map, k_pages, v_pages, status, stream
 int paged_append(PyObject* const* a) {
   const char* n = "paged_append";
@@ -225,8 +245,9 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define DM_ENTRY(name, args) \
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name, args>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {DM_ENTRY(paged_plan, 13),     DM_ENTRY(paged_append, 7), DM_ENTRY(paged_attention, 12),
-                         DM_ENTRY(add_rmsnorm_q8, 9), DM_ENTRY(w4_linear, 6),    {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {DM_ENTRY(paged_plan, 13),      DM_ENTRY(paged_plan_step, 12), DM_ENTRY(paged_append, 7),
+                         DM_ENTRY(paged_attention, 12), DM_ENTRY(add_rmsnorm_q8, 9),   DM_ENTRY(w4_linear, 6),
+                         {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

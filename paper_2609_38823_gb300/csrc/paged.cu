@@ -20,6 +20,7 @@ struct PlanArgs {
   int32_t *free_head_out, *table, *seq_len, *row_start, *slot_map, *positions, *status;
   int64_t n_free, max_pages, N;
   int B, shift;  // page size 1 << shift
+  bool by_request;  // one row at most of each request, and row b is request b's
 };
 
 // Exclusive sums of the block's values in thread order, and their totals.
@@ -83,9 +84,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_plan(PlanArgs a) {
   bool bad = false;
   int64_t nr = 0, np = 0;
   for (int b = b0; b < b1; ++b) {
-    const int64_t c = a.cached[b], f = a.fresh[b];
+    const int64_t c = a.cached[b], given = a.fresh[b], f = a.by_request ? min(given, int64_t{1}) : given;
     const int64_t cc = min(max(c, int64_t{0}), cap), end = min(cc + max(f, int64_t{0}), cap);
-    bad |= c < 0 || f < 0 || c > cap || cc + f > cap;
+    bad |= c < 0 || f < 0 || f < given || c > cap || cc + f > cap;
     if (lead) a.seq_len[b] = static_cast<int32_t>(end);
     held[b] = static_cast<int32_t>(cc);
     // the rows of a request that the table is too narrow for are rows all the same
@@ -100,7 +101,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_plan(PlanArgs a) {
     const int32_t r = rows[b], p = pages[b];
     rows[b] = static_cast<int32_t>(min(nr, int64_t{INT_MAX}));
     pages[b] = static_cast<int32_t>(min(np, int64_t{INT_MAX}));
-    if (lead) a.row_start[b] = rows[b];
+    if (lead && !a.by_request) a.row_start[b] = rows[b];
     nr += r;
     np += p;
   }
@@ -109,7 +110,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_plan(PlanArgs a) {
     rows[a.B] = static_cast<int32_t>(all_rows);
     pages[a.B] = static_cast<int32_t>(all_pages);
     if (lead) {
-      a.row_start[a.B] = rows[a.B];
+      if (!a.by_request) a.row_start[a.B] = rows[a.B];
       if (a.free_head_out != nullptr)
         *a.free_head_out = static_cast<int32_t>(min(head + all_pages, max(a.n_free, head)));
       bad |= tr > a.N || head < 0 || head + tp > a.n_free;
@@ -130,9 +131,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_plan(PlanArgs a) {
   }
   for (int64_t r = first; r < a.N; r += step) {
     int32_t slot = -1, pos = -1;
-    if (r < all_rows) {
-      const int b = find_request(rows, a.B, static_cast<int32_t>(r));
-      const int64_t p = held[b] + (r - rows[b]);
+    if (a.by_request ? rows[r] < rows[r + 1] : r < all_rows) {
+      const int b = a.by_request ? static_cast<int>(r) : find_request(rows, a.B, static_cast<int32_t>(r));
+      const int64_t p = held[b] + (a.by_request ? 0 : r - rows[b]);
       if (p < cap) {
         const int64_t have = (held[b] + ps1) >> a.shift, e = p >> a.shift;
         const int32_t page = e < have ? a.table[b * a.max_pages + e] : page_of(pages[b] + (e - have));
@@ -193,29 +194,23 @@ static bool ranges_overlap(const void* p, size_t n, const void* q, size_t m) {
   return a < b + m && b < a + n;
 }
 
-}  // namespace decomoe
-
-using namespace decomoe;
-
-extern "C" {
-
-int decomoe_paged_plan(const int32_t* cached, const int32_t* fresh, int64_t B, int page_size,
-                       const int32_t* free_pages, int64_t n_free, const int32_t* free_head, int32_t* free_head_out,
-                       int32_t* block_table, int64_t max_pages, int32_t* seq_len, int32_t* row_start,
-                       int32_t* slot_map, int32_t* positions, int64_t N, int32_t* status_dev,
-                       decomoe_stream_t stream) {
+static int plan_call(const char* name, bool by_request, const int32_t* cached, const int32_t* fresh, int64_t B,
+                     int page_size, const int32_t* free_pages, int64_t n_free, const int32_t* free_head,
+                     int32_t* free_head_out, int32_t* block_table, int64_t max_pages, int32_t* seq_len,
+                     int32_t* row_start, int32_t* slot_map, int32_t* positions, int64_t N, int32_t* status_dev,
+                     decomoe_stream_t stream) {
   clear_error();
-  DM_ARG_CHECK(B >= 0 && B <= DECOMOE_MAX_REQUESTS, "paged_plan: B must lie in [0, %d]", DECOMOE_MAX_REQUESTS);
-  DM_ARG_CHECK(page_size >= 1 && (page_size & (page_size - 1)) == 0, "paged_plan: page_size must be a power of two");
-  DM_ARG_CHECK(N >= 0 && N <= INT_MAX && n_free >= 0 && n_free <= INT_MAX, "paged_plan: bad N or n_free");
-  DM_ARG_CHECK(max_pages >= 0 && max_pages <= INT_MAX / page_size, "paged_plan: max_pages * page_size must be in [0, 2^31)");
-  DM_ARG_CHECK(row_start != nullptr && (N == 0 || slot_map != nullptr) && (n_free == 0 || free_pages != nullptr),
-               "paged_plan: null pointer");
-  DM_ARG_CHECK(B == 0 || (cached && fresh && seq_len && (block_table || max_pages == 0)), "paged_plan: null pointer");
+  DM_ARG_CHECK(B >= 0 && B <= DECOMOE_MAX_REQUESTS, "%s: B must lie in [0, %d]", name, DECOMOE_MAX_REQUESTS);
+  DM_ARG_CHECK(page_size >= 1 && (page_size & (page_size - 1)) == 0, "%s: page_size must be a power of two", name);
+  DM_ARG_CHECK(N >= 0 && N <= INT_MAX && n_free >= 0 && n_free <= INT_MAX, "%s: bad N or n_free", name);
+  DM_ARG_CHECK(max_pages >= 0 && max_pages <= INT_MAX / page_size, "%s: max_pages * page_size must be in [0, 2^31)", name);
+  DM_ARG_CHECK((by_request || row_start != nullptr) && (N == 0 || slot_map != nullptr) && (n_free == 0 || free_pages != nullptr),
+               "%s: null pointer", name);
+  DM_ARG_CHECK(B == 0 || (cached && fresh && seq_len && (block_table || max_pages == 0)), "%s: null pointer", name);
   const size_t bytes = static_cast<size_t>(B) * sizeof(int32_t);
   DM_ARG_CHECK(!ranges_overlap(cached, bytes, seq_len, bytes) && !ranges_overlap(fresh, bytes, seq_len, bytes),
-               "paged_plan: seq_len overlaps cached or fresh");
-  DM_ARG_CHECK(free_head_out == nullptr || free_head_out != free_head, "paged_plan: free_head_out is free_head");
+               "%s: seq_len overlaps cached or fresh", name);
+  DM_ARG_CHECK(free_head_out == nullptr || free_head_out != free_head, "%s: free_head_out is free_head", name);
   PlanArgs a = {};
   a.cached = cached;
   a.fresh = fresh;
@@ -233,6 +228,7 @@ int decomoe_paged_plan(const int32_t* cached, const int32_t* fresh, int64_t B, i
   a.N = N;
   a.B = static_cast<int>(B);
   a.shift = __builtin_ctz(static_cast<unsigned>(page_size));
+  a.by_request = by_request;
   const int64_t items = std::max<int64_t>(N, 1);
   const int grid = static_cast<int>(std::min<int64_t>(sm_count(), (items + PLAN_THREADS - 1) / PLAN_THREADS));
   const size_t smem = (3 * static_cast<size_t>(B) + 2) * sizeof(int32_t);
@@ -240,6 +236,29 @@ int decomoe_paged_plan(const int32_t* cached, const int32_t* fresh, int64_t B, i
     DM_CUDA_CHECK(cudaFuncSetAttribute(k_paged_plan, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
   DM_CUDA_CHECK(launch_pdl(k_paged_plan, dim3(grid), dim3(PLAN_THREADS), smem, reinterpret_cast<cudaStream_t>(stream), a));
   return DECOMOE_OK;
+}
+
+}  // namespace decomoe
+
+using namespace decomoe;
+
+extern "C" {
+
+int decomoe_paged_plan(const int32_t* cached, const int32_t* fresh, int64_t B, int page_size,
+                       const int32_t* free_pages, int64_t n_free, const int32_t* free_head, int32_t* free_head_out,
+                       int32_t* block_table, int64_t max_pages, int32_t* seq_len, int32_t* row_start,
+                       int32_t* slot_map, int32_t* positions, int64_t N, int32_t* status_dev,
+                       decomoe_stream_t stream) {
+  return plan_call("paged_plan", false, cached, fresh, B, page_size, free_pages, n_free, free_head, free_head_out,
+                   block_table, max_pages, seq_len, row_start, slot_map, positions, N, status_dev, stream);
+}
+
+int decomoe_paged_plan_step(const int32_t* cached, const int32_t* fresh, int64_t B, int page_size,
+                            const int32_t* free_pages, int64_t n_free, const int32_t* free_head,
+                            int32_t* free_head_out, int32_t* block_table, int64_t max_pages, int32_t* seq_len,
+                            int32_t* slot_map, int32_t* positions, int32_t* status_dev, decomoe_stream_t stream) {
+  return plan_call("paged_plan_step", true, cached, fresh, B, page_size, free_pages, n_free, free_head, free_head_out,
+                   block_table, max_pages, seq_len, nullptr, slot_map, positions, B, status_dev, stream);
 }
 
 int decomoe_paged_append(const void* k_new, int64_t k_row_stride, const void* v_new, int64_t v_row_stride, int64_t N,

@@ -22,7 +22,7 @@ import torch
 
 from . import (DECOMOE_BF16, decomoe_add_rmsnorm_q8, decomoe_moe_layer, decomoe_moe_layer_workspace_bytes,
                decomoe_paged_append, decomoe_paged_attention, decomoe_paged_attention_workspace_bytes,
-               decomoe_paged_plan, decomoe_w4_linear, workspace)
+               decomoe_paged_plan, decomoe_paged_plan_step, decomoe_w4_linear, workspace)
 
 
 def quantize_w4(w: torch.Tensor, group: int = 128):
@@ -73,12 +73,14 @@ class PagedCache:
         request, over those that add some. Repeating it before ``advance`` changes
         nothing."""
         self.active.logical_or_(fresh > 0)
-        self.plan_rows(fresh, slots, positions)
-
-    def plan_rows(self, fresh: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
-        """``plan`` without a look at `active`: what a decode step calls."""
         decomoe_paged_plan(self.cached, fresh, self.page_size, self.free, self.table, self.seq_len, self.row_start, slots,
                            positions, free_head=self.head, free_head_out=self.head_next, status=self.status)
+
+    def plan_step(self, fresh: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
+        """``plan`` for a decode step: one row where fresh [requests] is 1, none where it
+        is 0; slots and positions [requests] by request, -1 where none is added."""
+        decomoe_paged_plan_step(self.cached, fresh, self.page_size, self.free, self.table, self.seq_len, slots, positions,
+                                free_head=self.head, free_head_out=self.head_next, status=self.status)
 
     def advance(self) -> None:
         """The step's rows are in the cache."""
@@ -138,10 +140,7 @@ class DecodeStep:
         dev = cache.pool.device
         bf = dict(dtype=torch.bfloat16, device=dev)
         self.fresh = cache.active
-        # slots and positions as the plan numbers rows (live requests alone), and by request
-        self.rows, self.idle = torch.empty(B, dtype=torch.int32, device=dev), torch.empty(B, dtype=torch.bool, device=dev)
-        self.packed, self.placed = (torch.empty(2, B, dtype=torch.int32, device=dev) for _ in range(2))
-        self.slots, self.positions = self.placed
+        self.slots, self.positions = (torch.empty(B, dtype=torch.int32, device=dev) for _ in range(2))
         self.x8 = torch.empty(B, d, dtype=torch.float8_e4m3fn, device=dev)
         self.x8_scale = torch.empty(B, dtype=torch.float32, device=dev)
         self.qkv = torch.empty(B, hq + 2 * hkv, D, **bf)
@@ -157,12 +156,7 @@ class DecodeStep:
         last layer. trace(l, step, h_in, h_out), if given, is called after each
         layer's launches are queued (the buffers are reused by later layers)."""
         c = self.cache
-        # one row at most for each request, so that row_start[b] <= b stays inside the rows
-        torch.clamp(self.fresh, 0, 1, out=self.rows)
-        c.plan_rows(self.rows, *self.packed)
-        torch.index_select(self.packed, 1, c.row_start[:-1], out=self.placed)
-        torch.eq(self.rows, 0, out=self.idle)
-        self.placed.masked_fill_(self.idle, -1)
+        c.plan_step(self.fresh, self.slots, self.positions)
         h = h0
         for l, w in enumerate(self.layers):
             out = self.h[l & 1]
