@@ -620,6 +620,13 @@ DECOMOE_API int decomoe_attention(const void* q, int64_t n, const void* k_cache,
  * waits), and slot_map and positions [B] are by request, -1 where none is added.
  * More than one row counts as one and marks DECOMOE_ERR_BAD_INPUT.
  *
+ * decomoe_paged_advance: the lengths after the step, cached[b] = seq_len[b], and
+ * *free_head = *free_head_out (both may be NULL). Rows that got no page do not count:
+ * where the list ran out, a request ends in front of the first page that it asked for
+ * and did not get (a negative entry), so that a later plan can give it one. A length
+ * beyond max_pages * page_size is cut there. cached must overlap neither seq_len nor
+ * block_table.
+ *
  * decomoe_paged_append: the step's new rows into their slots, keys and values
  * in one launch. k_new, v_new: [N, width] dtype (bf16 or f32), rows
  * k_row_stride and v_row_stride elements apart (the rows of a fused projection
@@ -663,6 +670,9 @@ DECOMOE_API int decomoe_paged_plan_step(const int32_t* cached, const int32_t* fr
                                         int32_t* free_head_out, int32_t* block_table, int64_t max_pages,
                                         int32_t* seq_len, int32_t* slot_map, int32_t* positions, int32_t* status_dev,
                                         decomoe_stream_t stream);
+DECOMOE_API int decomoe_paged_advance(int32_t* cached, const int32_t* seq_len, const int32_t* block_table, int64_t B,
+                                      int64_t max_pages, int page_size, int32_t* free_head,
+                                      const int32_t* free_head_out, decomoe_stream_t stream);
 DECOMOE_API int decomoe_paged_append(const void* k_new, int64_t k_row_stride, const void* v_new, int64_t v_row_stride,
                                      int64_t N, int width, int dtype, const int32_t* slot_map, void* k_pages,
                                      void* v_pages, int64_t num_pages, int page_size, int64_t page_stride,

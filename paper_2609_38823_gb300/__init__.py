@@ -95,6 +95,7 @@ SIGNATURES = {
     "decomoe_moe_layer_workspace_layout": (_I, [_L, _I, _I, _I, _I, _I, _P]),
     "decomoe_paged_plan": (_I, [_P, _P, _L, _I, _P, _L, _P, _P, _P, _L, _P, _P, _P, _P, _L, _P, _P]),
     "decomoe_paged_plan_step": (_I, [_P, _P, _L, _I, _P, _L, _P, _P, _P, _L, _P, _P, _P, _P, _P]),
+    "decomoe_paged_advance": (_I, [_P, _P, _P, _L, _L, _I, _P, _P, _P]),
     "decomoe_paged_append": (_I, [_P, _L, _P, _L, _L, _I, _I, _P, _P, _P, _L, _I, _L, _P, _P]),
     "decomoe_paged_attention_workspace_bytes": (_S, [_L, _I, _I, _I]),
     "decomoe_paged_attention": (_I, [_P, _L, _L, _P, _P, _L, _I, _L, _P, _L, _P, _P, _P, _I, _I, _I, _F, _P, _P, _S,
@@ -653,6 +654,15 @@ def decomoe_paged_plan_step(cached, fresh, page_size, free_pages, block_table, s
                                     free_head, free_head_out, status, None if stream is None else stream.cuda_stream)
     if code:
         _check("decomoe_paged_plan_step", code)
+
+
+def decomoe_paged_advance(cached, seq_len, block_table, page_size, free_head=None, free_head_out=None, stream=None):
+    """The lengths after a step: cached[b] = seq_len[b] but for rows that got no page,
+    free_head[0] = free_head_out[0]."""
+    code = _calls().paged_advance(cached, seq_len, block_table, page_size, free_head, free_head_out,
+                                  None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_paged_advance", code)
 
 
 def decomoe_paged_append(k_new, v_new, slot_map, k_pages, v_pages, status=None, stream=None):

@@ -149,6 +149,19 @@ int paged_plan_step(PyObject* const* a) {
                                  ptr<int32_t>(status), stream(a[11]));
 }
 
+// cached, seq_len, block_table, page_size, free_head, free_head_out, stream
+int paged_advance(PyObject* const* a) {
+  const char* n = "paged_advance";
+  const at::Tensor *cached = index(a[0], n), *len = index(a[1], n), *table = index(a[2], n), *head = index(a[4], n, true),
+                   *head_out = index(a[5], n, true);
+  const int64_t B = cached->numel();
+  need(cached->dim() == 1 && shaped(len, {B}) && table->dim() == 2 && table->size(0) == B &&
+           (head == nullptr || head->numel() == 1) && (head_out == nullptr || head_out->numel() == 1),
+       "paged_advance: cached and seq_len [B], block_table [B, max_pages], free_head and free_head_out [1] expected");
+  return decomoe_paged_advance(ptr<int32_t>(cached), ptr<int32_t>(len), ptr<int32_t>(table), B, table->size(1),
+                               to_int(a[3]), ptr<int32_t>(head), ptr<int32_t>(head_out), stream(a[6]));
+}
+
 // k_new, v_new, slot_map, k_pages, v_pages, status, stream
 int paged_append(PyObject* const* a) {
   const char* n = "paged_append";
@@ -245,9 +258,9 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 
 #define DM_ENTRY(name, args) \
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name, args>)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {DM_ENTRY(paged_plan, 13),      DM_ENTRY(paged_plan_step, 12), DM_ENTRY(paged_append, 7),
-                         DM_ENTRY(paged_attention, 12), DM_ENTRY(add_rmsnorm_q8, 9),   DM_ENTRY(w4_linear, 6),
-                         {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {DM_ENTRY(paged_plan, 13),   DM_ENTRY(paged_plan_step, 12),  DM_ENTRY(paged_advance, 7),
+                         DM_ENTRY(paged_append, 7),  DM_ENTRY(paged_attention, 12), DM_ENTRY(add_rmsnorm_q8, 9),
+                         DM_ENTRY(w4_linear, 6),     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -149,6 +149,31 @@ __global__ void __launch_bounds__(PLAN_THREADS) k_paged_plan(PlanArgs a) {
   if (bad) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
 }
 
+// ------------------------------------------------------------------ advance
+// A request's rows after the step: a warp per request looks through the pages that the
+// step asked for, 32 entries at a time, for the first one that it did not get.
+__global__ void __launch_bounds__(256)
+    k_paged_advance(int32_t* cached, const int32_t* seq_len, const int32_t* table, int B, int64_t max_pages, int shift,
+                    int32_t* free_head, const int32_t* free_head_out) {
+  pdl_enter();
+  const int b = (blockIdx.x * blockDim.x + threadIdx.x) >> 5, lane = threadIdx.x & 31;
+  if (blockIdx.x == 0 && threadIdx.x == 0 && free_head != nullptr) *free_head = *free_head_out;
+  if (b >= B) return;
+  const int64_t ps1 = (int64_t{1} << shift) - 1;
+  const int64_t n = min(max(static_cast<int64_t>(seq_len[b]), int64_t{0}), max_pages << shift);
+  const int64_t have = (max(static_cast<int64_t>(cached[b]), int64_t{0}) + ps1) >> shift, need = (n + ps1) >> shift;
+  int64_t end = n;
+  for (int64_t e = have; e < need; e += 32) {
+    const unsigned gone = __ballot_sync(0xffffffffu, e + lane < need && table[b * max_pages + e + lane] < 0);
+    if (gone != 0) {
+      end = min(end, (e + __ffs(gone) - 1) << shift);
+      break;
+    }
+  }
+  __syncwarp();
+  if (lane == 0) cached[b] = static_cast<int32_t>(end);
+}
+
 // ------------------------------------------------------------------ append
 // A plain scatter, bound by bandwidth where there are many rows and by one round trip
 // where there are few. 1 << LANES threads take a row of keys and the same of values,
@@ -259,6 +284,27 @@ int decomoe_paged_plan_step(const int32_t* cached, const int32_t* fresh, int64_t
                             int32_t* slot_map, int32_t* positions, int32_t* status_dev, decomoe_stream_t stream) {
   return plan_call("paged_plan_step", true, cached, fresh, B, page_size, free_pages, n_free, free_head, free_head_out,
                    block_table, max_pages, seq_len, nullptr, slot_map, positions, B, status_dev, stream);
+}
+
+int decomoe_paged_advance(int32_t* cached, const int32_t* seq_len, const int32_t* block_table, int64_t B,
+                          int64_t max_pages, int page_size, int32_t* free_head, const int32_t* free_head_out,
+                          decomoe_stream_t stream) {
+  clear_error();
+  DM_ARG_CHECK(B >= 0 && B <= DECOMOE_MAX_REQUESTS, "paged_advance: B must lie in [0, %d]", DECOMOE_MAX_REQUESTS);
+  DM_ARG_CHECK(page_size >= 1 && (page_size & (page_size - 1)) == 0, "paged_advance: page_size must be a power of two");
+  DM_ARG_CHECK(max_pages >= 0 && max_pages <= INT_MAX / page_size,
+               "paged_advance: max_pages * page_size must be in [0, 2^31)");
+  DM_ARG_CHECK(B == 0 || (cached && seq_len && (block_table || max_pages == 0)), "paged_advance: null pointer");
+  DM_ARG_CHECK((free_head == nullptr) == (free_head_out == nullptr), "paged_advance: free_head and free_head_out go together");
+  const size_t bytes = static_cast<size_t>(B) * sizeof(int32_t);
+  DM_ARG_CHECK(!ranges_overlap(cached, bytes, seq_len, bytes) &&
+                   !ranges_overlap(cached, bytes, block_table, bytes * static_cast<size_t>(max_pages)),
+               "paged_advance: cached overlaps seq_len or block_table");
+  const int grid = static_cast<int>(std::max<int64_t>(1, (B * 32 + 255) / 256));
+  DM_CUDA_CHECK(launch_pdl(k_paged_advance, dim3(grid), dim3(256), 0, reinterpret_cast<cudaStream_t>(stream), cached,
+                           seq_len, block_table, static_cast<int>(B), max_pages,
+                           __builtin_ctz(static_cast<unsigned>(page_size)), free_head, free_head_out));
+  return DECOMOE_OK;
 }
 
 int decomoe_paged_append(const void* k_new, int64_t k_row_stride, const void* v_new, int64_t v_row_stride, int64_t N,

@@ -21,8 +21,9 @@ from typing import Callable, Optional, Sequence
 import torch
 
 from . import (DECOMOE_BF16, decomoe_add_rmsnorm_q8, decomoe_moe_layer, decomoe_moe_layer_workspace_bytes,
-               decomoe_paged_append, decomoe_paged_attention, decomoe_paged_attention_workspace_bytes,
-               decomoe_paged_plan, decomoe_paged_plan_step, decomoe_w4_linear, workspace)
+               decomoe_paged_advance, decomoe_paged_append, decomoe_paged_attention,
+               decomoe_paged_attention_workspace_bytes, decomoe_paged_plan, decomoe_paged_plan_step, decomoe_w4_linear,
+               workspace)
 
 
 def quantize_w4(w: torch.Tensor, group: int = 128):
@@ -83,9 +84,13 @@ class PagedCache:
                                 free_head=self.head, free_head_out=self.head_next, status=self.status)
 
     def advance(self) -> None:
-        """The step's rows are in the cache."""
-        self.cached.copy_(self.seq_len)
-        self.head.copy_(self.head_next)
+        """The step's rows are in the cache: those that got a page. Where the list of free
+        pages ran out (the status word then says DECOMOE_ERR_BAD_INPUT, and the step's
+        results of such a request lack its own row: look at it before using them), a
+        request ends in front of the first page that it did not get, and the next plan
+        tries again."""
+        decomoe_paged_advance(self.cached, self.seq_len, self.table, self.page_size, free_head=self.head,
+                              free_head_out=self.head_next)
 
     def release(self, request: int) -> None:
         """The request is over: its pages go back to the list (those of a hidden block

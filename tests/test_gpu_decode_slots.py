@@ -1,6 +1,7 @@
 """Slots of a decode step's batch that have no request, or whose request waits:
 they add no row, take no page and leave the other requests alone, in eager steps
-and in captured ones; a new prompt takes a slot up again."""
+and in captured ones; a new prompt takes a slot up again. A cache that ran out of pages
+goes on when it has some again."""
 import pytest
 import torch
 
@@ -146,3 +147,42 @@ def test_captured_steps_with_a_slot_released_and_taken_up_again():
         assert dm.decomoe_read_status(s.cache.status) == dm.DECOMOE_OK
         runs.append(torch.stack(got))
     assert torch.equal(runs[0], runs[1])
+
+
+def test_a_cache_that_ran_out_of_pages_goes_on():
+    """Rows without a page do not count: their request goes on where its rows end."""
+    cache = PagedCache(L, 3, pages=9, page_size=PS, max_pages=6, hkv=HKV, d=D)
+    layers, _ = _model()
+    held = _prompt(cache, [16, 15, 33], 1)  # 2 + 2 + 5 pages: none is left
+    step = DecodeStep(layers, cache, 3, HQ, K)
+    g = torch.Generator().manual_seed(2)
+    h0 = lambda: torch.randn(3, D_MODEL, generator=g).to(torch.bfloat16).to(DEV)  # noqa: E731
+    kept = [16, 15, 33]
+    for i in range(4):  # request 0 gets no page, request 1 fills its last one
+        step(h0())
+        slots = step.slots.tolist()
+        assert slots[0] == -1 and slots[2] >= 0 and (slots[1] >= 0) == (i == 0)
+        assert dm.decomoe_read_status(cache.status) == dm.DECOMOE_ERR_BAD_INPUT
+        for l in range(L):
+            for b in range(3):
+                if slots[b] >= 0:
+                    held[l][b][0].append(cache.k(l).reshape(-1, HKV, D)[slots[b]].cpu())
+        kept = [n + (x >= 0) for n, x in zip(kept, slots)]
+        cache.advance()
+        assert cache.cached.tolist() == kept and int(cache.head) == 9
+    assert kept == [16, 16, 37]
+    cache.release(2)
+    cache.status.zero_()
+    for i in range(3):
+        step(h0())
+        assert all(x >= 0 for x in step.slots.tolist()[:2]) and step.positions.tolist() == [16 + i, 16 + i, -1]
+        cache.advance()
+    assert dm.decomoe_read_status(cache.status) == dm.DECOMOE_OK
+    assert cache.cached.tolist() == [19, 19, 0] and int(cache.head) == 6
+    for l in range(L):
+        for b in (0, 1):
+            rows = cache.k(l)[cache.table[b, :2].long()].reshape(-1, HKV, D).cpu()
+            assert torch.equal(rows, torch.stack(held[l][b][0]))
+    cache.release(0)
+    cache.release(1)
+    assert int(cache.head) == 0 and sorted(cache.free.tolist()) == list(range(9))

@@ -103,3 +103,50 @@ def test_step_plan_refusals():
             call(**kw)
         assert e.value.code == dm.DECOMOE_ERR_INVALID_ARG
     torch.cuda.synchronize()
+
+
+def _advance(cached, seq_len, table, ps):
+    c, head, out = _i32(cached), _i32([3]), _i32([7])
+    t = _i32(table).view(len(cached), -1)
+    dm.decomoe_paged_advance(c, _i32(seq_len), t, ps, free_head=head, free_head_out=out)
+    first = c.clone()
+    dm.decomoe_paged_advance(c, _i32(seq_len), t, ps)  # the same plan once more: nothing is left to do
+    assert torch.equal(c, first) and int(head) == 7
+    return c.tolist()
+
+
+def test_rows_without_a_page_do_not_count():
+    table = [[0, -1, -1, -1],    # a decode row without a page
+             [1, -1, -1, -1],    # one row in the last page, one without
+             [2, 3, -1, -1],     # a prompt of which two pages were given out
+             [4, 5, -1, -1],     # a row in a held page
+             [6, 7, -1, -1],     # nothing added
+             [-1, -1, 8, 9]]     # a full one, whose first pages (a hidden block) were given back
+    assert _advance([4, 3, 0, 6, 8, 16], [5, 5, 9, 7, 8, 16], table, 4) == [4, 4, 8, 7, 8, 16]
+    assert _advance([0, -2, 3], [9, 4, -1], [[0, 1], [2, -1], [3, 4]], 4) == [8, 4, 0]  # cut at the table's end
+
+
+@pytest.mark.parametrize("B,ps,width,seed", [(1, 1, 300, 0), (70, 16, 100, 1), (4096, 8, 5, 2), (9, 64, 33, 3), (5, 4, 64, 4)])
+def test_advance_parity(B, ps, width, seed):
+    r = np.random.default_rng(seed)
+    cached = r.integers(0, width * ps + 1, B)
+    seq_len = np.minimum(cached + r.integers(0, width * ps, B), width * ps)
+    table, ref = r.integers(0, 1000, (B, width)), []
+    for b in range(B):
+        have, need = -(-int(cached[b]) // ps), -(-int(seq_len[b]) // ps)
+        cut = int(r.integers(have, need + 1))  # the list ran out from this page on
+        table[b, cut:] = -1
+        ref.append(min(int(seq_len[b]), cut * ps) if cut < need else int(seq_len[b]))
+    assert _advance(list(cached), list(seq_len), table, ps) == ref
+
+
+def test_advance_refusals():
+    c, n, t = _i32([1, 2]), _i32([2, 2]), _i32([[0], [1]])
+    for args in ((c, n[:1], t, 4), (c, n, t[:1], 4), (c, n.long(), t, 4), (c.cpu(), n, t, 4)):
+        with pytest.raises(ValueError):
+            dm.decomoe_paged_advance(*args)
+    for args, kw in (((c, c, t, 4), {}), ((c, n, t, 5), {}), ((t.view(-1), n, t, 4), {}), ((c, n, t, 4), {"free_head": _i32([0])})):
+        with pytest.raises(dm.DecomoeError) as e:
+            dm.decomoe_paged_advance(*args, **kw)
+        assert e.value.code == dm.DECOMOE_ERR_INVALID_ARG
+    assert c.tolist() == [1, 2]
