@@ -612,7 +612,7 @@ DECOMOE_API int decomoe_attention(const void* q, int64_t n, const void* k_cache,
  * length counts as 0; where the list runs out, the table gets -1; where the
  * table is too narrow, the request ends at max_pages * page_size rows; a row
  * without a page (or whose held page is negative) has slot -1; rows past N are
- * left out. seq_len must not overlap cached or fresh, nor free_head_out free_head.
+ * left out. Outputs overlap neither inputs nor one another.
  * positions may be NULL. One launch, no host synchronisation.
  *
  * decomoe_paged_plan_step: the same for a decode step, in which request b has row b:
@@ -624,15 +624,15 @@ DECOMOE_API int decomoe_attention(const void* q, int64_t n, const void* k_cache,
  * *free_head = *free_head_out (both may be NULL). Rows that got no page do not count:
  * where the list ran out, a request ends in front of the first page that it asked for
  * and did not get (a negative entry), so that a later plan can give it one. A length
- * beyond max_pages * page_size is cut there. cached must overlap neither seq_len nor
- * block_table.
+ * beyond max_pages * page_size is cut there. cached and free_head overlap no other array.
  *
  * decomoe_paged_append: the step's new rows into their slots, keys and values
  * in one launch. k_new, v_new: [N, width] dtype (bf16 or f32), rows
  * k_row_stride and v_row_stride elements apart (the rows of a fused projection
  * can be read in place); k_pages, v_pages: the pools, width = Hkv * D. A slot
  * of -1 is skipped; one outside the pool is skipped and marks
- * DECOMOE_ERR_BAD_INPUT. Two rows of the same slot: either may remain. width
+ * DECOMOE_ERR_BAD_INPUT. Two rows of the same slot: either may remain; new rows that lie
+ * in the pools themselves must not be rows that the call writes. width
  * and strides are multiples of 16 bytes, pointers 16-byte aligned.
  *
  * decomoe_paged_attention: one new token per request over its cache, which
@@ -657,7 +657,7 @@ DECOMOE_API int decomoe_attention(const void* q, int64_t n, const void* k_cache,
  * joins in key order. Deterministic: the same call gives the same bits, but the
  * last bits of a row depend on the other requests of the call and on the number
  * of SMs. ws: decomoe_paged_attention_workspace_bytes(...) bytes, 16-byte
- * aligned, any content. No host synchronisation: lengths, tables and slots
+ * aligned, any content; out and ws overlap nothing else. No host synchronisation: lengths, tables and slots
  * stay on the device, so a captured step can be replayed as they grow.
  * ------------------------------------------------------------------------ */
 DECOMOE_API int decomoe_paged_plan(const int32_t* cached, const int32_t* fresh, int64_t B, int page_size,
@@ -696,7 +696,8 @@ DECOMOE_API int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t
  * x, residual, sum_out, y: [T, d] dtype (bf16 or f32); weight: [d] dtype;
  * y8: [T, d] bytes (e4m3); y8_scale: [T] fp32. sum_out, y and the pair y8,
  * y8_scale may each be NULL (not wanted). fp32 math on the unrounded s, each
- * output rounded once. sum_out may be residual or x, y may be x (not both x).
+ * output rounded once. sum_out may be residual or x, y may be x or residual (not
+ * both the same); no output overlaps anything otherwise.
  * Rows of a multiple of 16 bytes, 16-byte aligned pointers (y8: 8-byte).
  *
  * decomoe_w4_linear: out[t, n] = sum_k x[t, k] * w[n, k] for a matrix in 4
@@ -706,7 +707,7 @@ DECOMOE_API int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t
  * x: [T, K] rows x_stride elements apart, x_dtype DECOMOE_BF16 (x_scale NULL)
  * or DECOMOE_E4M3 with x_scale [T] fp32, one factor per row (as
  * decomoe_add_rmsnorm_q8 leaves them). out: [T, N] contiguous, out_dtype
- * DECOMOE_BF16 or DECOMOE_F32. Products x (q - 8) are exact (a weight of zero adds
+ * DECOMOE_BF16 or DECOMOE_F32, and overlaps no input. Products x (q - 8) are exact (a weight of zero adds
  * nothing, however large its x), sums of a group and over the groups fp32, scales
  * applied to whole group sums, one rounding at the end: what the sums lose goes by
  * the sum of |x (q - 8) scale|. A row with a value that is not finite gives values that

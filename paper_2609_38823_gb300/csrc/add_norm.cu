@@ -192,6 +192,17 @@ extern "C" int decomoe_add_rmsnorm_q8(const void* x, const void* residual, const
   DM_ARG_CHECK(row_bytes % 16 == 0 && aligned16(x) && aligned16(residual) && aligned16(weight) && aligned16(sum_out) &&
                    aligned16(y) && (reinterpret_cast<uintptr_t>(y8) & 7u) == 0,
                "add_rmsnorm_q8: rows must be 16-byte multiples, pointers aligned");
+  // an output may be an input, element for element, but not lie across its rows
+  const size_t all = static_cast<size_t>(T) * static_cast<size_t>(row_bytes);
+  const Bytes in[] = {{x, all}, {residual, all}, {weight, static_cast<size_t>(row_bytes)}};
+  const Bytes outs[] = {{sum_out, all}, {y, all}, {y8, static_cast<size_t>(T) * static_cast<size_t>(d)},
+                        {y8_scale, static_cast<size_t>(T) * sizeof(float)}};
+  for (int i = 0; i < 4; ++i) {
+    bool apart = true;
+    for (int j = 0; j < 3; ++j) apart &= !overlaps(outs[i], {in[j]}) || (i < 2 && j < 2 && outs[i].p == in[j].p);
+    for (int j = 0; j < i; ++j) apart &= !overlaps(outs[i], {outs[j]});
+    DM_ARG_CHECK(apart, "add_rmsnorm_q8: an output overlaps an input or another output");
+  }
   AddNormArgs a = {};
   a.x = static_cast<const uint4*>(x);
   a.res = static_cast<const uint4*>(residual);

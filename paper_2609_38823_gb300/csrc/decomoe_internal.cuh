@@ -104,6 +104,21 @@ inline cudaError_t launch_pdl_late(void (*kern)(KArgs...), dim3 grid, dim3 block
   return cudaLaunchKernelEx(&cfg, kern, static_cast<KArgs>(args)...);
 }
 
+// The bytes that a call reads or writes at a pointer, and whether an output's are among
+// those of others (calls refuse that where blocks would read what others have written).
+struct Bytes {
+  const void* p;
+  size_t n;
+};
+inline bool overlaps(const Bytes& a, std::initializer_list<Bytes> others) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p);
+  for (const Bytes& b : others) {
+    const uintptr_t y = reinterpret_cast<uintptr_t>(b.p);
+    if (a.p != nullptr && b.p != nullptr && a.n > 0 && b.n > 0 && x < y + b.n && y < x + a.n) return true;
+  }
+  return false;
+}
+
 // Internal entry points shared between translation units.
 // TMA map of a 2-D bf16 tensor [outer, inner] row-major; box = box_outer rows x
 // box_inner columns (64 -> 128-byte swizzle, 32 -> 64-byte swizzle), zero fill

@@ -214,11 +214,6 @@ __global__ void __launch_bounds__(256)
   pdl_trigger();
 }
 
-static bool ranges_overlap(const void* p, size_t n, const void* q, size_t m) {
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return a < b + m && b < a + n;
-}
-
 static int plan_call(const char* name, bool by_request, const int32_t* cached, const int32_t* fresh, int64_t B,
                      int page_size, const int32_t* free_pages, int64_t n_free, const int32_t* free_head,
                      int32_t* free_head_out, int32_t* block_table, int64_t max_pages, int32_t* seq_len,
@@ -232,10 +227,16 @@ static int plan_call(const char* name, bool by_request, const int32_t* cached, c
   DM_ARG_CHECK((by_request || row_start != nullptr) && (N == 0 || slot_map != nullptr) && (n_free == 0 || free_pages != nullptr),
                "%s: null pointer", name);
   DM_ARG_CHECK(B == 0 || (cached && fresh && seq_len && (block_table || max_pages == 0)), "%s: null pointer", name);
-  const size_t bytes = static_cast<size_t>(B) * sizeof(int32_t);
-  DM_ARG_CHECK(!ranges_overlap(cached, bytes, seq_len, bytes) && !ranges_overlap(fresh, bytes, seq_len, bytes),
-               "%s: seq_len overlaps cached or fresh", name);
-  DM_ARG_CHECK(free_head_out == nullptr || free_head_out != free_head, "%s: free_head_out is free_head", name);
+  const size_t one = sizeof(int32_t), each = static_cast<size_t>(B) * one;
+  const Bytes in[] = {{cached, each}, {fresh, each}, {free_pages, static_cast<size_t>(n_free) * one}, {free_head, one}};
+  const Bytes out[] = {{block_table, each * static_cast<size_t>(max_pages)}, {seq_len, each}, {row_start, each + one},
+                       {slot_map, static_cast<size_t>(N) * one}, {positions, static_cast<size_t>(N) * one},
+                       {free_head_out, one}};
+  for (size_t i = 0; i < sizeof(out) / sizeof(out[0]); ++i) {
+    bool apart = !overlaps(out[i], {in[0], in[1], in[2], in[3]});
+    for (size_t j = 0; j < i; ++j) apart &= !overlaps(out[i], {out[j]});
+    DM_ARG_CHECK(apart, "%s: an output overlaps an input or another output", name);
+  }
   PlanArgs a = {};
   a.cached = cached;
   a.fresh = fresh;
@@ -296,10 +297,11 @@ int decomoe_paged_advance(int32_t* cached, const int32_t* seq_len, const int32_t
                "paged_advance: max_pages * page_size must be in [0, 2^31)");
   DM_ARG_CHECK(B == 0 || (cached && seq_len && (block_table || max_pages == 0)), "paged_advance: null pointer");
   DM_ARG_CHECK((free_head == nullptr) == (free_head_out == nullptr), "paged_advance: free_head and free_head_out go together");
-  const size_t bytes = static_cast<size_t>(B) * sizeof(int32_t);
-  DM_ARG_CHECK(!ranges_overlap(cached, bytes, seq_len, bytes) &&
-                   !ranges_overlap(cached, bytes, block_table, bytes * static_cast<size_t>(max_pages)),
-               "paged_advance: cached overlaps seq_len or block_table");
+  const size_t each = static_cast<size_t>(B) * sizeof(int32_t);
+  const Bytes lens = {seq_len, each}, table = {block_table, each * static_cast<size_t>(max_pages)};
+  DM_ARG_CHECK(!overlaps({cached, each}, {lens, table}) &&
+                   !overlaps({free_head, sizeof(int32_t)}, {{cached, each}, lens, table}),
+               "paged_advance: cached or free_head overlaps another array");
   const int grid = static_cast<int>(std::max<int64_t>(1, (B * 32 + 255) / 256));
   DM_CUDA_CHECK(launch_pdl(k_paged_advance, dim3(grid), dim3(256), 0, reinterpret_cast<cudaStream_t>(stream), cached,
                            seq_len, block_table, static_cast<int>(B), max_pages,

@@ -735,6 +735,21 @@ int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t B, const vo
     return DECOMOE_ERR_WORKSPACE;
   }
   DM_ARG_CHECK(aligned16(ws), "paged_attention: workspace must be 16-byte aligned");
+  {
+    const size_t each = static_cast<size_t>(B) * sizeof(int32_t);
+    const size_t pool = num_pages == 0 ? 0 : static_cast<size_t>((num_pages - 1) * page_stride + static_cast<int64_t>(page_size) * Hkv * D) * 2;
+    const Bytes in[] = {{q, static_cast<size_t>((B - 1) * q_stride + static_cast<int64_t>(Hq) * D) * 2},
+                        {k_pages, pool},
+                        {v_pages, pool},
+                        {block_table, each * static_cast<size_t>(max_pages)},
+                        {seq_len, each},
+                        {hide_begin, each},
+                        {hide_count, each}};
+    const Bytes o = {out, static_cast<size_t>(B) * Hq * D * 2}, w = {ws, decomoe_paged_attention_workspace_bytes(B, Hq, Hkv, D)};
+    bool apart = !overlaps(o, {w});
+    for (const Bytes& b : in) apart &= !overlaps(o, {b}) && !overlaps(w, {b});
+    DM_ARG_CHECK(apart, "paged_attention: out or the workspace overlaps an input or one another");
+  }
   PagedArgs a = {};
   a.q = static_cast<const __nv_bfloat16*>(q);
   a.k = static_cast<const __nv_bfloat16*>(k_pages);

@@ -615,6 +615,12 @@ extern "C" int decomoe_w4_linear(const void* x, int x_dtype, int64_t x_stride, c
                    (reinterpret_cast<uintptr_t>(w_scale) & 1u) == 0 &&
                    reinterpret_cast<uintptr_t>(out) % dtype_bytes(out_dtype) == 0,
                "w4_linear: x_stride must be at least K and a multiple of 16 bytes, x and w 16-byte aligned");
+  DM_ARG_CHECK(!overlaps({out, static_cast<size_t>(T * N) * dtype_bytes(out_dtype)},
+                         {{x, static_cast<size_t>(((T - 1) * x_stride + K) * xe)},
+                          {x_scale, static_cast<size_t>(T) * sizeof(float)},
+                          {w, static_cast<size_t>(N) * static_cast<size_t>(K / 2)},
+                          {w_scale, static_cast<size_t>(N) * static_cast<size_t>(K / group) * 2}}),
+               "w4_linear: out overlaps an input");
   W4Args a = {};
   a.x = x;
   a.xs = x_scale;
