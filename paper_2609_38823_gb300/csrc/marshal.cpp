@@ -8,6 +8,7 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -27,13 +28,24 @@ void need(bool ok, const char* what) {
   if (!ok) refuse(PyExc_ValueError, what);
 }
 
+// The device of the tensors of the call that is being marshalled; -1: none seen yet.
+thread_local int device_seen = -1;
+
 // A strided device tensor argument; null for None where that is allowed.
 const at::Tensor* tensor(PyObject* o, const char* what, bool none_ok = false) {
   if (o == Py_None && none_ok) return nullptr;
   if (!THPVariable_Check(o)) refuse(PyExc_TypeError, std::string(what) + ": a tensor expected");
   const at::Tensor& t = THPVariable_Unpack(o);
   if (t.layout() != at::kStrided || !t.is_cuda()) refuse(PyExc_ValueError, std::string(what) + ": device tensors expected");
+  const int at = static_cast<int>(t.get_device());
+  if (device_seen >= 0 && at != device_seen) refuse(PyExc_ValueError, std::string(what) + ": all tensors must be on one device");
+  device_seen = at;
   return &t;
+}
+// Launches, streams and the number of SMs go by the current device.
+void on_current(const char* what) {
+  if (device_seen >= 0 && device_seen != static_cast<int>(c10::cuda::current_device()))
+    refuse(PyExc_ValueError, std::string(what) + ": the tensors are not on the current device");
 }
 const at::Tensor* whole(PyObject* o, const char* what, bool none_ok = false) {
   const at::Tensor* t = tensor(o, what, none_ok);
@@ -123,6 +135,7 @@ int paged_plan(PyObject* const* a) {
            (status == nullptr || status->numel() >= 1),
        "paged_plan: cached, fresh, seq_len [B], row_start [B + 1], block_table [B, max_pages], free_pages [n], slot_map "
        "and positions [N], free_head and free_head_out [1] expected");
+  on_current(n);
   return decomoe_paged_plan(ptr<int32_t>(cached), ptr<int32_t>(fresh), B, to_int(a[2]), ptr<int32_t>(pages), pages->numel(),
                             ptr<int32_t>(head), ptr<int32_t>(head_out), ptr<int32_t>(table), table->size(1),
                             ptr<int32_t>(len), ptr<int32_t>(start), ptr<int32_t>(slots), ptr<int32_t>(pos), N,
@@ -143,6 +156,7 @@ int paged_plan_step(PyObject* const* a) {
            (status == nullptr || status->numel() >= 1),
        "paged_plan_step: cached, fresh, seq_len, slot_map and positions [B], block_table [B, max_pages], free_pages [n], "
        "free_head and free_head_out [1] expected");
+  on_current(n);
   return decomoe_paged_plan_step(ptr<int32_t>(cached), ptr<int32_t>(fresh), B, to_int(a[2]), ptr<int32_t>(pages),
                                  pages->numel(), ptr<int32_t>(head), ptr<int32_t>(head_out), ptr<int32_t>(table),
                                  table->size(1), ptr<int32_t>(len), ptr<int32_t>(slots), ptr<int32_t>(pos),
@@ -158,6 +172,7 @@ int paged_advance(PyObject* const* a) {
   need(cached->dim() == 1 && shaped(len, {B}) && table->dim() == 2 && table->size(0) == B &&
            (head == nullptr || head->numel() == 1) && (head_out == nullptr || head_out->numel() == 1),
        "paged_advance: cached and seq_len [B], block_table [B, max_pages], free_head and free_head_out [1] expected");
+  on_current(n);
   return decomoe_paged_advance(ptr<int32_t>(cached), ptr<int32_t>(len), ptr<int32_t>(table), B, table->size(1),
                                to_int(a[3]), ptr<int32_t>(head), ptr<int32_t>(head_out), stream(a[6]));
 }
@@ -173,6 +188,7 @@ int paged_append(PyObject* const* a) {
        "paged_append: k_new, v_new [N, Hkv, D] and slot_map [N] expected");
   if (k->scalar_type() != p.k->scalar_type() || v->scalar_type() != p.k->scalar_type())
     refuse(PyExc_TypeError, "paged_append: rows and pools must have one type");
+  on_current(n);
   return decomoe_paged_append(ptr(k), row_stride(*k, n), ptr(v), row_stride(*v, n), N, static_cast<int>(p.hkv * p.d),
                               dtype(*p.k, n), ptr<int32_t>(slots), ptr(p.k), ptr(p.v), p.pages, static_cast<int>(p.ps),
                               p.stride, ptr<int32_t>(status), stream(a[6]));
@@ -193,6 +209,7 @@ int paged_attention(PyObject* const* a) {
        "paged_attention: block_table [B, max_pages], seq_len, hide_begin and hide_count [B] expected");
   if (q->scalar_type() != at::kBFloat16 || p.k->scalar_type() != at::kBFloat16 || out->scalar_type() != at::kBFloat16)
     refuse(PyExc_TypeError, "paged_attention: q, pools and out must be bf16");
+  on_current(n);
   return decomoe_paged_attention(ptr(q), row_stride(*q, n), B, ptr(p.k), ptr(p.v), p.pages, static_cast<int>(p.ps), p.stride,
                                  ptr<int32_t>(table), table->size(1), ptr<int32_t>(len), ptr<int32_t>(hb), ptr<int32_t>(hc),
                                  static_cast<int>(hq), static_cast<int>(p.hkv), static_cast<int>(p.d), to_float(a[9]),
@@ -215,6 +232,7 @@ int add_rmsnorm_q8(PyObject* const* a) {
        "add_rmsnorm_q8: y8 [T, d] float8_e4m3fn expected");
   need(scale == nullptr || (scale->numel() == T && scale->scalar_type() == at::kFloat),
        "add_rmsnorm_q8: y8_scale [T] float32 expected");
+  on_current(n);
   return decomoe_add_rmsnorm_q8(ptr(x), ptr(res), ptr(w), T, static_cast<int>(d), to_float(a[7]), dtype(*x, n), ptr(sum),
                                 ptr(y), ptr(y8), ptr<float>(scale), stream(a[8]));
 }
@@ -237,6 +255,7 @@ int w4_linear(PyObject* const* a) {
     need(xs != nullptr && xs->scalar_type() == at::kFloat && xs->numel() == T, "w4_linear: e4m3 rows need x_scale [T] float32");
   else
     xt = dtype(*x, n);
+  on_current(n);
   return decomoe_w4_linear(ptr(x), xt, row_stride(*x, n), ptr<float>(xs), T, static_cast<int>(K), ptr(w), ptr(ws),
                            static_cast<int>(K / groups), N, ptr(out), dtype(*out, n), stream(a[5]));
 }
@@ -244,6 +263,7 @@ int w4_linear(PyObject* const* a) {
 template <int (*F)(PyObject* const*), int ARGS>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
   try {
+    device_seen = -1;
     if (n != ARGS) refuse(PyExc_TypeError, "wrong number of arguments");
     return PyLong_FromLong(F(args));
   } catch (const Refused& e) {
