@@ -89,3 +89,30 @@ def test_large_values_on_the_code_of_zero(kind, N, K, group, T):
     again = torch.empty_like(out)
     dm.decomoe_w4_linear(x.to(kind), w, ws, again, x_scale=xs)
     assert torch.equal(out, again)
+
+
+@pytest.mark.parametrize("kind", [BF16, E4M3])
+@pytest.mark.parametrize("N,K", [SMALL, LARGE])
+def test_values_that_are_not_finite(kind, N, K):
+    """NaN in a row makes all of it NaN; an infinity (bf16) gives the infinity of its weight's
+    sign, NaN on a weight of zero; the other rows keep their bits."""
+    w, ws = _weights(N, K, 64, 3)
+    ws = ws.abs() + 2.0 ** -10
+    x = torch.randn(11, K, device=DEV).to(kind)
+    xs = torch.ones(11, device=DEV) if kind == E4M3 else None
+    out = [torch.empty(11, N, dtype=F32, device=DEV) for _ in range(2)]
+    dm.decomoe_w4_linear(x, w, ws, out[0], x_scale=xs)
+    x[2, 70] = float("nan")
+    if kind == BF16:
+        x[9, 130], x[4, 131] = float("inf"), -float("inf")
+    dm.decomoe_w4_linear(x, w, ws, out[1], x_scale=xs)
+    assert torch.isnan(out[1][2]).all()
+    keep = [0, 1, 3, 5, 6, 7, 8, 10]
+    assert torch.equal(out[0][keep], out[1][keep])
+    if kind == BF16:
+        for t, q, sign in ((9, (w[:, 65] & 15).int() - 8, 1.0), (4, (w[:, 65] >> 4).int() - 8, -1.0)):
+            ref = torch.where(q == 0, float("nan"), sign * torch.sign(q.float()) * float("inf"))
+            assert torch.equal(torch.nan_to_num(out[1][t], nan=0.5, posinf=2.0, neginf=-2.0),
+                               torch.nan_to_num(ref, nan=0.5, posinf=2.0, neginf=-2.0))
+    else:
+        assert torch.equal(out[0][[4, 9]], out[1][[4, 9]])
