@@ -31,7 +31,9 @@ bool discard_scratch() { return g_discard_scratch.load(std::memory_order_relaxed
 
 // Programmatic launch pays for grids of at most one block per SM (the
 // persistent GEMMs and the decode-size kernels); kernels of many blocks ran
-// slower with it, so they launch plainly. decomoe_set_pdl(0) turns it off.
+// slower with it where they let the next kernel in at their start, so they launch
+// plainly, but for those that do so when their loads are done (launch_pdl_late).
+// decomoe_set_pdl(0) turns it off.
 static std::atomic<int> g_pdl{1};
 bool pdl_enabled(int64_t blocks) {
   return g_pdl.load(std::memory_order_relaxed) != 0 && blocks <= static_cast<int64_t>(sm_count());
