@@ -686,6 +686,59 @@ DECOMOE_API int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t
                                         decomoe_stream_t stream);
 
 /* ------------------------------------------------------------------------
+ * A paged key-value cache in 4 bits: the cache above at a quarter of its size. Plan,
+ * advance, tables and slots are the same calls and arrays; the pool of one layer is one
+ * array of bytes, [num_pages, Hkv, page_size / 8, tile], page_stride bytes (a multiple of
+ * 16) between pages. A tile holds eight consecutive rows of a KV head:
+ *   key codes [8, D / 2], key parameters [8, D / group, 2] bf16 (step, low), value codes,
+ *   value parameters: 16 * (D / 2 + 4 * D / group) bytes.
+ * A code q in 0..15 of a group of features stands for low + step * q. Two codes to a byte, the
+ * first in the low four bits; the 32-bit word c * (D / 32) + i of a row of key codes holds
+ * features 32 i + 8 c .. + 7, the 16-bit word r * (D / 32) + i of a row of value codes
+ * features 32 i + 4 r .. + 3. D 64 with groups of 32 or 64, or D 128 with groups of 32, 64
+ * or 128; page_size a power of two, 8 at least. The pool is 16-byte aligned; any content
+ * will do at the start. decomoe_paged_q4_page_bytes: a page's bytes (0: no such shape).
+ *
+ * decomoe_paged_append_q4: new rows into their slots, as decomoe_paged_append. k_new, v_new:
+ * [N, Hkv, D] bf16, rows k_row_stride and v_row_stride elements apart (multiples of 8). Of
+ * each group low = its least value, step = (its largest - low) / 15 rounded to bf16, q =
+ * (x - low) / step to the nearest (ties to the even code), at most 15. A group with a value
+ * that is not finite, or whose range fp32 cannot hold, reads back as NaN. A slot of -1 is
+ * skipped; any other outside the pool is skipped and marks DECOMOE_ERR_BAD_INPUT. Slots
+ * differ: of two rows of one slot codes and parameters may remain mixed.
+ *
+ * decomoe_paged_read_q4: rows of the cache in bf16, low + step * q in fp32 and then rounded: k_out, v_out
+ * [N, Hkv, D], rows k_row_stride and v_row_stride elements apart (k_out and v_out may be slices of the
+ * same rows), for what attends over several rows at a time (a prompt's next chunk:
+ * decomoe_attention over the rows read). A slot of -1 leaves its row as it was; any other outside the pool
+ * does too and marks DECOMOE_ERR_BAD_INPUT. The outputs overlap no input.
+ *
+ * decomoe_paged_attention_q4: decomoe_paged_attention over such a pool, with the same
+ * arguments otherwise and the same readings of lengths, hidden rows, tables, status,
+ * shares and bits. Keys and values are low + step * q, not rounded on the way; weights times steps
+ * are rounded to bf16 for the value product, all else is fp32. A group that reads back as NaN, or a query
+ * that is not finite, gives NaN in its own request and KV head. ws:
+ * decomoe_paged_attention_q4_workspace_bytes(...) bytes. A wait for a copy that runs past the
+ * time limit records DECOMOE_ERR_TIMEOUT in status_dev.
+ * ------------------------------------------------------------------------ */
+DECOMOE_API size_t decomoe_paged_q4_page_bytes(int page_size, int Hkv, int D, int group);
+DECOMOE_API int decomoe_paged_append_q4(const void* k_new, int64_t k_row_stride, const void* v_new, int64_t v_row_stride,
+                                        int64_t N, int Hkv, int D, int group, const int32_t* slot_map, void* pages,
+                                        int64_t num_pages, int page_size, int64_t page_stride, int32_t* status_dev,
+                                        decomoe_stream_t stream);
+DECOMOE_API int decomoe_paged_read_q4(const int32_t* slot_map, int64_t N, const void* pages, int64_t num_pages,
+                                      int page_size, int64_t page_stride, int Hkv, int D, int group, void* k_out,
+                                      int64_t k_row_stride, void* v_out, int64_t v_row_stride, int32_t* status_dev,
+                                      decomoe_stream_t stream);
+DECOMOE_API size_t decomoe_paged_attention_q4_workspace_bytes(int64_t B, int Hq, int Hkv, int D);
+DECOMOE_API int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const void* pages,
+                                           int64_t num_pages, int page_size, int64_t page_stride, int group,
+                                           const int32_t* block_table, int64_t max_pages, const int32_t* seq_len,
+                                           const int32_t* hide_begin, const int32_t* hide_count, int Hq, int Hkv, int D,
+                                           float scale, void* out, void* ws, size_t ws_bytes, int32_t* status_dev,
+                                           decomoe_stream_t stream);
+
+/* ------------------------------------------------------------------------
  * The dense steps around the attention of a decode layer (base-model steps
  * that the method leaves unchanged).
  *
@@ -722,6 +775,27 @@ DECOMOE_API int decomoe_add_rmsnorm_q8(const void* x, const void* residual, cons
 DECOMOE_API int decomoe_w4_linear(const void* x, int x_dtype, int64_t x_stride, const float* x_scale, int64_t T, int K,
                                   const void* w, const void* w_scale, int group, int64_t N, void* out, int out_dtype,
                                   decomoe_stream_t stream);
+
+/* ------------------------------------------------------------------------
+ * decomoe_token_logprobs: what a server returns beside the tokens, from the logits of the last
+ * layer (as decomoe_w4_linear leaves them). logits: [T, V] bf16 or f32, rows row_stride elements
+ * apart (any stride from V on, any alignment of the type). With p = softmax(scale * logits
+ * [t]) (scale: 1 / temperature, positive):
+ *   logprob[t] = ln p[tokens[t]]; entropy[t] = -sum p ln p;
+ *   top_id, top_logprob [T, n]: the n <= 32 largest logits of the row, largest first, the
+ *   lowest index first among equals, and their ln p.
+ * A row whose token is negative is padding: its logits are not read, its outputs left as they
+ * were; a token of V or more too, and it marks DECOMOE_ERR_BAD_INPUT. tokens NULL: all rows, no
+ * logprob. logprob, entropy, top_id and top_logprob may each be NULL (not wanted; without the last
+ * two n does not matter). fp32 throughout, each row in a fixed order: the same call gives the same
+ * bits (the last ones go by T, V, the rows' alignment and the number of SMs). Logits of minus infinity have probability 0; a row of
+ * nothing else gives -inf and an entropy of 0. NaN or +inf anywhere in a row make its
+ * probabilities NaN; among alternatives NaN ranks as minus infinity. V <= 2^24, T <= (2^31 - 1) / 16. One launch, no
+ * workspace, no host synchronisation; no output overlaps anything else.
+ * ------------------------------------------------------------------------ */
+DECOMOE_API int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, int64_t row_stride, int dtype,
+                                       const int32_t* tokens, float scale, int n, float* logprob, float* entropy,
+                                       int32_t* top_id, float* top_logprob, int32_t* status_dev, decomoe_stream_t stream);
 
 /* ------------------------------------------------------------------------
  * Bounded-wait status. Kernels that wait on device barriers give up after a

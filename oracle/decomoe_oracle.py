@@ -563,3 +563,94 @@ def w4_dequant(w, w_scale):
     q = np.stack([w % 16, w // 16], axis=-1).reshape(w.shape[0], -1) - 8
     s = np.asarray(w_scale, F64)
     return q * np.repeat(s, q.shape[1] // s.shape[1], axis=1)
+
+
+# ------------------------------------------------- a cache in 4 bits
+
+def bf16(x):
+    """Values rounded to bf16 (to nearest, ties to even) by way of fp32."""
+    u = np.ascontiguousarray(np.asarray(x, np.float64).astype(np.float32)).view(np.uint32).astype(np.uint64)
+    r = ((u + 0x7fff + ((u >> 16) & 1)) >> 16 << 16).astype(np.uint32).view(np.float32).astype(F64)
+    return np.where(np.isnan(np.asarray(x, F64)), np.nan, r)
+
+
+def q4_quantise(x, group):
+    """(codes [..., D], step [..., D / group], low [..., D / group]) of rows x of bf16 values:
+    low the group's least value, step (largest - low) / 15 rounded to bf16, the nearest code
+    (ties to even). A group with a value that is not finite: codes 0, NaN, NaN."""
+    x = np.asarray(x, F64)
+    g = x.reshape(x.shape[:-1] + (-1, group))
+    fine = np.isfinite(g).all(-1)
+    y = np.where(fine[..., None], g, 0.0)
+    low, high = y.min(-1), y.max(-1)
+    step = bf16((high - low) / 15.0)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        q = np.where(step[..., None] > 0, np.rint((y - low[..., None]) / step[..., None]), 0.0)
+    q = np.minimum(q, 15.0)
+    nan = np.where(fine, 0.0, np.nan)
+    return q.reshape(x.shape).astype(np.int64), step + nan, low + nan
+
+
+def _q4_places(D, value):
+    """Nibble of feature f in a row of codes."""
+    f = np.arange(D)
+    lanes, run = (8, 4) if value else (4, 8)
+    return ((f % 32) // run * (D // 32) + f // 32) * run + f % run
+
+
+def q4_rows_to_tile(codes, step, low, value):
+    """Bytes of eight rows [8, D]: codes, then parameters."""
+    D = codes.shape[1]
+    nib = np.zeros((8, D), np.int64)
+    nib[:, _q4_places(D, value)] = codes
+    par = np.stack([step, low], -1).astype(np.float32).view(np.uint32) >> 16
+    return np.concatenate([(nib[:, 0::2] + 16 * nib[:, 1::2]).astype(np.uint8).reshape(-1),
+                           par.astype("<u2").reshape(-1).view(np.uint8)])
+
+
+def q4_values(pages, D, group):
+    """(keys, values, |step (code - 8)| of values) [num_pages, page_size, Hkv, D] of a pool of bytes."""
+    pages = np.asarray(pages)
+    P, H, T, _ = pages.shape
+    G, out = D // group, []
+    half = 4 * D + 32 * G
+    for value in (False, True):
+        part = pages[..., value * half:(value + 1) * half]
+        b = part[..., :4 * D].reshape(P, H, T, 8, D // 2).astype(np.int64)
+        nib = np.stack([b % 16, b // 16], -1).reshape(P, H, T, 8, D)
+        q = nib[..., _q4_places(D, value)]
+        par = np.ascontiguousarray(part[..., 4 * D:]).view("<u2").astype(np.uint32) << 16
+        par = par.view(np.float32).astype(F64).reshape(P, H, T, 8, G, 2)
+        step, low = (np.repeat(par[..., i], group, -1) for i in (0, 1))
+        rows = lambda x: x.reshape(P, H, T * 8, D).transpose(0, 2, 1, 3)  # noqa: E731
+        with np.errstate(invalid="ignore"):
+            out.append(rows(low + step * q))
+            wide = rows(np.abs(step * (q - 8)))
+    return out[0], out[1], wide
+
+
+# ------------------------------------------------- token log probabilities
+
+def token_logprobs(x, tokens, n=0, scale=1.0):
+    """(logprob [T], entropy [T], top_id [T, n], top_logprob [T, n]) of logits x [T, V]: of
+    softmax(scale x); the n largest logits, the lowest index first among equals. Minus
+    infinity alone: -inf and an entropy of 0."""
+    x = np.asarray(x, F64)
+    T = x.shape[0]
+    lp, ent = np.full(T, np.nan), np.full(T, np.nan)
+    ids, top = np.zeros((T, n), np.int64), np.full((T, n), np.nan)
+    for t in range(T):
+        y = scale * x[t]
+        ids[t] = np.argsort(-np.where(np.isnan(x[t]), -np.inf, x[t]), kind="stable")[:n]
+        if np.isnan(y).any() or np.isposinf(y).any():
+            continue
+        m = y.max()
+        if np.isneginf(m):
+            logp, ent[t] = np.full(y.shape, -np.inf), 0.0
+        else:
+            logp = y - m - np.log(np.exp(y - m).sum())
+            p = np.exp(logp)
+            ent[t] = -(p[p > 0] * logp[p > 0]).sum()
+        lp[t] = logp[tokens[t]]
+        top[t] = logp[ids[t]]
+    return lp, ent, ids, top

@@ -97,6 +97,13 @@ SIGNATURES = {
     "decomoe_paged_plan_step": (_I, [_P, _P, _L, _I, _P, _L, _P, _P, _P, _L, _P, _P, _P, _P, _P]),
     "decomoe_paged_advance": (_I, [_P, _P, _P, _L, _L, _I, _P, _P, _P]),
     "decomoe_paged_append": (_I, [_P, _L, _P, _L, _L, _I, _I, _P, _P, _P, _L, _I, _L, _P, _P]),
+    "decomoe_paged_q4_page_bytes": (_S, [_I, _I, _I, _I]),
+    "decomoe_paged_append_q4": (_I, [_P, _L, _P, _L, _L, _I, _I, _I, _P, _P, _L, _I, _L, _P, _P]),
+    "decomoe_paged_read_q4": (_I, [_P, _L, _P, _L, _I, _L, _I, _I, _I, _P, _L, _P, _L, _P, _P]),
+    "decomoe_paged_attention_q4_workspace_bytes": (_S, [_L, _I, _I, _I]),
+    "decomoe_paged_attention_q4": (_I, [_P, _L, _L, _P, _L, _I, _L, _I, _P, _L, _P, _P, _P, _I, _I, _I, _F, _P, _P, _S,
+                                        _P, _P]),
+    "decomoe_token_logprobs": (_I, [_P, _L, _L, _L, _I, _P, _F, _I, _P, _P, _P, _P, _P, _P]),
     "decomoe_paged_attention_workspace_bytes": (_S, [_L, _I, _I, _I]),
     "decomoe_paged_attention": (_I, [_P, _L, _L, _P, _P, _L, _I, _L, _P, _L, _P, _P, _P, _I, _I, _I, _F, _P, _P, _S,
                                      _P, _P]),
@@ -687,6 +694,55 @@ def decomoe_paged_attention(q, k_pages, v_pages, block_table, seq_len, out, ws, 
                                     status, None if stream is None else stream.cuda_stream)
     if code:
         _check("decomoe_paged_attention", code)
+
+
+def decomoe_paged_q4_page_bytes(page_size, Hkv, D, group):
+    """Bytes of a page of a cache in 4 bits."""
+    return int(lib().decomoe_paged_q4_page_bytes(page_size, Hkv, D, group))
+
+
+def decomoe_paged_append_q4(k_new, v_new, slot_map, pages, status=None, stream=None):
+    """New key and value rows [N, Hkv, D] bf16 (rows may be slices of wider ones) in 4
+    bits into their slots of the pool [num_pages, Hkv, page_size / 8, tile bytes] uint8; the
+    size of a tile says how many features share a step."""
+    code = _calls().paged_append_q4(k_new, v_new, slot_map, pages, status, None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_paged_append_q4", code)
+
+
+def decomoe_paged_read_q4(slot_map, pages, k_out, v_out, status=None, stream=None):
+    """Rows of a cache in 4 bits as bf16 [N, Hkv, D], for what attends over several rows
+    at a time; a row of slot -1 is left as it was."""
+    code = _calls().paged_read_q4(slot_map, pages, k_out, v_out, status, None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_paged_read_q4", code)
+
+
+def decomoe_paged_attention_q4_workspace_bytes(B, Hq, Hkv, D):
+    return int(lib().decomoe_paged_attention_q4_workspace_bytes(B, Hq, Hkv, D))
+
+
+def decomoe_paged_attention_q4(q, pages, block_table, seq_len, out, ws, hide_begin=None, hide_count=None, scale=0.0,
+                               status=None, stream=None):
+    """decomoe_paged_attention over a pool in 4 bits [num_pages, Hkv, page_size / 8, tile
+    bytes]."""
+    code = _calls().paged_attention_q4(q, pages, block_table, seq_len, out, ws, hide_begin, hide_count, scale, status,
+                                       None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_paged_attention_q4", code)
+
+
+def decomoe_token_logprobs(logits, tokens, logprob=None, entropy=None, top_id=None, top_logprob=None, scale=1.0,
+                           status=None, stream=None):
+    """From logits [T, V] (bf16 or f32, rows may be slices of wider ones): the log
+    probability of each row's token (int32 [T]; negative: a padded row, left as it was),
+    the row's entropy, and its n most probable tokens with their log probabilities
+    (top_id int32, top_logprob f32 [T, n], n <= 32), of softmax(scale * logits). tokens
+    and each output may be None."""
+    code = _calls().token_logprobs(logits, tokens, logprob, entropy, top_id, top_logprob, scale, status,
+                                   None if stream is None else stream.cuda_stream)
+    if code:
+        _check("decomoe_token_logprobs", code)
 
 
 def decomoe_add_rmsnorm_q8(x, residual, weight, sum_out=None, y=None, y8=None, y8_scale=None, eps=1e-6, stream=None):

@@ -23,7 +23,7 @@ LIB = os.path.join(HERE, "libdecomoe.so")
 EXT = os.path.join(HERE, "_marshal.so")
 
 CU_SOURCES = ["api.cu", "route.cu", "dispatch.cu", "expert_gemm.cu", "combine_compact.cu", "calib_gate.cu", "layer.cu", "decode_layer.cu", "attention.cu",
-              "paged.cu", "paged_attention.cu", "add_norm.cu", "w4_linear.cu"]
+              "paged.cu", "paged_attention.cu", "paged_q4.cu", "paged_attention_q4.cu", "add_norm.cu", "w4_linear.cu", "logprobs.cu"]
 C_SOURCES = ["prefix.c"]
 EXT_SOURCE = "marshal.cpp"
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

@@ -102,6 +102,28 @@ Pool pool(PyObject* k, PyObject* v, const char* what) {
   return p;
 }
 
+// The pool of a cache in 4 bits, [num_pages, Hkv, page_size / 8, tile bytes], for heads of d.
+struct Pool4 {
+  const at::Tensor* t;
+  int64_t pages, ps, hkv, group, stride;
+};
+Pool4 pool4(PyObject* o, int64_t d, const char* what) {
+  Pool4 p = {};
+  p.t = tensor(o, what);
+  if (p.t->dim() != 4 || p.t->scalar_type() != at::kByte)
+    refuse(PyExc_ValueError, std::string(what) + ": a pool [num_pages, Hkv, page_size / 8, tile bytes] uint8 expected");
+  p.pages = p.t->size(0);
+  p.hkv = p.t->size(1);
+  p.ps = 8 * p.t->size(2);
+  const int64_t groups = d > 0 && d <= 128 ? (p.t->size(3) - 8 * d) / 64 : 0;
+  if (groups < 1 || groups > d || d % groups != 0 || p.t->size(3) != 8 * d + 64 * groups)
+    refuse(PyExc_ValueError, std::string(what) + ": a tile of the pool has 16 * (D / 2 + 4 * D / group) bytes");
+  p.group = d / groups;
+  p.stride = row_stride(*p.t, what);
+  need(p.hkv <= INT32_MAX && p.t->size(2) <= INT32_MAX / 8, "pool: sizes out of range");
+  return p;
+}
+
 int to_int(PyObject* o) {
   const long v = PyLong_AsLong(o);
   if (v == -1 && PyErr_Occurred()) throw Refused{nullptr, ""};
@@ -216,6 +238,90 @@ int paged_attention(PyObject* const* a) {
                                  ptr(out), ptr(ws), ws->nbytes(), ptr<int32_t>(status), stream(a[11]));
 }
 
+// k_new, v_new, slot_map, pages, status, stream
+int paged_append_q4(PyObject* const* a) {
+  const char* n = "paged_append_q4";
+  const at::Tensor *k = tensor(a[0], n), *v = tensor(a[1], n), *slots = index(a[2], n), *status = index(a[4], n, true);
+  need(k->dim() == 3, "paged_append_q4: k_new [N, Hkv, D] expected");
+  const Pool4 p = pool4(a[3], k->size(2), n);
+  const int64_t N = slots->numel(), d = k->size(2);
+  need(slots->dim() == 1 && shaped(k, {N, p.hkv, d}) && shaped(v, {N, p.hkv, d}) && (status == nullptr || status->numel() >= 1),
+       "paged_append_q4: k_new, v_new [N, Hkv, D] and slot_map [N] expected");
+  if (k->scalar_type() != at::kBFloat16 || v->scalar_type() != at::kBFloat16)
+    refuse(PyExc_TypeError, "paged_append_q4: rows must be bf16");
+  on_current(n);
+  return decomoe_paged_append_q4(ptr(k), row_stride(*k, n), ptr(v), row_stride(*v, n), N, static_cast<int>(p.hkv),
+                                 static_cast<int>(d), static_cast<int>(p.group), ptr<int32_t>(slots), ptr(p.t), p.pages,
+                                 static_cast<int>(p.ps), p.stride, ptr<int32_t>(status), stream(a[5]));
+}
+
+// slot_map, pages, k_out, v_out, status, stream
+int paged_read_q4(PyObject* const* a) {
+  const char* n = "paged_read_q4";
+  const at::Tensor *slots = index(a[0], n), *k = tensor(a[2], n), *v = tensor(a[3], n), *status = index(a[4], n, true);
+  need(k->dim() == 3, "paged_read_q4: k_out [N, Hkv, D] expected");
+  const Pool4 p = pool4(a[1], k->size(2), n);
+  const int64_t N = slots->numel(), d = k->size(2);
+  need(slots->dim() == 1 && shaped(k, {N, p.hkv, d}) && shaped(v, {N, p.hkv, d}) && (status == nullptr || status->numel() >= 1),
+       "paged_read_q4: k_out, v_out [N, Hkv, D] and slot_map [N] expected");
+  if (k->scalar_type() != at::kBFloat16 || v->scalar_type() != at::kBFloat16)
+    refuse(PyExc_TypeError, "paged_read_q4: rows must be bf16");
+  on_current(n);
+  return decomoe_paged_read_q4(ptr<int32_t>(slots), N, ptr(p.t), p.pages, static_cast<int>(p.ps), p.stride,
+                               static_cast<int>(p.hkv), static_cast<int>(d), static_cast<int>(p.group), ptr(k),
+                               row_stride(*k, n), ptr(v), row_stride(*v, n), ptr<int32_t>(status), stream(a[5]));
+}
+
+// q, pages, block_table, seq_len, out, ws, hide_begin, hide_count, scale, status, stream
+int paged_attention_q4(PyObject* const* a) {
+  const char* n = "paged_attention_q4";
+  const at::Tensor *q = tensor(a[0], n), *table = index(a[2], n), *len = index(a[3], n), *out = whole(a[4], n),
+                   *ws = whole(a[5], n), *hb = index(a[6], n, true), *hc = index(a[7], n, true),
+                   *status = index(a[9], n, true);
+  need(q->dim() == 3 && out->sizes() == q->sizes(), "paged_attention_q4: q and out [B, Hq, D] expected");
+  const int64_t B = q->size(0), hq = q->size(1), d = q->size(2);
+  const Pool4 p = pool4(a[1], d, n);
+  need(shaped(len, {B}) && table->dim() == 2 && table->size(0) == B && (hb == nullptr || shaped(hb, {B})) &&
+           (hc == nullptr || shaped(hc, {B})) && (status == nullptr || status->numel() >= 1) && hq <= INT32_MAX,
+       "paged_attention_q4: block_table [B, max_pages], seq_len, hide_begin and hide_count [B] expected");
+  if (q->scalar_type() != at::kBFloat16 || out->scalar_type() != at::kBFloat16)
+    refuse(PyExc_TypeError, "paged_attention_q4: q and out must be bf16");
+  on_current(n);
+  return decomoe_paged_attention_q4(ptr(q), row_stride(*q, n), B, ptr(p.t), p.pages, static_cast<int>(p.ps), p.stride,
+                                    static_cast<int>(p.group), ptr<int32_t>(table), table->size(1), ptr<int32_t>(len),
+                                    ptr<int32_t>(hb), ptr<int32_t>(hc), static_cast<int>(hq), static_cast<int>(p.hkv),
+                                    static_cast<int>(d), to_float(a[8]), ptr(out), ptr(ws), ws->nbytes(),
+                                    ptr<int32_t>(status), stream(a[10]));
+}
+
+// logits, tokens, logprob, entropy, top_id, top_logprob, scale, status, stream
+int token_logprobs(PyObject* const* a) {
+  const char* n = "token_logprobs";
+  const at::Tensor *x = tensor(a[0], n), *tokens = index(a[1], n, true), *logprob = whole(a[2], n, true),
+                   *entropy = whole(a[3], n, true), *id = index(a[4], n, true), *top = whole(a[5], n, true),
+                   *status = index(a[7], n, true);
+  need(x->dim() == 2, "token_logprobs: logits [T, V] expected");
+  const int64_t T = x->size(0), V = x->size(1);
+  need((tokens == nullptr || shaped(tokens, {T})) && (logprob == nullptr || shaped(logprob, {T})) &&
+           (entropy == nullptr || shaped(entropy, {T})) && (status == nullptr || status->numel() >= 1),
+       "token_logprobs: tokens, logprob and entropy [T] expected");
+  const at::Tensor* best = id != nullptr ? id : top;
+  int64_t k = 0;
+  if (best != nullptr) {
+    need(best->dim() == 2 && best->size(0) == T, "token_logprobs: top_id and top_logprob [T, n] expected");
+    k = best->size(1);
+    need((id == nullptr || shaped(id, {T, k})) && (top == nullptr || shaped(top, {T, k})) && k <= INT32_MAX,
+         "token_logprobs: top_id and top_logprob must have one shape");
+  }
+  for (const at::Tensor* t : {logprob, entropy, top})
+    if (t != nullptr && t->scalar_type() != at::kFloat)
+      refuse(PyExc_TypeError, "token_logprobs: logprob, entropy and top_logprob must be float32");
+  on_current(n);
+  return decomoe_token_logprobs(ptr(x), T, V, row_stride(*x, n), dtype(*x, n), ptr<int32_t>(tokens), to_float(a[6]),
+                                static_cast<int>(k), ptr<float>(logprob), ptr<float>(entropy), k > 0 ? ptr<int32_t>(id) : nullptr,
+                                k > 0 ? ptr<float>(top) : nullptr, ptr<int32_t>(status), stream(a[8]));
+}
+
 // x, residual, weight, sum_out, y, y8, y8_scale, eps, stream
 int add_rmsnorm_q8(PyObject* const* a) {
   const char* n = "add_rmsnorm_q8";
@@ -279,8 +385,9 @@ PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t n) {
 #define DM_ENTRY(name, args) \
   {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(entry<name, args>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {DM_ENTRY(paged_plan, 13),   DM_ENTRY(paged_plan_step, 12),  DM_ENTRY(paged_advance, 7),
-                         DM_ENTRY(paged_append, 7),  DM_ENTRY(paged_attention, 12), DM_ENTRY(add_rmsnorm_q8, 9),
-                         DM_ENTRY(w4_linear, 6),     {nullptr, nullptr, 0, nullptr}};
+                         DM_ENTRY(paged_append, 7),  DM_ENTRY(paged_attention, 12), DM_ENTRY(paged_append_q4, 6),
+                         DM_ENTRY(paged_read_q4, 6), DM_ENTRY(paged_attention_q4, 11), DM_ENTRY(token_logprobs, 9),
+                         DM_ENTRY(add_rmsnorm_q8, 9), DM_ENTRY(w4_linear, 6),     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

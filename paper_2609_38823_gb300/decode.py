@@ -9,8 +9,10 @@ under its expert prefix, every step a library call.
 ``plan`` gives a step's rows their pages and slots, on the device. A request's
 visual block stays in its pages and is left out of the attention from the layer at
 which the request's exit was taken (``hide``), so the cache is not copied.
+The pages hold bf16, or 4 bits a value (``bits=4``).
 ``DecodeStep`` sequences the calls; it makes no host synchronisation, so that a
-step can be captured in a CUDA graph and replayed while the requests grow. No
+step can be captured in a CUDA graph and replayed while the requests grow.
+``DecodeHead`` turns its result into logits and log probabilities. No
 position encoding is applied: ``rotate`` is called on the queries and keys of every
 layer, with the rows' positions, where a model has one.
 """
@@ -20,10 +22,11 @@ from typing import Callable, Optional, Sequence
 
 import torch
 
-from . import (DECOMOE_BF16, decomoe_add_rmsnorm_q8, decomoe_moe_layer, decomoe_moe_layer_workspace_bytes,
-               decomoe_paged_advance, decomoe_paged_append, decomoe_paged_attention,
-               decomoe_paged_attention_workspace_bytes, decomoe_paged_plan, decomoe_paged_plan_step, decomoe_w4_linear,
-               workspace)
+from . import (DECOMOE_BF16, decomoe_add_rmsnorm_q8, decomoe_attention, decomoe_moe_layer,
+               decomoe_moe_layer_workspace_bytes, decomoe_paged_advance, decomoe_paged_append, decomoe_paged_append_q4,
+               decomoe_paged_attention, decomoe_paged_attention_q4, decomoe_paged_attention_q4_workspace_bytes,
+               decomoe_paged_attention_workspace_bytes, decomoe_paged_plan, decomoe_paged_plan_step,
+               decomoe_paged_q4_page_bytes, decomoe_paged_read_q4, decomoe_token_logprobs, decomoe_w4_linear, workspace)
 
 
 def quantize_w4(w: torch.Tensor, group: int = 128):
@@ -40,18 +43,29 @@ def quantize_w4(w: torch.Tensor, group: int = 128):
 
 class PagedCache:
     """Keys and values of `layers` layers for up to `requests` requests in
-    `pages` pages of `page_size` rows, bf16. `max_pages` bounds a request.
+    `pages` pages of `page_size` rows, bf16, or with `bits` 4 in codes with a step and a
+    low for every `group` features. `max_pages` bounds a request.
 
     `active` [requests] says which slots a decode step adds a row to (1) and which it
     leaves alone (0: no request, or one that waits). All do at the start; a released slot
     does not until rows are planned for it again."""
 
     def __init__(self, layers: int, requests: int, pages: int, page_size: int, max_pages: int, hkv: int, d: int,
-                 device="cuda"):
+                 device="cuda", bits: int = 16, group: int = 64):
         i32 = dict(dtype=torch.int32, device=device)
-        # keys and values of a page side by side: the two pools are slices of one buffer
-        self.pool = torch.zeros(layers, pages, 2, page_size, hkv, d, dtype=torch.bfloat16, device=device)
-        self.page_size = page_size
+        if bits == 16:
+            # keys and values of a page side by side: the two pools are slices of one buffer
+            self.pool = torch.zeros(layers, pages, 2, page_size, hkv, d, dtype=torch.bfloat16, device=device)
+        elif bits == 4:
+            size = decomoe_paged_q4_page_bytes(page_size, hkv, d, group)
+            if size == 0:
+                raise ValueError("a cache in 4 bits has heads of 64 or 128, groups of 32, 64 or (heads of 128) 128, and "
+                                 "pages of a power of two of rows, 8 at least")
+            self.pool = torch.zeros(layers, pages, hkv, page_size // 8, size // (hkv * (page_size // 8)), dtype=torch.uint8,
+                                    device=device)
+        else:
+            raise ValueError("a cache holds 16 or 4 bits a value")
+        self.page_size, self.hkv, self.d, self.bits = page_size, hkv, d, bits
         self.table = torch.full((requests, max_pages), -1, **i32)
         self.free = torch.arange(pages, **i32)       # given out from free[head] on
         self.head, self.head_next = torch.zeros(1, **i32), torch.zeros(1, **i32)
@@ -67,6 +81,41 @@ class PagedCache:
 
     def v(self, layer: int) -> torch.Tensor:
         return self.pool[layer, :, 1]
+
+    def append(self, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor) -> None:
+        """New rows [N, Hkv, D] of a layer into their slots."""
+        if self.bits == 4:
+            decomoe_paged_append_q4(k_new, v_new, slots, self.pool[layer], status=self.status)
+        else:
+            decomoe_paged_append(k_new, v_new, slots, self.k(layer), self.v(layer), status=self.status)
+
+    def workspace_bytes(self, B: int, hq: int) -> int:
+        f = decomoe_paged_attention_q4_workspace_bytes if self.bits == 4 else decomoe_paged_attention_workspace_bytes
+        return f(B, hq, self.hkv, self.d)
+
+    def attend(self, layer: int, q: torch.Tensor, out: torch.Tensor, ws: torch.Tensor) -> None:
+        """One new token per request, q and out [B, Hq, D], over its rows of a layer."""
+        if self.bits == 4:
+            decomoe_paged_attention_q4(q, self.pool[layer], self.table, self.seq_len, out, ws, hide_begin=self.hide_begin,
+                                       hide_count=self.hide_count[layer], status=self.status)
+        else:
+            decomoe_paged_attention(q, self.k(layer), self.v(layer), self.table, self.seq_len, out, ws,
+                                    hide_begin=self.hide_begin, hide_count=self.hide_count[layer], status=self.status)
+
+    def slots_of(self, request: int, rows: int) -> torch.Tensor:
+        """Slots of a request's first `rows` rows, in order."""
+        j = torch.arange(rows, dtype=torch.int32, device=self.table.device)
+        return self.table[request, j // self.page_size] * self.page_size + j % self.page_size
+
+    def attend_chunk(self, layer: int, q: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                     out: torch.Tensor, ws: torch.Tensor) -> None:
+        """A prompt's next chunk on a cache in 4 bits: q and out [n, Hq, D] of the last n of the
+        rows in `slots` [C] (stored already), which are read into k and v [C, Hkv, D] bf16 and
+        attended causally; ws as decomoe_attention has it."""
+        if self.bits != 4:
+            raise ValueError("a chunk over the pages is for a cache in 4 bits")
+        decomoe_paged_read_q4(slots, self.pool[layer], k, v, status=self.status)
+        decomoe_attention(q, k, v, out, ws, status=self.status)
 
     def plan(self, fresh: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:
         """Pages, slots [N] and positions [N] of the rows that this step adds
@@ -139,7 +188,7 @@ class DecodeStep:
                  rotate: Optional[Callable[[torch.Tensor, torch.Tensor, torch.Tensor], None]] = None):
         self.layers, self.cache, self.B, self.hq, self.topk, self.eps = list(layers), cache, B, hq, k, eps
         self.rotate = rotate
-        hkv, D = cache.pool.shape[4:]
+        hkv, D = cache.hkv, cache.d
         E, d = layers[0].w_r.shape
         m = layers[0].w_down.shape[2]
         dev = cache.pool.device
@@ -153,7 +202,7 @@ class DecodeStep:
         self.heads = torch.empty(B, hq, D, **bf)
         self.proj, self.h1, self.xn = (torch.empty(B, d, **bf) for _ in range(3))
         self.h = [torch.empty(B, d, **bf) for _ in range(2)]
-        self.attn_ws = workspace(decomoe_paged_attention_workspace_bytes(B, hq, hkv, D), dev)
+        self.attn_ws = workspace(cache.workspace_bytes(B, hq), dev)
         self.moe_ws = workspace(decomoe_moe_layer_workspace_bytes(B, d, E, k, m, DECOMOE_BF16), dev)
 
     def __call__(self, h0: torch.Tensor, trace=None) -> torch.Tensor:
@@ -169,9 +218,8 @@ class DecodeStep:
             decomoe_w4_linear(self.x8, *w.w_qkv, self.qkv.view(self.B, -1), x_scale=self.x8_scale)
             if self.rotate is not None:
                 self.rotate(self.q, self.k_new, self.positions)
-            decomoe_paged_append(self.k_new, self.v_new, self.slots, c.k(l), c.v(l), status=c.status)
-            decomoe_paged_attention(self.q, c.k(l), c.v(l), c.table, c.seq_len, self.heads, self.attn_ws,
-                                    hide_begin=c.hide_begin, hide_count=c.hide_count[l], status=c.status)
+            c.append(l, self.k_new, self.v_new, self.slots)
+            c.attend(l, self.q, self.heads, self.attn_ws)
             decomoe_w4_linear(self.heads.view(self.B, -1), *w.w_out, self.proj)
             decomoe_add_rmsnorm_q8(self.proj, h, w.norm_moe, self.h1, self.xn, eps=self.eps)
             decomoe_moe_layer(self.xn, w.w_r, w.bias, w.w_gate_up, w.w_down, self.topk, out, self.moe_ws, K_fixed=w.K,
@@ -180,3 +228,32 @@ class DecodeStep:
                 trace(l, self, h, out)
             h = out
         return h
+
+
+class DecodeHead:
+    """The end of a step: norm, vocabulary projection [V, d] in 4 bits as a (bytes, scales)
+    pair, and what a server returns beside the tokens. Each call overwrites `logits` [B, V],
+    `logprob` and `entropy` [B] and, for n > 0, `top_id` and `top_logprob` [B, n]."""
+
+    def __init__(self, norm, w_vocab, B: int, n: int = 0, eps: float = 1e-6, dtype=torch.float32):
+        w, scale = w_vocab
+        V, d, dev = w.shape[0], 2 * w.shape[1], w.device
+        f32 = dict(dtype=torch.float32, device=dev)
+        self.norm, self.w_vocab, self.eps = norm, (w, scale), eps
+        self.x8, self.x8_scale = torch.empty(B, d, dtype=torch.float8_e4m3fn, device=dev), torch.empty(B, **f32)
+        self.logits = torch.empty(B, V, dtype=dtype, device=dev)
+        self.logprob, self.entropy = torch.zeros(B, **f32), torch.zeros(B, **f32)
+        self.top_id = torch.zeros(B, n, dtype=torch.int32, device=dev) if n else None
+        self.top_logprob = torch.zeros(B, n, **f32) if n else None
+
+    def __call__(self, h: torch.Tensor) -> torch.Tensor:
+        """The logits of hidden states [B, d]."""
+        decomoe_add_rmsnorm_q8(h, None, self.norm, y8=self.x8, y8_scale=self.x8_scale, eps=self.eps)
+        decomoe_w4_linear(self.x8, *self.w_vocab, self.logits, x_scale=self.x8_scale)
+        return self.logits
+
+    def score(self, tokens: Optional[torch.Tensor] = None, temperature: float = 1.0) -> None:
+        """Log probabilities of tokens [B] int32 (negative: a slot without one, left as it
+        was), or without tokens each row's entropy and alternatives alone."""
+        decomoe_token_logprobs(self.logits, tokens, None if tokens is None else self.logprob, self.entropy, self.top_id,
+                               self.top_logprob, scale=1.0 / temperature)
