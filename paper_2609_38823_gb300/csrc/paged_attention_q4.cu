@@ -6,25 +6,25 @@
 
 namespace decomoe {
 
-constexpr int Q4A_STAGES = 4;
+constexpr int Q4A_KEYS = 32;     // rows of a tile
+constexpr int Q4A_SETS = Q4A_KEYS / 8;
 constexpr int Q4A_BLOCKS = 320;  // of a launch, at most
 constexpr int Q4A_EXTRA = 3;     // what a (request, KV head) pair costs beside its tiles, in tiles
+constexpr int q4a_stages(int D) { return D == 128 ? 3 : 4; }
 
 // A tile: KEYS consecutive rows of a request from a multiple of KEYS on (so that eight rows
 // always lie together in a page), those that are hidden or past the length left out of
 // the sums. Tiles of hidden rows alone are not numbered.
-template <int D, int G>
-struct Q4aTile {
-  using L = Q4Tile<D, G>;
-  static constexpr int KEYS = 2048 / D;  // 16 or 32
-  static constexpr int SETS = KEYS / 8;  // pieces of eight rows
-  static constexpr int STAGE = SETS * L::BYTES;
-  static constexpr int ROW = pga_row(D);
-  static __device__ __forceinline__ int before(const PgaReq& r) { return (r.h0 + KEYS - 1) / KEYS; }  // the hidden block
-  static __device__ __forceinline__ int after(const PgaReq& r) { return max(before(r), (r.h0 + r.hc) / KEYS); }
+struct Q4aTiles {
+  static __device__ __forceinline__ int before(const PgaReq& r) {  // the hidden block
+    return static_cast<int>(static_cast<unsigned>(r.h0 + Q4A_KEYS - 1) / Q4A_KEYS);
+  }
+  static __device__ __forceinline__ int after(const PgaReq& r) {
+    return max(before(r), static_cast<int>(static_cast<unsigned>(r.h0 + r.hc) / Q4A_KEYS));
+  }
   static __device__ __forceinline__ int count(const PgaReq& r) {
     const int n = r.seen + r.hc;
-    return before(r) + (r.h0 + r.hc < n ? (n + KEYS - 1) / KEYS - after(r) : 0);
+    return before(r) + (r.h0 + r.hc < n ? static_cast<int>(static_cast<unsigned>(n + Q4A_KEYS - 1) / Q4A_KEYS) - after(r) : 0);
   }
 };
 
@@ -53,42 +53,84 @@ __device__ __forceinline__ void q4a_lds(uint32_t addr, uint32_t (&v)[N]) {
   else
     v[0] = q4a_lds(addr);
 }
-// The codes at bits 4 s of the two halves of w, as bf16 numbers q - 8: 128 + q is exact
-// in bf16, and so is its difference from 136.
-__device__ __forceinline__ uint32_t q4a_codes(uint32_t w, int s) {
-  const uint32_t u = ((w >> (4 * s)) & 0x000f000fu) | 0x43004300u;
-  const __nv_bfloat162 c = __halves2bfloat162(__ushort_as_bfloat16(0x4308), __ushort_as_bfloat16(0x4308));
-  const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162*>(&u), c);
-  return *reinterpret_cast<const uint32_t*>(&r);
+// The four codes of each half of w as bf16 pairs of (code - 8) / 64, exact: masked in
+// place a code is a subnormal number, code 2^-133 or (four bits up) code 2^-129, which one multiply-add
+// brings there.
+__device__ __forceinline__ uint32_t q4a_fma(uint32_t u, uint32_t by) {
+  uint32_t r;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(u), "r"(by), "r"(0xbe00be00u));  // - 1/8
+  return r;
 }
+__device__ __forceinline__ void q4a_codes(uint32_t w, uint32_t (&f)[4]) {
+  const uint32_t v = w >> 8;
+  f[0] = q4a_fma(w & 0x000f000fu, 0x7f007f00u);  // 2^127
+  f[1] = q4a_fma(w & 0x00f000f0u, 0x7d007d00u);  // 2^123
+  f[2] = q4a_fma(v & 0x000f000fu, 0x7f007f00u);
+  f[3] = q4a_fma(v & 0x00f000f0u, 0x7d007d00u);
+}
+
+// Where the copies of a warp stand in the numbered tiles: a tile of a pair, and the pair's
+// rows, table and place in a page.
+struct Q4aLook {
+  int b, h, t, tiles, before, skip, n, h0, he;
+  const int32_t* table;
+  const uint8_t* head;
+  __device__ __forceinline__ void pair(const PagedQ4Args& a, int tile_bytes) {
+    head = a.pages + (static_cast<int64_t>(a.qt == 1 ? h : h / a.qt) << a.shift >> 3) * tile_bytes;
+  }
+  __device__ __forceinline__ void enter(const PagedQ4Args& a, int tile_bytes) {
+    bool bad = false;  // marked by the launch's first look at the lengths
+    const PgaReq r = pga_request(a, b, &bad);
+    tiles = Q4aTiles::count(r);
+    before = Q4aTiles::before(r);
+    skip = Q4aTiles::after(r) - before;
+    n = r.seen + r.hc;
+    h0 = r.h0;
+    he = r.h0 + r.hc;
+    table = a.table + b * a.max_pages;
+    pair(a, tile_bytes);
+  }
+  // To the next tile; in the last pair it stays past the end (nobody looks).
+  __device__ __forceinline__ void next(const PagedQ4Args& a, const int* pre, int tile_bytes) {
+    if (++t < tiles) return;
+    t = 0;
+    if (++h < a.hv) return pair(a, tile_bytes);
+    h = 0;
+    do ++b;
+    while (b < a.B && pre[b + 1] == pre[b]);
+    if (b < a.B) enter(a, tile_bytes);
+  }
+};
 
 template <int D, int G, int NT>
 __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attention_q4(PagedQ4Args a) {
-  using T = Q4aTile<D, G>;
   using L = Q4Tile<D, G>;
+  constexpr int STAGES = q4a_stages(D);
+  constexpr int STAGE = Q4A_SETS * L::BYTES;
+  constexpr int SUB = Q4A_KEYS / 16;
   constexpr int BLK = D / 32;      // blocks of 32 features
   constexpr int BG = BLK / G;      // of a group
-  constexpr int ROWS = 8 * NT;
-  constexpr int RING = Q4A_STAGES * T::STAGE;
-  static_assert(ROWS * T::ROW * 4 <= RING, "a piece fits the ring");
+  constexpr int ROWS = 8 * NT, ROW = pga_row(D);
+  constexpr int RING = STAGES * STAGE;
+  static_assert(ROWS * ROW * 4 <= RING, "a piece fits the ring");
   extern __shared__ __align__(1024) uint8_t q4a_smem[];
-  __shared__ __align__(8) uint64_t bars[PGA_WARPS][Q4A_STAGES];
-  __shared__ uint32_t seen_mask[PGA_WARPS][Q4A_STAGES];
+  __shared__ __align__(8) uint64_t bars[PGA_WARPS][STAGES];
+  __shared__ int4 tile_info[PGA_WARPS][STAGES];  // rows seen, request, head tile, whether the pair ends
   __shared__ int3 meta[PGA_WARPS];
   __shared__ int abort_flag;
   int* pre = reinterpret_cast<int*>(q4a_smem + PGA_WARPS * RING);
   int* nz = pre + a.B + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) abort_flag = 0;
-  if (lane < Q4A_STAGES) mbar_init(smem_u32(&bars[warp][lane]), 1);
+  if (lane < STAGES) mbar_init(smem_u32(&bars[warp][lane]), 1);
   fence_mbar_init();
   pdl_enter();
-  const PgaPlan plan = pga_begin<T, D>(a, pre, nz);
+  const PgaPlan plan = pga_begin<Q4aTiles, D>(a, pre, nz);
   const int me = blockIdx.x * PGA_WARPS + warp;
   // lane 0 seeks the start of this warp's share, lane 1 that of the next one's
-  PgaWalk<T> look;
+  PgaWalk<Q4aTiles> seek;
   const int from = plan.place(me + (lane & 1));
-  const int first = from < plan.total ? look.seek(plan, from) : pre[a.B] * a.hv;
+  const int first = from < plan.total ? seek.seek(plan, from) : pre[a.B] * a.hv;
   const int r0 = __shfl_sync(0xffffffffu, first, 0), r1 = __shfl_sync(0xffffffffu, first, 1);
   const int gs = a.hq / a.hkv;
 
@@ -96,43 +138,44 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
   const uint32_t ring_s = smem_u32(ring), bar_s = smem_u32(&bars[warp][0]);
   float* mine = reinterpret_cast<float*>(ring);  // the last piece, once the ring is drained
   if (lane == 0) meta[warp] = make_int3(0, 0, 0);
-  float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * ROWS * T::ROW;
+  float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * ROWS * ROW;
 
   if (r0 < r1) {
-    // ---- lookup, copy and use, each at its own tile
-    look.b = __shfl_sync(0xffffffffu, look.b, 0);
-    look.h = __shfl_sync(0xffffffffu, look.h, 0);
-    look.t = __shfl_sync(0xffffffffu, look.t, 0);
-    look.enter(a);
-    PgaWalk<T> use = look;
+    // ---- lookup and copy of tiles, ahead of their use
+    Q4aLook look;
+    look.b = __shfl_sync(0xffffffffu, seek.b, 0);
+    look.h = __shfl_sync(0xffffffffu, seek.h, 0);
+    look.t = __shfl_sync(0xffffffffu, seek.t, 0);
+    look.enter(a, L::BYTES);
+    bool began = look.t > 0;  // the piece's pair began in an earlier share
     const int in_page = (1 << a.shift) - 1;
-    int page = -1;
+    int page = -1, off = 0;
     uint32_t want = 0;  // the tile's rows that the request sees
-    const uint8_t* src = nullptr;
     auto lookup = [&]() {  // the page of this lane's eight rows
-      const int at = (look.t < T::before(look.r) ? look.t : look.t - T::before(look.r) + T::after(look.r)) * T::KEYS;
-      const int j = at + lane, n = look.r.seen + look.r.hc;
-      want = __ballot_sync(0xffffffffu, lane < T::KEYS && j < n && (j < look.r.h0 || j >= look.r.h0 + look.r.hc));
+      const int at = (look.t < look.before ? look.t : look.t + look.skip) * Q4A_KEYS;
+      const int j = at + lane;
+      want = __ballot_sync(0xffffffffu, j < look.n && (j < look.h0 || j >= look.he));
       const int p = at + lane * 8;
       page = -1;
-      if (lane < T::SETS && ((want >> (lane * 8)) & 0xffu)) page = a.table[look.b * a.max_pages + (p >> a.shift)];
-      src = a.pages + ((static_cast<int64_t>(look.h / a.qt) << a.shift >> 3) + ((p & in_page) >> 3)) * L::BYTES;
+      off = ((p & in_page) >> 3) * L::BYTES;
+      if (lane < Q4A_SETS && ((want >> (lane * 8)) & 0xffu)) page = look.table[p >> a.shift];
     };
     auto issue = [&](int slot) {
-      const bool some = lane < T::SETS && ((want >> (lane * 8)) & 0xffu);
+      const bool some = lane < Q4A_SETS && ((want >> (lane * 8)) & 0xffu);
       const bool there = some && page >= 0 && page < a.num_pages;
       if (some && !there) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
       const uint32_t sets = __ballot_sync(0xffffffffu, there), bar = bar_s + slot * 8;
       if (lane == 0) {
         uint32_t mask = want;
+        if (sets != (1u << Q4A_SETS) - 1)
 #pragma unroll
-        for (int i = 0; i < T::SETS; ++i)
-          if (!((sets >> i) & 1u)) mask &= ~(0xffu << (8 * i));
-        seen_mask[warp][slot] = mask;
+          for (int i = 0; i < Q4A_SETS; ++i)
+            if (!((sets >> i) & 1u)) mask &= ~(0xffu << (8 * i));
+        tile_info[warp][slot] = make_int4(static_cast<int>(mask), look.b, look.h, look.t + 1 == look.tiles);
         mbar_arrive_expect_tx(bar, __popc(sets) * L::BYTES);
       }
       __syncwarp();
-      if (there) q4a_bulk(ring_s + slot * T::STAGE + lane * L::BYTES, src + page * a.page_stride, L::BYTES, bar);
+      if (there) q4a_bulk(ring_s + slot * STAGE + lane * L::BYTES, look.head + page * a.page_stride + off, L::BYTES, bar);
     };
     const int n = r1 - r0;
     lookup();
@@ -141,10 +184,11 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
     // c + 4 of eight values, features 32 i + 4 r .. + 3
     const int r = lane >> 2, c = lane & 3, kr = (r >> 1) + 4 * (r & 1);
     uint32_t qf[NT][BLK][4], qs[NT][G == 4 ? 3 : 2];
-    float o[2 * BLK][NT][4], off[NT][2][G], m[NT][2], l[NT][2];
+    float o[2 * BLK][NT][4], low[NT][2][G], m[NT][2], l[NT][2];
+    int b = look.b, h = look.h;  // of the piece
     auto begin_piece = [&]() {
-      const int g = use.h / a.qt, q0 = (use.h - g * a.qt) * ROWS;
-      const __nv_bfloat16* q = a.q + use.b * a.q_stride + static_cast<int64_t>(g) * gs * D;
+      const int g = a.qt == 1 ? h : h / a.qt, q0 = (h - g * a.qt) * ROWS;
+      const __nv_bfloat16* q = a.q + b * a.q_stride + static_cast<int64_t>(g) * gs * D;
 #pragma unroll
       for (int x = 0; x < NT; ++x) {
         const int row = q0 + x * 8 + r;
@@ -162,13 +206,14 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
           qf[x][i][2] = __byte_perm(u.y, u.w, 0x5410);
           qf[x][i][3] = __byte_perm(u.y, u.w, 0x7632);
         }
-        // a group's sum as three bf16 numbers (24 bits), each with its eightfold in front
+        // a 64th of a group's sum (as the codes are 64ths) in three bf16 numbers, 24 bits, each
+        // with its eightfold in front
         uint32_t piece[G][3];
 #pragma unroll
         for (int i = 0; i < G; ++i) {
           sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
           sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
-          float rest = sum[i];
+          float rest = sum[i] * 0.015625f;
 #pragma unroll
           for (int k = 0; k < 3; ++k) {
             const float f = __bfloat162float(__float2bfloat16_rn(rest));
@@ -192,7 +237,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
           m[x][i] = -INFINITY;
           l[x][i] = 0.f;
 #pragma unroll
-          for (int g2 = 0; g2 < G; ++g2) off[x][i][g2] = 0.f;
+          for (int g2 = 0; g2 < G; ++g2) low[x][i][g2] = 0.f;
         }
 #pragma unroll
         for (int s = 0; s < 2 * BLK; ++s)
@@ -200,7 +245,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
           for (int i = 0; i < 4; ++i) o[s][x][i] = 0.f;
       }
     };
-    // a finished piece: its sums over the lanes, the offsets added to the outputs
+    // a finished piece: its sums over the lanes, the lows added to the outputs
     auto end_piece = [&]() {
 #pragma unroll
       for (int x = 0; x < NT; ++x)
@@ -211,11 +256,11 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
 #pragma unroll
           for (int g = 0; g < G; ++g) {
 #pragma unroll
-            for (int w = 4; w < 32; w <<= 1) off[x][i][g] += __shfl_xor_sync(0xffffffffu, off[x][i][g], w);
+            for (int w = 4; w < 32; w <<= 1) low[x][i][g] += __shfl_xor_sync(0xffffffffu, low[x][i][g], w);
 #pragma unroll
             for (int s = 2 * BG * g; s < 2 * BG * (g + 1); ++s) {
-              o[s][x][i] += off[x][i][g];
-              o[s][x][i + 2] += off[x][i][g];
+              o[s][x][i] = fmaf(o[s][x][i], 64.f, low[x][i][g]);
+              o[s][x][i + 2] = fmaf(o[s][x][i + 2], 64.f, low[x][i][g]);
             }
           }
         }
@@ -225,7 +270,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
       for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float* row = dst + (x * 8 + 2 * c + i) * T::ROW;
+          float* row = dst + (x * 8 + 2 * c + i) * ROW;
 #pragma unroll
           for (int s = 0; s < BLK; ++s)
             *reinterpret_cast<float4*>(row + 32 * s + 4 * r) =
@@ -236,16 +281,16 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
           }
         }
     };
-    bool began = use.t > 0;  // the piece's pair began in an earlier share
     int slot = 0, fill = 0;
     uint32_t parity = 0;
+    const float sl2 = 64.f * a.sl2;  // of scores in 64ths
     // the first steps only fill the ring (one copy of the code: a short share runs it cold)
-    for (int i = 1 - Q4A_STAGES; i < n; ++i) {
-      if (i + Q4A_STAGES - 1 < n) {
+    for (int i = 1 - STAGES; i < n; ++i) {
+      if (i + STAGES - 1 < n) {
         issue(fill);
-        fill = fill + 1 == Q4A_STAGES ? 0 : fill + 1;
-        if (i + Q4A_STAGES < n) {
-          look.next(a, pre);
+        fill = fill + 1 == STAGES ? 0 : fill + 1;
+        if (i + STAGES < n) {
+          look.next(a, pre, L::BYTES);
           lookup();
         }
       }
@@ -256,146 +301,177 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
       if (!__all_sync(0xffffffffu, mbar_wait(bar_s + slot * 8, parity, a.limit_ns, &abort_flag))) {
         if (lane == 0) report_status(a.status, DECOMOE_ERR_TIMEOUT);
         // no results; what is in flight gets the same time to land
-        for (int k = 1; k < Q4A_STAGES && i + k < n; ++k) {
-          slot = slot + 1 == Q4A_STAGES ? (parity ^= 1, 0) : slot + 1;
+        for (int k = 1; k < STAGES && i + k < n; ++k) {
+          slot = slot + 1 == STAGES ? (parity ^= 1, 0) : slot + 1;
           mbar_wait(bar_s + slot * 8, parity, a.limit_ns, &abort_flag);
         }
         break;
       }
-      const uint32_t stage = ring_s + slot * T::STAGE;
-      const uint32_t mask = seen_mask[warp][slot];
+      const uint32_t stage = ring_s + slot * STAGE;
+      const int4 info = tile_info[warp][slot];
+      if (info.y != b || info.z != h) {  // a new pair
+        b = info.y;
+        h = info.z;
+        began = false;
+        begin_piece();
+      }
+      const uint32_t mask = static_cast<uint32_t>(info.x);
+      // ---- scores: sum over the groups of step (q (code - 8)) + (low + 8 step) (sum of q)
+      float sc[SUB][NT][4];
 #pragma unroll
-      for (int u = 0; u < T::SETS / 2; ++u) {
+      for (int u = 0; u < SUB; ++u) {
         const uint32_t at[2] = {stage + 2 * u * L::BYTES, stage + (2 * u + 1) * L::BYTES};
-        // ---- scores: sum over the groups of step (q (code - 8)) + (low + 8 step) (sum of q)
-        uint32_t kp[2][G];
-        float sc[NT][4] = {};
-        {
-          uint32_t kw[2][BLK], kx[4];
+        uint32_t kw[2][BLK], kx[4], kp[2][G];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            q4a_lds(at[h] + L::K + kr * L::CODES + c * (L::CODES / 4), kw[h]);
-            q4a_lds(at[h] + L::KP + kr * L::PARAMS, kp[h]);
-            kx[h] = kx[h + 2] = q4a_lds(at[h] + L::KP + kr * L::PARAMS + (c % G) * 4);
+        for (int hf = 0; hf < 2; ++hf) {
+          q4a_lds(at[hf] + L::K + kr * L::CODES + c * (L::CODES / 4), kw[hf]);
+          q4a_lds(at[hf] + L::KP + kr * L::PARAMS, kp[hf]);
+          kx[hf] = kx[hf + 2] = q4a_lds(at[hf] + L::KP + kr * L::PARAMS + (c % G) * 4);
+        }
+#pragma unroll
+        for (int x = 0; x < NT; ++x) {
+#pragma unroll
+          for (int i2 = 0; i2 < 4; ++i2) sc[u][x][i2] = 0.f;
+          pga_mma(sc[u][x], kx, qs[x][0], qs[x][1]);
+          if constexpr (G == 4) pga_mma(sc[u][x], kx, qs[x][2], 0u);
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          float acc[NT][4] = {};
+#pragma unroll
+          for (int i2 = g * BG; i2 < (g + 1) * BG; ++i2) {
+            uint32_t f0[4], f1[4];
+            q4a_codes(kw[0][i2], f0);
+            q4a_codes(kw[1][i2], f1);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              const uint32_t f[4] = {f0[2 * s], f1[2 * s], f0[2 * s + 1], f1[2 * s + 1]};
+#pragma unroll
+              for (int x = 0; x < NT; ++x) pga_mma(acc[x], f, qf[x][i2][2 * s], qf[x][i2][2 * s + 1]);
+            }
           }
 #pragma unroll
-          for (int x = 0; x < NT; ++x) {
-            pga_mma(sc[x], kx, qs[x][0], qs[x][1]);
-            if constexpr (G == 4) pga_mma(sc[x], kx, qs[x][2], 0u);
-          }
+          for (int x = 0; x < NT; ++x)
 #pragma unroll
-          for (int g = 0; g < G; ++g) {
-            float acc[NT][4] = {};
+            for (int i2 = 0; i2 < 4; ++i2) sc[u][x][i2] = fmaf(bf16_lo(kp[i2 >> 1][g]), acc[x][i2], sc[u][x][i2]);
+        }
+      }
+      if (mask != 0xffffffffu) {
 #pragma unroll
-            for (int i2 = g * BG; i2 < (g + 1) * BG; ++i2)
+        for (int u = 0; u < SUB; ++u)
 #pragma unroll
-              for (int s = 0; s < 2; ++s) {
-                const uint32_t f[4] = {q4a_codes(kw[0][i2], 2 * s), q4a_codes(kw[1][i2], 2 * s),
-                                       q4a_codes(kw[0][i2], 2 * s + 1), q4a_codes(kw[1][i2], 2 * s + 1)};
+          for (int hf = 0; hf < 2; ++hf)
+            if (!((mask >> (16 * u + 8 * hf + kr)) & 1u)) {
+              // anything may lie where nothing is seen
 #pragma unroll
-                for (int x = 0; x < NT; ++x) pga_mma(acc[x], f, qf[x][i2][2 * s], qf[x][i2][2 * s + 1]);
-              }
+              for (int x = 0; x < NT; ++x) sc[u][x][2 * hf] = sc[u][x][2 * hf + 1] = -INFINITY;
+            }
+      }
+      // ---- the maxima so far, raised only where one is passed by 2^8: weights up to 2^8 cost no
+      // digits, and rescaling the outputs is rare
 #pragma unroll
-            for (int x = 0; x < NT; ++x)
+      for (int x = 0; x < NT; ++x) {
+        float mx[2];
 #pragma unroll
-              for (int i2 = 0; i2 < 4; ++i2) sc[x][i2] = fmaf(bf16_lo(kp[i2 >> 1][g]), acc[x][i2], sc[x][i2]);
+        for (int i2 = 0; i2 < 2; ++i2) {
+          mx[i2] = fmaxf(sc[0][x][i2], sc[0][x][i2 + 2]);
+#pragma unroll
+          for (int u = 1; u < SUB; ++u) mx[i2] = fmaxf(mx[i2], fmaxf(sc[u][x][i2], sc[u][x][i2 + 2]));
+        }
+#pragma unroll
+        for (int w = 4; w < 32; w <<= 1) {
+          mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], w));
+          mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], w));
+        }
+        mx[0] *= sl2;
+        mx[1] *= sl2;
+        if (__any_sync(0xffffffffu, mx[0] > m[x][0] + 8.f || mx[1] > m[x][1] + 8.f)) {
+#pragma unroll
+          for (int i2 = 0; i2 < 2; ++i2) {
+            const float to = fmaxf(m[x][i2], mx[i2]);
+            // nothing seen so far, and nothing here: any factor does
+            const float f = to == -INFINITY ? 1.f : pga_ex2(m[x][i2] - to);
+            m[x][i2] = to;
+            l[x][i2] *= f;
+#pragma unroll
+            for (int g = 0; g < G; ++g) low[x][i2][g] *= f;
+#pragma unroll
+            for (int s = 0; s < 2 * BLK; ++s) {
+              o[s][x][i2] *= f;
+              o[s][x][i2 + 2] *= f;
+            }
           }
         }
-        // ---- weights
-        const uint32_t sees = mask >> (16 * u);
-        const bool lo = (sees >> kr) & 1u, hi = (sees >> (8 + kr)) & 1u;
+      }
+      // ---- weights and values
+      float ref[NT][2];
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
+#pragma unroll
+        for (int i2 = 0; i2 < 2; ++i2) ref[x][i2] = m[x][i2] == -INFINITY ? 0.f : m[x][i2];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u) {
+        const uint32_t at[2] = {stage + 2 * u * L::BYTES, stage + (2 * u + 1) * L::BYTES};
         uint32_t vp[2][G];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          q4a_lds(at[h] + L::VP + kr * L::PARAMS, vp[h]);
+        for (int hf = 0; hf < 2; ++hf) q4a_lds(at[hf] + L::VP + kr * L::PARAMS, vp[hf]);
+        if (mask != 0xffffffffu) {
 #pragma unroll
-          for (int g = 0; g < G; ++g) vp[h][g] = (h ? hi : lo) ? vp[h][g] : 0u;  // anything may lie there
+          for (int hf = 0; hf < 2; ++hf)
+            if (!((mask >> (16 * u + 8 * hf + kr)) & 1u))
+#pragma unroll
+              for (int g = 0; g < G; ++g) vp[hf][g] = 0u;
         }
         uint32_t p[NT][G][2];
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
-          float mx[2];
-#pragma unroll
-          for (int i2 = 0; i2 < 2; ++i2) {
-            sc[x][i2] = lo ? sc[x][i2] * a.sl2 : -INFINITY;
-            sc[x][i2 + 2] = hi ? sc[x][i2 + 2] * a.sl2 : -INFINITY;
-            mx[i2] = fmaxf(sc[x][i2], sc[x][i2 + 2]);
-          }
-#pragma unroll
-          for (int w = 4; w < 32; w <<= 1) {
-            mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], w));
-            mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], w));
-          }
-          if (__any_sync(0xffffffffu, mx[0] > m[x][0] || mx[1] > m[x][1])) {
-#pragma unroll
-            for (int i2 = 0; i2 < 2; ++i2) {
-              const float to = fmaxf(m[x][i2], mx[i2]);
-              // nothing seen so far, and nothing here: any factor does
-              const float f = to == -INFINITY ? 1.f : pga_ex2(m[x][i2] - to);
-              m[x][i2] = to;
-              l[x][i2] *= f;
-#pragma unroll
-              for (int g = 0; g < G; ++g) off[x][i2][g] *= f;
-#pragma unroll
-              for (int s = 0; s < 2 * BLK; ++s) {
-                o[s][x][i2] *= f;
-                o[s][x][i2 + 2] *= f;
-              }
-            }
-          }
           float w[4];
 #pragma unroll
-          for (int i2 = 0; i2 < 4; ++i2) {
-            const float ref = m[x][i2 & 1] == -INFINITY ? 0.f : m[x][i2 & 1];
-            w[i2] = pga_ex2(sc[x][i2] - ref);
-          }
+          for (int i2 = 0; i2 < 4; ++i2) w[i2] = pga_ex2(fmaf(sc[u][x][i2], sl2, -ref[x][i2 & 1]));
           l[x][0] += w[0] + w[2];
           l[x][1] += w[1] + w[3];
           // weights times steps are the operands of the value product; lows and 8 steps add up in fp32
 #pragma unroll
           for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-              const float step = bf16_lo(vp[h][g]), at8 = fmaf(8.f, step, bf16_hi(vp[h][g]));
-              off[x][0][g] = fmaf(w[2 * h], at8, off[x][0][g]);
-              off[x][1][g] = fmaf(w[2 * h + 1], at8, off[x][1][g]);
-              p[x][g][h] = pga_transpose(pack_bf16x2(w[2 * h] * step, w[2 * h + 1] * step));
+            for (int hf = 0; hf < 2; ++hf) {
+              const float step = bf16_lo(vp[hf][g]), at8 = fmaf(8.f, step, bf16_hi(vp[hf][g]));
+              low[x][0][g] = fmaf(w[2 * hf], at8, low[x][0][g]);
+              low[x][1][g] = fmaf(w[2 * hf + 1], at8, low[x][1][g]);
+              p[x][g][hf] = pga_transpose(pack_bf16x2(w[2 * hf] * step, w[2 * hf + 1] * step));
             }
         }
-        // ---- values
         uint32_t vw[2][2][BLK / 2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
           for (int k = 0; k < 2; ++k)
-            q4a_lds(at[h] + L::V + (c + 4 * k) * L::CODES + r * (L::CODES / 8), vw[h][k]);
+            q4a_lds(at[hf] + L::V + (c + 4 * k) * L::CODES + r * (L::CODES / 8), vw[hf][k]);
 #pragma unroll
         for (int i2 = 0; i2 < BLK; ++i2) {
-          uint32_t t[2];  // of the two keys of each half
-#pragma unroll
-          for (int h = 0; h < 2; ++h) t[h] = __byte_perm(vw[h][0][i2 / 2], vw[h][1][i2 / 2], i2 & 1 ? 0x7632 : 0x5410);
+          uint32_t f0[4], f1[4];  // of the two keys of each half
+          q4a_codes(__byte_perm(vw[0][0][i2 / 2], vw[0][1][i2 / 2], i2 & 1 ? 0x7632 : 0x5410), f0);
+          q4a_codes(__byte_perm(vw[1][0][i2 / 2], vw[1][1][i2 / 2], i2 & 1 ? 0x7632 : 0x5410), f1);
 #pragma unroll
           for (int s = 0; s < 2; ++s) {
-            const uint32_t f[4] = {q4a_codes(t[0], 2 * s), q4a_codes(t[0], 2 * s + 1), q4a_codes(t[1], 2 * s),
-                                   q4a_codes(t[1], 2 * s + 1)};
+            const uint32_t f[4] = {f0[2 * s], f0[2 * s + 1], f1[2 * s], f1[2 * s + 1]};
 #pragma unroll
             for (int x = 0; x < NT; ++x) pga_mma(o[2 * i2 + s][x], f, p[x][i2 / BG][0], p[x][i2 / BG][1]);
           }
         }
       }
       __syncwarp();
-      slot = slot + 1 == Q4A_STAGES ? (parity ^= 1, 0) : slot + 1;
-      const bool ends = use.t + 1 == use.tiles;
-      if (ends || i + 1 == n) {
+      slot = slot + 1 == STAGES ? (parity ^= 1, 0) : slot + 1;
+      if (info.w || i + 1 == n) {
         end_piece();
-        if (!ends) {  // goes on in the next share; the ring is empty
+        if (!info.w) {  // goes on in the next share; the ring is empty
           keep_piece(mine);
-          if (lane == 0) meta[warp] = make_int3(began ? 2 : 1, use.b, use.h);
+          if (lane == 0) meta[warp] = make_int3(began ? 2 : 1, b, h);
         } else if (began) {
           // begun before the block: it is all that the block holds of its pair
-          keep_piece(warp == 0 ? part : a.early + static_cast<int64_t>(me) * ROWS * T::ROW);
+          keep_piece(warp == 0 ? part : a.early + static_cast<int64_t>(me) * ROWS * ROW);
         } else {
-          const int g = use.h / a.qt, q0 = (use.h - g * a.qt) * ROWS;
+          const int g = a.qt == 1 ? h : h / a.qt, q0 = (h - g * a.qt) * ROWS;
 #pragma unroll
           for (int x = 0; x < NT; ++x)
 #pragma unroll
@@ -403,7 +479,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
               const int row = q0 + x * 8 + 2 * c + i2;
               if (row < gs) {
                 const float f = l[x][i2] != 0.f ? 1.f / l[x][i2] : 0.f;
-                __nv_bfloat16* dst = a.out + (static_cast<int64_t>(use.b) * a.hq + g * gs + row) * D + 4 * r;
+                __nv_bfloat16* dst = a.out + (static_cast<int64_t>(b) * a.hq + g * gs + row) * D + 4 * r;
 #pragma unroll
                 for (int s = 0; s < BLK; ++s)
                   *reinterpret_cast<uint2*>(dst + 32 * s) =
@@ -412,13 +488,6 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
               }
             }
         }
-        if (i + 1 < n) {
-          use.next(a, pre);
-          began = false;
-          begin_piece();
-        }
-      } else {
-        ++use.t;
       }
     }
   }
@@ -510,8 +579,7 @@ int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const
   a.hv = Hkv * a.qt;
   a.sl2 = (scale > 0.f ? scale : 1.f / sqrtf(static_cast<float>(D))) * 1.4426950408889634f;
   a.extra = Q4A_EXTRA;
-  const int keys = 2048 / D;
-  const int64_t most = B * ((max_pages * page_size + keys - 1) / keys + 1) * a.hv;  // tiles, at most
+  const int64_t most = B * ((max_pages * page_size + Q4A_KEYS - 1) / Q4A_KEYS + 1) * a.hv;  // tiles, at most
   DM_ARG_CHECK(most + Q4A_EXTRA * B * a.hv <= INT_MAX, "paged_attention_q4: B * max_pages * page_size * heads is too large");
   const int per_sm = rows == 8 ? 2 : 1;
   const int grid = static_cast<int>(
@@ -520,7 +588,7 @@ int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const
   a.early = static_cast<float*>(ws);
   a.part = a.early + static_cast<size_t>(grid) * PGA_WARPS * piece;
   a.info = reinterpret_cast<int4*>(a.part + static_cast<size_t>(grid) * 2 * piece);
-  const size_t smem = static_cast<size_t>(PGA_WARPS) * Q4A_STAGES * (keys / 8) * q4_tile_bytes(D, group) +
+  const size_t smem = static_cast<size_t>(PGA_WARPS) * q4a_stages(D) * Q4A_SETS * q4_tile_bytes(D, group) +
                       2 * (static_cast<size_t>(B) + 1) * sizeof(int);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   auto go = [&](auto main, auto join) -> int {

@@ -10,125 +10,188 @@ struct Q4Rows {
   uint8_t* pages;
   int64_t N, rows, k_stride, v_stride, page_stride;  // rows: of the pool; strides of k and v in elements
   int32_t* status;
-  int hkv, shift;
+  int hkv, shift, lanes;  // 1 << lanes threads to a row
 };
 
-// Eight features of a row per lane, so that a lane holds a 32-bit word of codes of a key
-// or two 16-bit words of a value, D / 8 lanes per (row, KV head, key or value).
+// A lane has eight features of a KV head at a time, of the key and of the value: a 32-bit
+// word of the key's codes, two 16-bit words of the value's. 1 << lanes threads (at most a
+// warp) walk over a row, CHUNKS pieces of a thread loaded ahead, so that a warp has up to 2 KB in flight.
 template <int D, int G>
 struct Q4Lane {
   using T = Q4Tile<D, G>;
-  static constexpr int LANES = D / 8, BLOCKS = D / 32, GROUP = D / G, GL = GROUP / 8;  // GL lanes to a group
-  int64_t n;      // row of the call; -1: none
-  int head, t;    // KV head, lane of the row
-  bool value;
-  uint8_t* tile;  // its part of the tile: codes of the row, and its parameters
-  int codes, params;
-  __device__ __forceinline__ Q4Lane(const Q4Rows& a) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
-    t = static_cast<int>(i % LANES);
-    const int64_t part = i / LANES;
-    value = part & 1;
-    head = static_cast<int>((part >> 1) % a.hkv);
-    n = (part >> 1) / a.hkv;
-    tile = nullptr;
-    if (n >= a.N) {
-      n = -1;
-      return;
-    }
-    const int slot = a.slots[n];
-    if (slot < 0 || slot >= a.rows) {
-      if (slot >= a.rows || slot < -1) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
-      n = -1;
-      return;
-    }
-    const int off = slot & ((1 << a.shift) - 1);
-    tile = a.pages + (slot >> a.shift) * a.page_stride +
-           ((static_cast<int64_t>(head) << a.shift >> 3) + (off >> 3)) * T::BYTES;
-    const int row = off & 7;
-    codes = (value ? T::V : T::K) + row * T::CODES;
-    params = (value ? T::VP : T::KP) + row * T::PARAMS + (t / GL) * 4;
+  static constexpr int LANES = D / 8, BLOCKS = D / 32, GL = D / G / 8;  // lanes of a head's row, and of a group
+  static constexpr int CHUNKS = 2;
+  // Words of a value's row lie apart (16-bit word (2 (t & 3) + j) BLOCKS + (t >> 2) of lane t's
+  // half j): two lanes 4 apart hold the halves of two 32-bit words, one for each of them. The
+  // same exchange leads back.
+  static __device__ __forceinline__ uint32_t exchange(uint32_t w, int t) {
+    const bool odd = (t >> 2) & 1;
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, w, 4);
+    return odd ? __byte_perm(other, w, 0x7632) : __byte_perm(w, other, 0x5410);
   }
-  __device__ __forceinline__ int key_word() const { return codes + ((t & 3) * BLOCKS + (t >> 2)) * 4; }
-  __device__ __forceinline__ int value_word() const { return codes + (2 * (t & 3) * BLOCKS + (t >> 2)) * 2; }
+  static __device__ __forceinline__ int key_word(int t) { return ((t & 3) * BLOCKS + (t >> 2)) * 4; }
+  static __device__ __forceinline__ int value_word(int t) {  // of exchange()
+    return ((2 * (t & 3) + ((t >> 2) & 1)) * BLOCKS + (t >> 3) * 2) * 2;
+  }
 };
+
+// The eight rows of a head in which a slot lies; null for a slot of -1, or (marked) outside the pool.
+template <class T>
+__device__ __forceinline__ uint8_t* q4_tile(const Q4Rows& a, int slot, bool mark) {
+  if (slot < 0 || slot >= a.rows) {
+    if (mark && slot != -1) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
+    return nullptr;
+  }
+  const int off = slot & ((1 << a.shift) - 1);
+  return a.pages + (slot >> a.shift) * a.page_stride + static_cast<int64_t>(off >> 3) * T::BYTES;
+}
 
 __device__ __forceinline__ void q4_unpack8(const uint4& u, float (&x)[8]) {
   x[0] = bf16_lo(u.x), x[1] = bf16_hi(u.x), x[2] = bf16_lo(u.y), x[3] = bf16_hi(u.y);
   x[4] = bf16_lo(u.z), x[5] = bf16_hi(u.z), x[6] = bf16_lo(u.w), x[7] = bf16_hi(u.w);
 }
 
-template <int D, int G>
-__global__ void __launch_bounds__(256) k_paged_append_q4(Q4Rows a, const __nv_bfloat16* k, const __nv_bfloat16* v) {
-  using L = Q4Lane<D, G>;
-  pdl_wait();
-  const L l(a);
-  float x[8] = {};
-  if (l.n >= 0) {
-    const __nv_bfloat16* src = (l.value ? v + l.n * a.v_stride : k + l.n * a.k_stride) + l.head * D + l.t * 8;
-    q4_unpack8(*reinterpret_cast<const uint4*>(src), x);
-  }
-  pdl_trigger();
-  // NaN where a value is not finite (a difference of its own is not zero)
+// The codes of eight features of a group that GL lanes share, and the group's parameters.
+template <int GL>
+__device__ __forceinline__ uint32_t q4_quantise(const uint4& u, uint32_t* params) {
+  float x[8];
+  q4_unpack8(u, x);
+  // NaN where a value is not finite (its difference from itself is not zero)
   float lo = x[0], hi = x[0], odd = 0.f;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     lo = fminf(lo, x[j]);
     hi = fmaxf(hi, x[j]);
-    odd += x[j] - x[j];
+    odd = fmaf(x[j], 0.f, odd);
   }
 #pragma unroll
-  for (int w = 1; w < L::GL; w <<= 1) {
+  for (int w = 1; w < GL; w <<= 1) {
     lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, w));
     hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, w));
     odd += __shfl_xor_sync(0xffffffffu, odd, w);
   }
-  if (l.n < 0) return;
   const float range = hi - lo;
   const bool finite = odd == 0.f && range <= FLT_MAX;
-  const __nv_bfloat16 step_b = __float2bfloat16_rn(__fdiv_rn(range, 15.f));
-  const float step = __bfloat162float(step_b);
+  const float step = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f)));
+  *params = finite ? pack_bf16x2(step, lo) : 0x7fff7fffu;
+  if (!finite || step == 0.f) return 0;
+  // (x - lo) / step by the step's reciprocal: the addition of 3 * 2^22 rounds it to an integer in
+  // the low bits. It may miss the nearest code only where a value lies half way between two
+  // but for a rounding, which the exact remainder shows; those groups, and steps near or
+  // below the normal numbers, divide.
+  constexpr float MAGIC = 12582912.f;
+  const float inv = __frcp_rn(step);
   uint32_t code = 0;
-  if (finite && step > 0.f) {
+  float far = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float q = fminf(rintf(__fdiv_rn(x[j] - lo, step)), 15.f);
-      code |= static_cast<uint32_t>(q) << (4 * j);
+  for (int j = 0; j < 8; ++j) {
+    const float r = x[j] - lo, t = fmaf(r, inv, MAGIC);
+    far = fmaxf(far, fabsf(fmaf(MAGIC - t, step, r)));
+    code += __float_as_uint(t) << (4 * j);
+  }
+  if (far < 0.5f * step && step >= 0x1p-110f) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) code -= 0x4b400000u << (4 * j);
+    return code;
+  }
+  code = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    code |= static_cast<uint32_t>(fminf(rintf(__fdiv_rn(x[j] - lo, step)), 15.f)) << (4 * j);
+  return code;
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(256) k_paged_append_q4(Q4Rows a, const __nv_bfloat16* k, const __nv_bfloat16* v) {
+  using L = Q4Lane<D, G>;
+  using T = Q4Tile<D, G>;
+  pdl_wait();
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, n = i >> a.lanes;
+  const int lanes = 1 << a.lanes, sub = static_cast<int>(i) & (lanes - 1), words = a.hkv * L::LANES;
+  const int slot = n < a.N ? a.slots[n] : -1;
+  uint8_t* tile = q4_tile<T>(a, slot, sub == 0);
+  const int row = slot & 7;
+  const __nv_bfloat16 *kr = k + n * a.k_stride, *vr = v + n * a.v_stride;
+  const int64_t per_head = static_cast<int64_t>(T::BYTES) << a.shift >> 3;
+  // (every lane of a warp goes round as often: the groups' exchanges need them all)
+  for (int c0 = 0; c0 < words; c0 += L::CHUNKS * lanes) {
+    uint4 ku[L::CHUNKS] = {}, vu[L::CHUNKS] = {};
+#pragma unroll
+    for (int j = 0; j < L::CHUNKS; ++j) {
+      const int c = c0 + j * lanes + sub;
+      if (tile != nullptr && c < words) {
+        ku[j] = *reinterpret_cast<const uint4*>(kr + c * 8);
+        vu[j] = *reinterpret_cast<const uint4*>(vr + c * 8);
+      }
+    }
+    if (c0 + L::CHUNKS * lanes >= words) pdl_trigger();
+#pragma unroll
+    for (int j = 0; j < L::CHUNKS; ++j) {
+      const int c = c0 + j * lanes + sub, t = c % L::LANES;
+      if (c0 + j * lanes >= words) break;
+      uint32_t kp, vp;
+      const uint32_t kc = q4_quantise<L::GL>(ku[j], &kp), vc = L::exchange(q4_quantise<L::GL>(vu[j], &vp), t);
+      if (tile == nullptr || c >= words) continue;
+      uint8_t* at = tile + (c / L::LANES) * per_head;
+      *reinterpret_cast<uint32_t*>(at + T::K + row * T::CODES + L::key_word(t)) = kc;
+      *reinterpret_cast<uint32_t*>(at + T::V + row * T::CODES + L::value_word(t)) = vc;
+      if (t % L::GL == 0) {
+        *reinterpret_cast<uint32_t*>(at + T::KP + row * T::PARAMS + t / L::GL * 4) = kp;
+        *reinterpret_cast<uint32_t*>(at + T::VP + row * T::PARAMS + t / L::GL * 4) = vp;
+      }
     }
   }
-  if (l.value) {
-    uint16_t* dst = reinterpret_cast<uint16_t*>(l.tile + l.value_word());
-    dst[0] = static_cast<uint16_t>(code);
-    dst[L::BLOCKS] = static_cast<uint16_t>(code >> 16);
-  } else {
-    *reinterpret_cast<uint32_t*>(l.tile + l.key_word()) = code;
+}
+
+// low + step * code of eight codes, the lowest bits first, as bf16.
+__device__ __forceinline__ uint4 q4_values8(uint32_t code, uint32_t params) {
+  const float step = bf16_lo(params), lo = bf16_hi(params);
+  float x[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float q = __uint_as_float(((code >> (4 * j)) & 15u) | 0x4b000000u) - 8388608.f;
+    x[j] = fmaf(step, q, lo);
   }
-  if (l.t % L::GL == 0)
-    *reinterpret_cast<uint32_t*>(l.tile + l.params) = finite ? pack_bf16x2(step, lo) : 0x7fff7fffu;
+  return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
 
 template <int D, int G>
 __global__ void __launch_bounds__(256) k_paged_read_q4(Q4Rows a, __nv_bfloat16* k, __nv_bfloat16* v) {
   using L = Q4Lane<D, G>;
+  using T = Q4Tile<D, G>;
   pdl_wait();
-  const L l(a);
-  if (l.n < 0) return;
-  uint32_t code;
-  if (l.value) {
-    const uint16_t* src = reinterpret_cast<const uint16_t*>(l.tile + l.value_word());
-    code = src[0] | static_cast<uint32_t>(src[L::BLOCKS]) << 16;
-  } else {
-    code = *reinterpret_cast<const uint32_t*>(l.tile + l.key_word());
-  }
-  const uint32_t p = *reinterpret_cast<const uint32_t*>(l.tile + l.params);
-  pdl_trigger();
-  const float step = bf16_lo(p), lo = bf16_hi(p);
-  float x[8];
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, n = i >> a.lanes;
+  const int lanes = 1 << a.lanes, sub = static_cast<int>(i) & (lanes - 1), words = a.hkv * L::LANES;
+  const int slot = n < a.N ? a.slots[n] : -1;
+  const uint8_t* tile = q4_tile<T>(a, slot, sub == 0);
+  const int row = slot & 7;
+  __nv_bfloat16 *kr = k + n * a.k_stride, *vr = v + n * a.v_stride;
+  const int64_t per_head = static_cast<int64_t>(T::BYTES) << a.shift >> 3;
+  for (int c0 = 0; c0 < words; c0 += L::CHUNKS * lanes) {
+    uint32_t kc[L::CHUNKS], vc[L::CHUNKS], kp[L::CHUNKS], vp[L::CHUNKS];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = fmaf(step, static_cast<float>((code >> (4 * j)) & 15u), lo);
-  __nv_bfloat16* dst = (l.value ? v + l.n * a.v_stride : k + l.n * a.k_stride) + l.head * D + l.t * 8;
-  *reinterpret_cast<uint4*>(dst) =
-      make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+    for (int j = 0; j < L::CHUNKS; ++j) {
+      const int c = c0 + j * lanes + sub, t = c % L::LANES;
+      kc[j] = vc[j] = kp[j] = vp[j] = 0;
+      if (tile != nullptr && c < words) {
+        const uint8_t* at = tile + (c / L::LANES) * per_head;
+        kc[j] = *reinterpret_cast<const uint32_t*>(at + T::K + row * T::CODES + L::key_word(t));
+        vc[j] = *reinterpret_cast<const uint32_t*>(at + T::V + row * T::CODES + L::value_word(t));
+        kp[j] = *reinterpret_cast<const uint32_t*>(at + T::KP + row * T::PARAMS + t / L::GL * 4);
+        vp[j] = *reinterpret_cast<const uint32_t*>(at + T::VP + row * T::PARAMS + t / L::GL * 4);
+      }
+    }
+    if (c0 + L::CHUNKS * lanes >= words) pdl_trigger();
+#pragma unroll
+    for (int j = 0; j < L::CHUNKS; ++j) {
+      const int c = c0 + j * lanes + sub;
+      if (c0 + j * lanes >= words) break;
+      const uint32_t w = L::exchange(vc[j], c % L::LANES);
+      if (tile == nullptr || c >= words) continue;
+      *reinterpret_cast<uint4*>(kr + c * 8) = q4_values8(kc[j], kp[j]);
+      *reinterpret_cast<uint4*>(vr + c * 8) = q4_values8(w, vp[j]);
+    }
+  }
 }
 
 // The checks that the two calls share, and their arguments.
@@ -156,6 +219,8 @@ static int q4_rows(const char* name, const void* k, int64_t k_row_stride, const 
   a->status = status_dev;
   a->hkv = Hkv;
   a->shift = __builtin_ctz(static_cast<unsigned>(page_size));
+  a->lanes = 3;  // the least power of two that covers a row, at most a warp
+  while (a->lanes < 5 && (1 << a->lanes) < Hkv * (D / 8)) ++a->lanes;
   return DECOMOE_OK;
 }
 
@@ -190,8 +255,7 @@ int decomoe_paged_append_q4(const void* k_new, int64_t k_row_stride, const void*
                           {slot_map, static_cast<size_t>(N) * 4}}),
                "paged_append_q4: the pool overlaps an input");
   a.pages = static_cast<uint8_t*>(pages);
-  const int64_t grid = (N * Hkv * 2 * (D / 8) + 255) / 256;
-  DM_ARG_CHECK(grid <= INT_MAX, "paged_append_q4: too many rows");
+  const int64_t grid = ((N << a.lanes) + 255) / 256;
   return q4_dispatch(D, group, [&](auto d, auto g) -> int {
     DM_CUDA_CHECK(launch_pdl_late(k_paged_append_q4<d.value, g.value>, dim3(static_cast<unsigned>(grid)), dim3(256), 0,
                                   reinterpret_cast<cudaStream_t>(stream), a, static_cast<const __nv_bfloat16*>(k_new),
@@ -220,8 +284,7 @@ int decomoe_paged_read_q4(const int32_t* slot_map, int64_t N, const void* pages,
   DM_ARG_CHECK(!overlaps(k, {slots, pool}) && !overlaps(v, {slots, pool}) && (side_by_side || !overlaps(k, {v})),
                "paged_read_q4: an output overlaps an input or the other output");
   a.pages = const_cast<uint8_t*>(static_cast<const uint8_t*>(pages));
-  const int64_t grid = (N * Hkv * 2 * (D / 8) + 255) / 256;
-  DM_ARG_CHECK(grid <= INT_MAX, "paged_read_q4: too many rows");
+  const int64_t grid = ((N << a.lanes) + 255) / 256;
   return q4_dispatch(D, group, [&](auto d, auto g) -> int {
     DM_CUDA_CHECK(launch_pdl_late(k_paged_read_q4<d.value, g.value>, dim3(static_cast<unsigned>(grid)), dim3(256), 0,
                                   reinterpret_cast<cudaStream_t>(stream), a, static_cast<__nv_bfloat16*>(k_out),
