@@ -609,7 +609,8 @@ def q4_rows_to_tile(codes, step, low, value):
 
 
 def q4_values(pages, D, group):
-    """(keys, values, |step (code - 8)| of values) [num_pages, page_size, Hkv, D] of a pool of bytes."""
+    """(keys, values, step code of keys, step code of values) [num_pages, page_size, Hkv, D]
+    of a pool of bytes."""
     pages = np.asarray(pages)
     P, H, T, _ = pages.shape
     G, out = D // group, []
@@ -625,8 +626,8 @@ def q4_values(pages, D, group):
         rows = lambda x: x.reshape(P, H, T * 8, D).transpose(0, 2, 1, 3)  # noqa: E731
         with np.errstate(invalid="ignore"):
             out.append(rows(low + step * q))
-            wide = rows(np.abs(step * (q - 8)))
-    return out[0], out[1], wide
+            out.append(rows(step * q))
+    return out[0], out[2], out[1], out[3]
 
 
 # ------------------------------------------------- token log probabilities

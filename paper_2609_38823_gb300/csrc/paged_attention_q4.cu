@@ -1,6 +1,8 @@
 // Attention of one new token per request over a paged key-value cache in 4 bits
 // (decoding on the text-only cache, DecoMoE Section 3.2 and Algorithm 2, last step, for a
 // batch of requests), the visual block of a request left out where it has exited.
+#include <cuda_fp16.h>
+
 #include "paged_q4.cuh"
 #include "paged_share.cuh"
 
@@ -10,7 +12,7 @@ constexpr int Q4A_KEYS = 32;     // rows of a tile
 constexpr int Q4A_SETS = Q4A_KEYS / 8;
 constexpr int Q4A_BLOCKS = 320;  // of a launch, at most
 constexpr int Q4A_EXTRA = 3;     // what a (request, KV head) pair costs beside its tiles, in tiles
-constexpr int q4a_stages(int D) { return D == 128 ? 3 : 4; }
+constexpr int q4a_stages(int D) { return 2; }
 
 // A tile: KEYS consecutive rows of a request from a multiple of KEYS on (so that eight rows
 // always lie together in a page), those that are hidden or past the length left out of
@@ -53,52 +55,80 @@ __device__ __forceinline__ void q4a_lds(uint32_t addr, uint32_t (&v)[N]) {
   else
     v[0] = q4a_lds(addr);
 }
-// The four codes of each half of w as bf16 pairs of (code - 8) / 64, exact: masked in
-// place a code is a subnormal number, code 2^-133 or (four bits up) code 2^-129, which one multiply-add
-// brings there.
-__device__ __forceinline__ uint32_t q4a_fma(uint32_t u, uint32_t by) {
-  uint32_t r;
-  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(u), "r"(by), "r"(0xbe00be00u));  // - 1/8
-  return r;
+// pga_mma onto zeros.
+__device__ __forceinline__ void q4a_mma0(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
+// The same product of fp16 numbers, onto zeros or c.
+template <bool ZERO>
+__device__ __forceinline__ void q4a_mma_h(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  if constexpr (ZERO)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t q4a_half2(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// The larger ones of two pairs of bf16 numbers, NaN being none.
+__device__ __forceinline__ uint32_t q4a_max2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 r = __hmax2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// The four codes of each half of w as fp16 pairs: masked in place a code's bits are those of a
+// subnormal number, code 2^-24 or, the second and fourth, code 2^-20. The products take
+// them as they are.
 __device__ __forceinline__ void q4a_codes(uint32_t w, uint32_t (&f)[4]) {
   const uint32_t v = w >> 8;
-  f[0] = q4a_fma(w & 0x000f000fu, 0x7f007f00u);  // 2^127
-  f[1] = q4a_fma(w & 0x00f000f0u, 0x7d007d00u);  // 2^123
-  f[2] = q4a_fma(v & 0x000f000fu, 0x7f007f00u);
-  f[3] = q4a_fma(v & 0x00f000f0u, 0x7d007d00u);
+  f[0] = w & 0x000f000fu;
+  f[1] = w & 0x00f000f0u;
+  f[2] = v & 0x000f000fu;
+  f[3] = v & 0x00f000f0u;
 }
 
-// Where the copies of a warp stand in the numbered tiles: a tile of a pair, and the pair's
-// rows, table and place in a page.
+// The first `count` (none or all where it is outside) of eight rows.
+__device__ __forceinline__ uint32_t q4a_first(int count) { return (1u << min(max(count, 0), 8)) - 1u; }
+
+// Where the copies of a warp stand, BATCH tiles at a time: lane 4 k + s looks after set s
+// (eight rows) of the batch's tile k, so that lengths, tables and places are worked out
+// once in BATCH tiles. The pages of a batch are loaded when the one before it is begun.
+constexpr int Q4A_BATCH = 8;
 struct Q4aLook {
-  int b, h, t, tiles, before, skip, n, h0, he;
-  const int32_t* table;
-  const uint8_t* head;
-  __device__ __forceinline__ void pair(const PagedQ4Args& a, int tile_bytes) {
-    head = a.pages + (static_cast<int64_t>(a.qt == 1 ? h : h / a.qt) << a.shift >> 3) * tile_bytes;
+  int b, h, t, tiles;  // this lane's tile
+  int left;            // tiles of the share from this lane's tile on; none: <= 0
+  int at, page;        // its eight rows: the first, and their page
+  uint32_t want;       // those that the request sees
+  // To the tile `by` tiles on.
+  __device__ __forceinline__ void advance(const PagedQ4Args& a, const int* pre, int by) {
+    left -= by;
+    if (left <= 0) return;
+    t += by;
+    while (t >= tiles) {
+      t -= tiles;
+      if (++h < a.hv) continue;
+      h = 0;
+      do ++b;
+      while (pre[b + 1] == pre[b]);
+      tiles = pre[b + 1] - pre[b];
+    }
   }
-  __device__ __forceinline__ void enter(const PagedQ4Args& a, int tile_bytes) {
+  __device__ __forceinline__ void load(const PagedQ4Args& a, int set) {
+    want = 0;
+    if (left <= 0) return;
     bool bad = false;  // marked by the launch's first look at the lengths
     const PgaReq r = pga_request(a, b, &bad);
-    tiles = Q4aTiles::count(r);
-    before = Q4aTiles::before(r);
-    skip = Q4aTiles::after(r) - before;
-    n = r.seen + r.hc;
-    h0 = r.h0;
-    he = r.h0 + r.hc;
-    table = a.table + b * a.max_pages;
-    pair(a, tile_bytes);
-  }
-  // To the next tile; in the last pair it stays past the end (nobody looks).
-  __device__ __forceinline__ void next(const PagedQ4Args& a, const int* pre, int tile_bytes) {
-    if (++t < tiles) return;
-    t = 0;
-    if (++h < a.hv) return pair(a, tile_bytes);
-    h = 0;
-    do ++b;
-    while (b < a.B && pre[b + 1] == pre[b]);
-    if (b < a.B) enter(a, tile_bytes);
+    const int before = Q4aTiles::before(r), he = r.h0 + r.hc;
+    at = (t < before ? t : t - before + Q4aTiles::after(r)) * Q4A_KEYS + set * 8;
+    want = q4a_first(r.seen + r.hc - at) & ~(q4a_first(he - at) & ~q4a_first(r.h0 - at));
+    if (want != 0) page = a.table[b * a.max_pages + (at >> a.shift)];
   }
 };
 
@@ -115,7 +145,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
   static_assert(ROWS * ROW * 4 <= RING, "a piece fits the ring");
   extern __shared__ __align__(1024) uint8_t q4a_smem[];
   __shared__ __align__(8) uint64_t bars[PGA_WARPS][STAGES];
-  __shared__ int4 tile_info[PGA_WARPS][STAGES];  // rows seen, request, head tile, whether the pair ends
+  __shared__ int4 tile_info[PGA_WARPS][2 * Q4A_BATCH];  // rows seen, request, head tile, whether the pair ends
   __shared__ int3 meta[PGA_WARPS];
   __shared__ int abort_flag;
   int* pre = reinterpret_cast<int*>(q4a_smem + PGA_WARPS * RING);
@@ -142,82 +172,107 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
 
   if (r0 < r1) {
     // ---- lookup and copy of tiles, ahead of their use
-    Q4aLook look;
-    look.b = __shfl_sync(0xffffffffu, seek.b, 0);
-    look.h = __shfl_sync(0xffffffffu, seek.h, 0);
-    look.t = __shfl_sync(0xffffffffu, seek.t, 0);
-    look.enter(a, L::BYTES);
-    bool began = look.t > 0;  // the piece's pair began in an earlier share
-    const int in_page = (1 << a.shift) - 1;
-    int page = -1, off = 0;
-    uint32_t want = 0;  // the tile's rows that the request sees
-    auto lookup = [&]() {  // the page of this lane's eight rows
-      const int at = (look.t < look.before ? look.t : look.t + look.skip) * Q4A_KEYS;
-      const int j = at + lane;
-      want = __ballot_sync(0xffffffffu, j < look.n && (j < look.h0 || j >= look.he));
-      const int p = at + lane * 8;
-      page = -1;
-      off = ((p & in_page) >> 3) * L::BYTES;
-      if (lane < Q4A_SETS && ((want >> (lane * 8)) & 0xffu)) page = look.table[p >> a.shift];
+    const int n = r1 - r0;
+    int b = __shfl_sync(0xffffffffu, seek.b, 0), h = __shfl_sync(0xffffffffu, seek.h, 0);  // of the piece
+    const int t0 = __shfl_sync(0xffffffffu, seek.t, 0);
+    bool began = t0 > 0;  // the piece's pair began in an earlier share
+    const int set = lane & (Q4A_SETS - 1), mine_of = lane / Q4A_SETS;
+    Q4aLook look = {b, h, t0, pre[b + 1] - pre[b], n, 0, 0, 0};
+    look.advance(a, pre, mine_of);
+    look.load(a, set);
+    const uint8_t* src = nullptr;
+    uint32_t bytes = 0;  // of the tile
+    bool there = false;
+    auto begin_batch = [&](int which) {
+      there = look.want != 0 && look.page >= 0 && look.page < a.num_pages;
+      if (look.want != 0 && !there) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
+      uint32_t mask = there ? look.want << (8 * set) : 0u;
+      mask |= __shfl_xor_sync(0xffffffffu, mask, 1);
+      mask |= __shfl_xor_sync(0xffffffffu, mask, 2);
+      bytes = __popc(__ballot_sync(0xffffffffu, there) >> (lane & ~(Q4A_SETS - 1)) & ((1u << Q4A_SETS) - 1)) * L::BYTES;
+      if (there)
+        src = a.pages + look.page * a.page_stride +
+              ((static_cast<int64_t>(a.qt == 1 ? look.h : look.h / a.qt) << a.shift >> 3) +
+               ((look.at & ((1 << a.shift) - 1)) >> 3)) * L::BYTES;
+      if (set == 0)
+        tile_info[warp][(which & 1) * Q4A_BATCH + mine_of] =
+            make_int4(static_cast<int>(mask), look.b, look.h, look.t + 1 == look.tiles);
+      look.advance(a, pre, Q4A_BATCH);
+      look.load(a, set);
+      __syncwarp();
     };
-    auto issue = [&](int slot) {
-      const bool some = lane < Q4A_SETS && ((want >> (lane * 8)) & 0xffu);
-      const bool there = some && page >= 0 && page < a.num_pages;
-      if (some && !there) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
-      const uint32_t sets = __ballot_sync(0xffffffffu, there), bar = bar_s + slot * 8;
-      if (lane == 0) {
-        uint32_t mask = want;
-        if (sets != (1u << Q4A_SETS) - 1)
-#pragma unroll
-          for (int i = 0; i < Q4A_SETS; ++i)
-            if (!((sets >> i) & 1u)) mask &= ~(0xffu << (8 * i));
-        tile_info[warp][slot] = make_int4(static_cast<int>(mask), look.b, look.h, look.t + 1 == look.tiles);
-        mbar_arrive_expect_tx(bar, __popc(sets) * L::BYTES);
+    auto issue = [&](int tile, int slot) {
+      if (tile % Q4A_BATCH == 0) begin_batch(tile / Q4A_BATCH);
+      if (mine_of == tile % Q4A_BATCH) {
+        const uint32_t bar = bar_s + slot * 8;
+        if (set == 0) mbar_arrive_expect_tx(bar, bytes);
+        __syncwarp(((1u << Q4A_SETS) - 1) << (lane & ~(Q4A_SETS - 1)));
+        if (there) q4a_bulk(ring_s + slot * STAGE + set * L::BYTES, src, L::BYTES, bar);
       }
       __syncwarp();
-      if (there) q4a_bulk(ring_s + slot * STAGE + lane * L::BYTES, look.head + page * a.page_stride + off, L::BYTES, bar);
     };
-    const int n = r1 - r0;
-    lookup();
 
     // a lane's part of the operands: row kr of eight keys, word (kr, c) of the codes; keys c and
     // c + 4 of eight values, features 32 i + 4 r .. + 3
     const int r = lane >> 2, c = lane & 3, kr = (r >> 1) + 4 * (r & 1);
     uint32_t qf[NT][BLK][4], qs[NT][G == 4 ? 3 : 2];
-    float o[2 * BLK][NT][4], low[NT][2][G], m[NT][2], l[NT][2];
-    int b = look.b, h = look.h;  // of the piece
+    float sl2[NT][2];
+    float o[2 * BLK][NT][4], low[NT][2][G], m[NT][2], ref[NT][2], l[NT][2];
+    float pass[NT][2];  // ref: m, 0 for none; pass: m + 8
+    // steps seen so far are below room; grow, a power of two, times those is below 2^6
+    float room = 0.f, grow = 1.f;
     auto begin_piece = [&]() {
       const int g = a.qt == 1 ? h : h / a.qt, q0 = (h - g * a.qt) * ROWS;
       const __nv_bfloat16* q = a.q + b * a.q_stride + static_cast<int64_t>(g) * gs * D;
 #pragma unroll
       for (int x = 0; x < NT; ++x) {
         const int row = q0 + x * 8 + r;
+        // the queries times a power of two that brings their largest into [2^14, 2^15)
+        float v[BLK][8], most = 0.f;
+#pragma unroll
+        for (int i = 0; i < BLK; ++i) {
+          uint4 u = make_uint4(0, 0, 0, 0);
+          if (row < gs) u = *reinterpret_cast<const uint4*>(q + static_cast<int64_t>(row) * D + 32 * i + 8 * c);
+          v[i][0] = bf16_lo(u.x), v[i][1] = bf16_hi(u.x), v[i][2] = bf16_lo(u.y), v[i][3] = bf16_hi(u.y);
+          v[i][4] = bf16_lo(u.z), v[i][5] = bf16_hi(u.z), v[i][6] = bf16_lo(u.w), v[i][7] = bf16_hi(u.w);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) most = fmaxf(most, fabsf(v[i][j]));
+        }
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const uint32_t up = min(268u - (__float_as_uint(most) >> 23), 253u);  // its exponent
+        const float by = most <= FLT_MAX ? __uint_as_float(up << 23) : NAN;
         float sum[G];
 #pragma unroll
         for (int i = 0; i < G; ++i) sum[i] = 0.f;
 #pragma unroll
         for (int i = 0; i < BLK; ++i) {
-          uint4 u = make_uint4(0, 0, 0, 0);
-          if (row < gs) u = *reinterpret_cast<const uint4*>(q + static_cast<int64_t>(row) * D + 32 * i + 8 * c);
-          sum[i / BG] += ((bf16_lo(u.x) + bf16_hi(u.x)) + (bf16_lo(u.y) + bf16_hi(u.y))) +
-                         ((bf16_lo(u.z) + bf16_hi(u.z)) + (bf16_lo(u.w) + bf16_hi(u.w)));
-          qf[x][i][0] = __byte_perm(u.x, u.z, 0x5410);
-          qf[x][i][1] = __byte_perm(u.x, u.z, 0x7632);
-          qf[x][i][2] = __byte_perm(u.y, u.w, 0x5410);
-          qf[x][i][3] = __byte_perm(u.y, u.w, 0x7632);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            v[i][j] *= by;
+            sum[i / BG] += v[i][j];
+          }
+          // (odd codes come as 16 code)
+          qf[x][i][0] = q4a_half2(v[i][0], v[i][4]);
+          qf[x][i][1] = q4a_half2(v[i][1] * 0.0625f, v[i][5] * 0.0625f);
+          qf[x][i][2] = q4a_half2(v[i][2], v[i][6]);
+          qf[x][i][3] = q4a_half2(v[i][3] * 0.0625f, v[i][7] * 0.0625f);
         }
-        // a 64th of a group's sum (as the codes are 64ths) in three bf16 numbers, 24 bits, each
-        // with its eightfold in front
+        // what brings a score of these back (codes are 2^-24), and softmax's factor
+        const float back = 0x1p24f * a.sl2 * __uint_as_float((254u - up) << 23);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) sl2[x][i] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + i));
+        // a group's sum (times 2^-24, as the codes) in three bf16 numbers, 24 bits: factors of low
         uint32_t piece[G][3];
 #pragma unroll
         for (int i = 0; i < G; ++i) {
           sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
           sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
-          float rest = sum[i] * 0.015625f;
+          float rest = sum[i] * 0x1p-24f;
 #pragma unroll
           for (int k = 0; k < 3; ++k) {
             const float f = __bfloat162float(__float2bfloat16_rn(rest));
-            piece[i][k] = pack_bf16x2(8.f * f, f);
+            piece[i][k] = pack_bf16x2(0.f, f);
             rest -= f;
           }
         }
@@ -234,8 +289,8 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          m[x][i] = -INFINITY;
-          l[x][i] = 0.f;
+          m[x][i] = pass[x][i] = -INFINITY;
+          ref[x][i] = l[x][i] = 0.f;
 #pragma unroll
           for (int g2 = 0; g2 < G; ++g2) low[x][i][g2] = 0.f;
         }
@@ -244,9 +299,12 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[s][x][i] = 0.f;
       }
+      room = 0.f;
+      grow = 1.f;
     };
     // a finished piece: its sums over the lanes, the lows added to the outputs
     auto end_piece = [&]() {
+      const float back = __uint_as_float((254u << 23) - __float_as_uint(grow));  // 1 / grow
 #pragma unroll
       for (int x = 0; x < NT; ++x)
 #pragma unroll
@@ -259,8 +317,8 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
             for (int w = 4; w < 32; w <<= 1) low[x][i][g] += __shfl_xor_sync(0xffffffffu, low[x][i][g], w);
 #pragma unroll
             for (int s = 2 * BG * g; s < 2 * BG * (g + 1); ++s) {
-              o[s][x][i] = fmaf(o[s][x][i], 64.f, low[x][i][g]);
-              o[s][x][i + 2] = fmaf(o[s][x][i + 2], 64.f, low[x][i][g]);
+              o[s][x][i] = fmaf(o[s][x][i] * 0x1p24f, back, low[x][i][g]);
+              o[s][x][i + 2] = fmaf(o[s][x][i + 2] * 0x1p20f, back, low[x][i][g]);
             }
           }
         }
@@ -283,16 +341,11 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
     };
     int slot = 0, fill = 0;
     uint32_t parity = 0;
-    const float sl2 = 64.f * a.sl2;  // of scores in 64ths
     // the first steps only fill the ring (one copy of the code: a short share runs it cold)
     for (int i = 1 - STAGES; i < n; ++i) {
       if (i + STAGES - 1 < n) {
-        issue(fill);
+        issue(i + STAGES - 1, fill);
         fill = fill + 1 == STAGES ? 0 : fill + 1;
-        if (i + STAGES < n) {
-          look.next(a, pre, L::BYTES);
-          lookup();
-        }
       }
       if (i < 0) {
         if (i == -1) begin_piece();
@@ -308,7 +361,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
         break;
       }
       const uint32_t stage = ring_s + slot * STAGE;
-      const int4 info = tile_info[warp][slot];
+      const int4 info = tile_info[warp][i % (2 * Q4A_BATCH)];
       if (info.y != b || info.z != h) {  // a new pair
         b = info.y;
         h = info.z;
@@ -316,7 +369,8 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
         begin_piece();
       }
       const uint32_t mask = static_cast<uint32_t>(info.x);
-      // ---- scores: sum over the groups of step (q (code - 8)) + (low + 8 step) (sum of q)
+      // ---- scores: sum over the groups of step (q code) + low (sum of q); queries are exact
+      // in fp16 but where a value lies below 2^-27 of the query's largest
       float sc[SUB][NT][4];
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
@@ -330,14 +384,12 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
         }
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
-#pragma unroll
-          for (int i2 = 0; i2 < 4; ++i2) sc[u][x][i2] = 0.f;
-          pga_mma(sc[u][x], kx, qs[x][0], qs[x][1]);
+          q4a_mma0(sc[u][x], kx, qs[x][0], qs[x][1]);
           if constexpr (G == 4) pga_mma(sc[u][x], kx, qs[x][2], 0u);
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          float acc[NT][4] = {};
+          float acc[NT][4];
 #pragma unroll
           for (int i2 = g * BG; i2 < (g + 1) * BG; ++i2) {
             uint32_t f0[4], f1[4];
@@ -347,7 +399,10 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
             for (int s = 0; s < 2; ++s) {
               const uint32_t f[4] = {f0[2 * s], f1[2 * s], f0[2 * s + 1], f1[2 * s + 1]};
 #pragma unroll
-              for (int x = 0; x < NT; ++x) pga_mma(acc[x], f, qf[x][i2][2 * s], qf[x][i2][2 * s + 1]);
+              for (int x = 0; x < NT; ++x) {
+                if (i2 == g * BG && s == 0) q4a_mma_h<true>(acc[x], f, qf[x][i2][0], qf[x][i2][1]);
+                else q4a_mma_h<false>(acc[x], f, qf[x][i2][2 * s], qf[x][i2][2 * s + 1]);
+              }
             }
           }
 #pragma unroll
@@ -357,6 +412,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
         }
       }
       if (mask != 0xffffffffu) {
+        __syncwarp();  // (a branch of its own: as predicates it would cost every tile)
 #pragma unroll
         for (int u = 0; u < SUB; ++u)
 #pragma unroll
@@ -367,78 +423,101 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
               for (int x = 0; x < NT; ++x) sc[u][x][2 * hf] = sc[u][x][2 * hf + 1] = -INFINITY;
             }
       }
-      // ---- the maxima so far, raised only where one is passed by 2^8: weights up to 2^8 cost no
-      // digits, and rescaling the outputs is rare
+      uint32_t vp[SUB][2][G];
 #pragma unroll
-      for (int x = 0; x < NT; ++x) {
-        float mx[2];
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) q4a_lds(stage + (2 * u + hf) * L::BYTES + L::VP + kr * L::PARAMS, vp[u][hf]);
+      if (mask != 0xffffffffu) {
+        __syncwarp();
+#pragma unroll
+        for (int u = 0; u < SUB; ++u)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf)
+            if (!((mask >> (16 * u + 8 * hf + kr)) & 1u))
+#pragma unroll
+              for (int g = 0; g < G; ++g) vp[u][hf][g] = 0u;
+      }
+      // ---- a query's maximum, raised only where a score passes it by 2^8 (weights up to 2^8 cost no
+      // digits), and the scale of the steps, which keeps weights times steps, the fp16 operands
+      // of the value product, below 2^14: the lanes compare theirs only where one of them has to
+      // change, and rescaling the outputs is rare
+      uint32_t widest = 0;  // bf16 bits of the largest step (they are not negative; NaN: its sums say so)
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+          for (int g = 0; g < G; ++g) widest = q4a_max2(widest, vp[u][hf][g]);
+      bool raise = bf16_lo(widest) >= room;
+      float mx[NT][2];
+#pragma unroll
+      for (int x = 0; x < NT; ++x)
 #pragma unroll
         for (int i2 = 0; i2 < 2; ++i2) {
-          mx[i2] = fmaxf(sc[0][x][i2], sc[0][x][i2 + 2]);
 #pragma unroll
-          for (int u = 1; u < SUB; ++u) mx[i2] = fmaxf(mx[i2], fmaxf(sc[u][x][i2], sc[u][x][i2 + 2]));
+          for (int u = 0; u < SUB; ++u) {
+            sc[u][x][i2] *= sl2[x][i2];
+            sc[u][x][i2 + 2] *= sl2[x][i2];
+            const float y = fmaxf(sc[u][x][i2], sc[u][x][i2 + 2]);
+            mx[x][i2] = u == 0 ? y : fmaxf(mx[x][i2], y);
+          }
+          raise |= mx[x][i2] > pass[x][i2];
+        }
+      if (__any_sync(0xffffffffu, raise)) {
+#pragma unroll
+        for (int w = 1; w < 32; w <<= 1) widest = q4a_max2(widest, __shfl_xor_sync(0xffffffffu, widest, w));
+        float wider = 1.f;
+        if (bf16_lo(widest) >= room) {
+          const uint32_t e = max(widest >> 7 & 0xffu, 7u);  // the largest step is below 2^(e - 126)
+          room = e < 254 ? __uint_as_float((e + 1) << 23) : INFINITY;
+          const float to = __uint_as_float((259u - min(e, 254u)) << 23);  // 2^(132 - e)
+          wider = to * __uint_as_float((254u << 23) - __float_as_uint(grow));  // its inverse: a power of two
+          grow = to;
         }
 #pragma unroll
-        for (int w = 4; w < 32; w <<= 1) {
-          mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], w));
-          mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], w));
-        }
-        mx[0] *= sl2;
-        mx[1] *= sl2;
-        if (__any_sync(0xffffffffu, mx[0] > m[x][0] + 8.f || mx[1] > m[x][1] + 8.f)) {
+        for (int x = 0; x < NT; ++x)
 #pragma unroll
           for (int i2 = 0; i2 < 2; ++i2) {
-            const float to = fmaxf(m[x][i2], mx[i2]);
+#pragma unroll
+            for (int w = 4; w < 32; w <<= 1) mx[x][i2] = fmaxf(mx[x][i2], __shfl_xor_sync(0xffffffffu, mx[x][i2], w));
+            const float to = fmaxf(m[x][i2], mx[x][i2]);
             // nothing seen so far, and nothing here: any factor does
             const float f = to == -INFINITY ? 1.f : pga_ex2(m[x][i2] - to);
             m[x][i2] = to;
+            pass[x][i2] = to + 8.f;
+            ref[x][i2] = to == -INFINITY ? 0.f : to;
             l[x][i2] *= f;
 #pragma unroll
             for (int g = 0; g < G; ++g) low[x][i2][g] *= f;
 #pragma unroll
             for (int s = 0; s < 2 * BLK; ++s) {
-              o[s][x][i2] *= f;
-              o[s][x][i2 + 2] *= f;
+              o[s][x][i2] *= f * wider;
+              o[s][x][i2 + 2] *= f * wider;
             }
           }
-        }
       }
       // ---- weights and values
-      float ref[NT][2];
-#pragma unroll
-      for (int x = 0; x < NT; ++x)
-#pragma unroll
-        for (int i2 = 0; i2 < 2; ++i2) ref[x][i2] = m[x][i2] == -INFINITY ? 0.f : m[x][i2];
 #pragma unroll
       for (int u = 0; u < SUB; ++u) {
         const uint32_t at[2] = {stage + 2 * u * L::BYTES, stage + (2 * u + 1) * L::BYTES};
-        uint32_t vp[2][G];
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) q4a_lds(at[hf] + L::VP + kr * L::PARAMS, vp[hf]);
-        if (mask != 0xffffffffu) {
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-            if (!((mask >> (16 * u + 8 * hf + kr)) & 1u))
-#pragma unroll
-              for (int g = 0; g < G; ++g) vp[hf][g] = 0u;
-        }
         uint32_t p[NT][G][2];
 #pragma unroll
         for (int x = 0; x < NT; ++x) {
           float w[4];
 #pragma unroll
-          for (int i2 = 0; i2 < 4; ++i2) w[i2] = pga_ex2(fmaf(sc[u][x][i2], sl2, -ref[x][i2 & 1]));
+          for (int i2 = 0; i2 < 4; ++i2) w[i2] = pga_ex2(sc[u][x][i2] - ref[x][i2 & 1]);
           l[x][0] += w[0] + w[2];
           l[x][1] += w[1] + w[3];
-          // weights times steps are the operands of the value product; lows and 8 steps add up in fp32
+          // weights times steps are the operands of the value product; lows add up in fp32
 #pragma unroll
           for (int g = 0; g < G; ++g)
 #pragma unroll
             for (int hf = 0; hf < 2; ++hf) {
-              const float step = bf16_lo(vp[hf][g]), at8 = fmaf(8.f, step, bf16_hi(vp[hf][g]));
-              low[x][0][g] = fmaf(w[2 * hf], at8, low[x][0][g]);
-              low[x][1][g] = fmaf(w[2 * hf + 1], at8, low[x][1][g]);
-              p[x][g][hf] = pga_transpose(pack_bf16x2(w[2 * hf] * step, w[2 * hf + 1] * step));
+              const float step = bf16_lo(vp[u][hf][g]) * grow, at0 = bf16_hi(vp[u][hf][g]);
+              low[x][0][g] = fmaf(w[2 * hf], at0, low[x][0][g]);
+              low[x][1][g] = fmaf(w[2 * hf + 1], at0, low[x][1][g]);
+              p[x][g][hf] = pga_transpose(q4a_half2(w[2 * hf] * step, w[2 * hf + 1] * step));
             }
         }
         uint32_t vw[2][2][BLK / 2];
@@ -456,7 +535,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
           for (int s = 0; s < 2; ++s) {
             const uint32_t f[4] = {f0[2 * s], f0[2 * s + 1], f1[2 * s], f1[2 * s + 1]};
 #pragma unroll
-            for (int x = 0; x < NT; ++x) pga_mma(o[2 * i2 + s][x], f, p[x][i2 / BG][0], p[x][i2 / BG][1]);
+            for (int x = 0; x < NT; ++x) q4a_mma_h<false>(o[2 * i2 + s][x], f, p[x][i2 / BG][0], p[x][i2 / BG][1]);
           }
         }
       }

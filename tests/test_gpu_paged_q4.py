@@ -4,13 +4,16 @@
 Attention: keys and values of the pool are the oracle's inputs, so what differs is the
 kernel's arithmetic. With p the softmax weights, per output element:
   2^-8 |ref|                   rounding of the output to bf16 (half a step)
-  2^-8 sum p |step (q - 8)|    weights times steps rounded to bf16, each by 2^-8 of itself at most
+  2^-11 sum p step q           weights times steps rounded to fp16, each by 2^-11 of itself at most, or
+  n 2^-26 max step             by half of fp16's last place, 2^-25, times codes up to 15, where the n keys'
+                               largest step times the largest weight is 2^5 or more
   2 delta sum p |v|            scores off by delta change a weight by the factor exp(+-delta), and
                                the sum of the weights by as much
 with delta = (D + 32) 2^-23 sum |q k| scale: fp32 sums of D products and of the groups' terms, in
 tensor-core sums that may cut off instead of rounding (2^-23), and the exponentials' 2^-22, which
-the 32 covers where sum |q k| scale is 1 or more; below that 2^-20 stands for it. Sums of outputs over n
-keys in fp32 add n 2^-23 sum p |v|."""
+the 32 covers where sum |q k| scale is 1 or more; below that 2^-20 stands for it. sum |q k| counts the
+kernel's own terms, |q| (step code + |low|). Sums of outputs over n keys in fp32 add n 2^-23 sum p (step code +
+|low|)."""
 import numpy as np
 import pytest
 import torch
@@ -148,7 +151,7 @@ def test_read_values(d, group, n, hkv, ps):
     for at in (4 * d, 8 * d + 32 * G):  # parameters of a sensible size
         par = (torch.rand(pages, hkv, ps // 8, 16 * G, generator=torch.Generator().manual_seed(at)) - 0.3).to(torch.bfloat16)
         pool[..., at:at + 32 * G] = par.view(torch.uint8)
-    k, v, _ = O.q4_values(pool.numpy(), d, group)
+    k, v, *_ = O.q4_values(pool.numpy(), d, group)
     r = np.random.default_rng(n)
     slots = r.permutation(pages * ps)[:n]
     out = torch.full((n, 2 * hkv + 1, d), 7.0, dtype=torch.bfloat16, device=DEV)  # keys and values side by side
@@ -198,7 +201,7 @@ def test_rows_read_back_for_a_chunk_of_a_prompt():
     out, ko, vo = torch.empty_like(q), *(torch.empty(C, hkv, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
     ws = dm.workspace(dm.decomoe_attention_workspace_bytes(n2, C, hq, hkv, d), DEV)
     cache.attend_chunk(0, q, cache.slots_of(1, C), ko, vo, out, ws)
-    kd, vd, _ = O.q4_values(cache.pool[0].cpu().numpy(), d, group)
+    kd, vd, *_ = O.q4_values(cache.pool[0].cpu().numpy(), d, group)
     flat = lambda x: x.reshape(-1, hkv, d)[cache.slots_of(1, C).cpu().numpy()]  # noqa: E731
     assert np.array_equal(f64(ko), O.bf16(flat(kd))) and np.array_equal(f64(vo), O.bf16(flat(vd)))
     assert_close_out(f64(out), O.attention(f64(q), f64(ko), f64(vo)), BF16_REL_L2, BF16_MAX_ABS, "chunk")
@@ -253,7 +256,7 @@ def _ref(q, pool, table, lens, group, hide=None, scale=None):
     q = f64(q)
     B, hq, d = q.shape
     ps, hkv = 8 * pool.shape[2], pool.shape[1]
-    kd, vd, wide = O.q4_values(pool.cpu().numpy(), d, group)
+    kd, vd, span, code = O.q4_values(pool.cpu().numpy(), d, group)
     out, tol = np.zeros(q.shape), np.zeros(q.shape)
     scale = d ** -0.5 if not scale else scale
     for b, n in enumerate(lens):
@@ -263,14 +266,17 @@ def _ref(q, pool, table, lens, group, hide=None, scale=None):
         at = (np.asarray(table)[b, j // ps], j % ps)
         for h in range(hq):
             g = h // (hq // hkv)
-            k, v, w = kd[at][:, g], vd[at][:, g], wide[at][:, g]
+            k, v = kd[at][:, g], vd[at][:, g]
             s = scale * (k @ q[b, h])
             p = np.exp(s - s.max())
             p /= p.sum()
-            size = (np.abs(k) @ np.abs(q[b, h])).max() * scale
+            ks, vs = span[at][:, g], code[at][:, g]
+            size = ((ks + np.abs(k - ks)) @ np.abs(q[b, h])).max() * scale
             delta = (d + 32) * 2.0 ** -23 * size + 2.0 ** -20
+            terms = p @ (vs + np.abs(v - vs))
             out[b, h] = p @ v
-            tol[b, h] = 2.0 ** -8 * (np.abs(out[b, h]) + p @ w) + (2 * delta + len(j) * 2.0 ** -23) * (p @ np.abs(v))
+            tol[b, h] = (2.0 ** -8 * np.abs(out[b, h]) + 2.0 ** -11 * (p @ vs) + len(j) * 2.0 ** -26 * vs.max()
+                         + (2 * delta + len(j) * 2.0 ** -23) * terms)
     return out, tol
 
 
@@ -405,7 +411,7 @@ def test_pool_beyond_32_bit_offsets():
     assert (np.abs(f64(out) - ref) <= tol).all()
     ko, vo = (torch.empty(1, hkv, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
     dm.decomoe_paged_read_q4(_i32([(P - 1) * ps + 63]), pool, ko, vo)
-    k, v, _ = O.q4_values(small.numpy(), d, group)
+    k, v, *_ = O.q4_values(small.numpy(), d, group)
     assert np.array_equal(f64(ko[0]), O.bf16(k[0, 63])) and np.array_equal(f64(vo[0]), O.bf16(v[0, 63]))
 
 
@@ -526,7 +532,7 @@ def test_decode_steps_on_a_cache_in_4_bits():
         hide = [(0, 0), (0, 0), (16, 100) if l >= 1 else (0, 0)]
         ref, tol = _ref(s.q, cache.pool[l], cache.table.cpu().numpy(), cache.seq_len.tolist(), group, hide)
         assert (np.abs(f64(s.heads) - ref) <= tol).all()
-        k, _, _ = O.q4_values(cache.pool[l].cpu().numpy(), D, group)
+        k, *_ = O.q4_values(cache.pool[l].cpu().numpy(), D, group)
         codes, st, low = O.q4_quantise(f64(s.k_new), group)
         assert np.array_equal(k.reshape(-1, HKV, D)[s.slots.cpu().numpy()], np.repeat(low, group, -1) + np.repeat(st, group, -1) * codes)
         seen.append(l)
@@ -580,3 +586,39 @@ def test_refusals():
     with pytest.raises(ValueError):
         PagedCache(1, 1, pages=2, page_size=4, max_pages=2, hkv=1, d=64, bits=4)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("low,high", [(-30, -30), (-80, -80), (25, 25), (90, 90), (-25, 25), (0, 12)])
+def test_attention_values_of_any_size(low, high):
+    """Values whose sizes lie far from 1, or far apart from key to key: the weights are scaled with the
+    largest step seen so far."""
+    lens, hq, hkv, d, group, ps = [300, 77, 1200], 8, 2, 128, 64, 16
+    q, pool, table = _case(lens, hq, hkv, d, group, ps, 11)
+    r = np.random.default_rng(5)
+    for b, n in enumerate(lens):
+        k = _rows(n, hkv, d, b)
+        v = (_rows(n, hkv, d, 20 + b).double() * torch.from_numpy(2.0 ** r.integers(low, high + 1, (n, 1, 1)))).to(torch.bfloat16)
+        slots = [table[b, j // ps] * ps + j % ps for j in range(n)]
+        dm.decomoe_paged_append_q4(k.to(DEV), v.to(DEV), _i32(slots), pool)
+    ref, tol = _ref(q, pool, table, lens, group)
+    off = np.abs(f64(_attend(q.to(DEV), pool, table, lens)) - ref)
+    assert (off <= tol + 2.0 ** -133).all(), (off / np.maximum(tol, 1e-300)).max()
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-12, 1e12, 1e30])
+def test_attention_queries_of_any_size(size):
+    lens = [300, 77]
+    q, pool, table = _case(lens, 8, 2, 128, 32, 16, 12, k_scale=1.0 / size if 1e-13 < size < 1e13 else 1.0)
+    q = (q.double() * size).to(torch.bfloat16)
+    out = _attend(q.to(DEV), pool, table, lens)
+    ref, tol = _ref(q, pool, table, lens, 32)
+    assert (np.abs(f64(out) - ref) <= tol).all()
+
+
+def test_attention_queries_of_zeros():
+    lens = [300, 17, 5]
+    q, pool, table = _case(lens, 8, 2, 128, 32, 16, 13)
+    q[0], q[1, 3], q[2] = 0, 0, 2.0 ** -130
+    out = _attend(q.to(DEV), pool, table, lens)
+    ref, tol = _ref(q, pool, table, lens, 32)
+    assert (np.abs(f64(out) - ref) <= tol).all()

@@ -193,9 +193,9 @@ def test_oracle_codes_are_the_nearest_and_survive_the_layout(d, group):
     for c in range(16):  # no other code is nearer
         assert (mine <= np.abs(lo + s * c - x) + 1e-12).all()
     k, v = O.q4_rows_to_tile(q, step, low, False), O.q4_rows_to_tile(15 - q, step, low, True)
-    keys, values, wide = O.q4_values(np.concatenate([k, v])[None, None, None], d, group)
+    keys, values, span, wide = O.q4_values(np.concatenate([k, v])[None, None, None], d, group)
     assert np.array_equal(keys[0, :, 0], lo + s * q) and np.array_equal(values[0, :, 0], lo + s * (15 - q))
-    assert np.array_equal(wide[0, :, 0], np.abs(s * (7 - q)))
+    assert np.array_equal(wide[0, :, 0], s * (15 - q)) and np.array_equal(span[0, :, 0], s * q)
     # the places by hand: feature 32 i + 8 c + j of a key, 32 i + 4 r + j of a value
     f = 32 + 8 * 2 + 5
     byte = 4 * (2 * (d // 32) + 1) + 5 // 2
