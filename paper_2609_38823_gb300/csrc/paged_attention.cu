@@ -30,6 +30,8 @@ namespace decomoe {
 // 6.2 TB/s but for the 3 us before the first tile and the 4 us of the joins. One request of
 // 2049 rows 8.6 us, all of it latency: of the scan and the search in front, and of the second
 // launch behind (the contiguous kernel of attention.cu, which has neither, takes 5.0).
+constexpr int PGA_WARPS = 8;
+constexpr int PGA_THREADS = 32 * PGA_WARPS;
 constexpr int PGA_STAGES = 3;
 constexpr int PGA_BLOCKS = 160;  // of a launch, at most
 constexpr int PGA_STAGE = 8192;  // bytes of one tile: keys, then values
@@ -75,7 +77,7 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
   int* nz = pre + a.B + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_enter();
-  const PgaPlan plan = pga_begin<T, D>(a, pre, nz);
+  const PgaPlan plan = pga_begin<T, D, PGA_WARPS>(a, pre, nz);
   const int me = blockIdx.x * PGA_WARPS + warp;
   // lane 0 seeks the start of this warp's share, lane 1 that of the next one's
   PgaWalk<T> look;
@@ -310,7 +312,7 @@ __global__ void __launch_bounds__(PGA_THREADS, 1) k_paged_attention(PagedArgs a)
     }
   }
   __syncthreads();
-  pga_join_block<D, NT>(a, plan, meta, pga_smem, PGA_STAGES * PGA_STAGE);
+  pga_join_block<D, NT, PGA_WARPS>(a, plan, meta, pga_smem, PGA_STAGES * PGA_STAGE);
 }
 
 }  // namespace decomoe

@@ -10,7 +10,8 @@ namespace decomoe {
 
 constexpr int Q4A_KEYS = 32;     // rows of a tile
 constexpr int Q4A_SETS = Q4A_KEYS / 8;
-constexpr int Q4A_BLOCKS = 320;  // of a launch, at most
+constexpr int Q4A_BLOCKS = 160;  // of a launch, at most
+constexpr int q4a_warps(int NT) { return NT == 1 ? 16 : 8; }  // of a block, one block per SM: as many as their registers allow
 constexpr int Q4A_EXTRA = 3;     // what a (request, KV head) pair costs beside its tiles, in tiles
 constexpr int q4a_stages(int D) { return 2; }
 
@@ -94,18 +95,20 @@ __device__ __forceinline__ void q4a_codes(uint32_t w, uint32_t (&f)[4]) {
   f[3] = v & 0x00f000f0u;
 }
 
-// The first `count` (none or all where it is outside) of eight rows.
-__device__ __forceinline__ uint32_t q4a_first(int count) { return (1u << min(max(count, 0), 8)) - 1u; }
+// The first `count` (none or all where it is outside) of a tile's rows.
+__device__ __forceinline__ uint32_t q4a_first(int count) {
+  return count >= Q4A_KEYS ? 0xffffffffu : (1u << max(count, 0)) - 1u;
+}
 
 // Where the copies of a warp stand, BATCH tiles at a time: lane 4 k + s looks after set s
-// (eight rows) of the batch's tile k, so that lengths, tables and places are worked out
+// (eight rows) of the batch's tile k and the page that it lies in, so that lengths, tables and places are worked out
 // once in BATCH tiles. The pages of a batch are loaded when the one before it is begun.
 constexpr int Q4A_BATCH = 8;
 struct Q4aLook {
   int b, h, t, tiles;  // this lane's tile
   int left;            // tiles of the share from this lane's tile on; none: <= 0
   int at, page;        // its eight rows: the first, and their page
-  uint32_t want;       // those that the request sees
+  uint32_t want;       // the tile's rows in that page that the request sees
   // To the tile `by` tiles on.
   __device__ __forceinline__ void advance(const PagedQ4Args& a, const int* pre, int by) {
     left -= by;
@@ -120,21 +123,23 @@ struct Q4aLook {
       tiles = pre[b + 1] - pre[b];
     }
   }
-  __device__ __forceinline__ void load(const PagedQ4Args& a, int set) {
+  __device__ __forceinline__ void load(const PagedQ4Args& a, int set, uint32_t in_page) {
     want = 0;
     if (left <= 0) return;
     bool bad = false;  // marked by the launch's first look at the lengths
     const PgaReq r = pga_request(a, b, &bad);
     const int before = Q4aTiles::before(r), he = r.h0 + r.hc;
-    at = (t < before ? t : t - before + Q4aTiles::after(r)) * Q4A_KEYS + set * 8;
-    want = q4a_first(r.seen + r.hc - at) & ~(q4a_first(he - at) & ~q4a_first(r.h0 - at));
+    at = (t < before ? t : t - before + Q4aTiles::after(r)) * Q4A_KEYS;
+    want = q4a_first(r.seen + r.hc - at) & ~(q4a_first(he - at) & ~q4a_first(r.h0 - at)) & in_page;
+    at += set * 8;
     if (want != 0) page = a.table[b * a.max_pages + (at >> a.shift)];
   }
 };
 
 template <int D, int G, int NT>
-__global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attention_q4(PagedQ4Args a) {
+__global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(PagedQ4Args a) {
   using L = Q4Tile<D, G>;
+  constexpr int WARPS = q4a_warps(NT);
   constexpr int STAGES = q4a_stages(D);
   constexpr int STAGE = Q4A_SETS * L::BYTES;
   constexpr int SUB = Q4A_KEYS / 16;
@@ -144,19 +149,19 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
   constexpr int RING = STAGES * STAGE;
   static_assert(ROWS * ROW * 4 <= RING, "a piece fits the ring");
   extern __shared__ __align__(1024) uint8_t q4a_smem[];
-  __shared__ __align__(8) uint64_t bars[PGA_WARPS][STAGES];
-  __shared__ int4 tile_info[PGA_WARPS][2 * Q4A_BATCH];  // rows seen, request, head tile, whether the pair ends
-  __shared__ int3 meta[PGA_WARPS];
+  __shared__ __align__(8) uint64_t bars[WARPS][STAGES];
+  __shared__ int4 tile_info[WARPS][2 * Q4A_BATCH];  // rows seen, request, head tile, whether the pair ends
+  __shared__ int3 meta[WARPS];
   __shared__ int abort_flag;
-  int* pre = reinterpret_cast<int*>(q4a_smem + PGA_WARPS * RING);
+  int* pre = reinterpret_cast<int*>(q4a_smem + WARPS * RING);
   int* nz = pre + a.B + 1;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) abort_flag = 0;
   if (lane < STAGES) mbar_init(smem_u32(&bars[warp][lane]), 1);
   fence_mbar_init();
   pdl_enter();
-  const PgaPlan plan = pga_begin<Q4aTiles, D>(a, pre, nz);
-  const int me = blockIdx.x * PGA_WARPS + warp;
+  const PgaPlan plan = pga_begin<Q4aTiles, D, WARPS>(a, pre, nz);
+  const int me = blockIdx.x * WARPS + warp;
   // lane 0 seeks the start of this warp's share, lane 1 that of the next one's
   PgaWalk<Q4aTiles> seek;
   const int from = plan.place(me + (lane & 1));
@@ -178,15 +183,19 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
     bool began = t0 > 0;  // the piece's pair began in an earlier share
     const int set = lane & (Q4A_SETS - 1), mine_of = lane / Q4A_SETS;
     Q4aLook look = {b, h, t0, pre[b + 1] - pre[b], n, 0, 0, 0};
+    // sets of a tile in one page, which one copy takes: those of this lane's, and whether it is the first
+    const int in_one = min(1 << a.shift, Q4A_KEYS) / 8;
+    const bool leads = (set & (in_one - 1)) == 0;
+    const uint32_t in_page = (in_one == Q4A_SETS ? 0xffffffffu : (1u << (8 * in_one)) - 1u) << (8 * (set & -in_one));
     look.advance(a, pre, mine_of);
-    look.load(a, set);
+    look.load(a, set, in_page);
     const uint8_t* src = nullptr;
     uint32_t bytes = 0;  // of the tile
     bool there = false;
     auto begin_batch = [&](int which) {
       there = look.want != 0 && look.page >= 0 && look.page < a.num_pages;
       if (look.want != 0 && !there) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
-      uint32_t mask = there ? look.want << (8 * set) : 0u;
+      uint32_t mask = there ? look.want : 0u;
       mask |= __shfl_xor_sync(0xffffffffu, mask, 1);
       mask |= __shfl_xor_sync(0xffffffffu, mask, 2);
       bytes = __popc(__ballot_sync(0xffffffffu, there) >> (lane & ~(Q4A_SETS - 1)) & ((1u << Q4A_SETS) - 1)) * L::BYTES;
@@ -198,7 +207,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
         tile_info[warp][(which & 1) * Q4A_BATCH + mine_of] =
             make_int4(static_cast<int>(mask), look.b, look.h, look.t + 1 == look.tiles);
       look.advance(a, pre, Q4A_BATCH);
-      look.load(a, set);
+      look.load(a, set, in_page);
       __syncwarp();
     };
     auto issue = [&](int tile, int slot) {
@@ -207,7 +216,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
         const uint32_t bar = bar_s + slot * 8;
         if (set == 0) mbar_arrive_expect_tx(bar, bytes);
         __syncwarp(((1u << Q4A_SETS) - 1) << (lane & ~(Q4A_SETS - 1)));
-        if (there) q4a_bulk(ring_s + slot * STAGE + set * L::BYTES, src, L::BYTES, bar);
+        if (there && leads) q4a_bulk(ring_s + slot * STAGE + set * L::BYTES, src, in_one * L::BYTES, bar);
       }
       __syncwarp();
     };
@@ -571,7 +580,7 @@ __global__ void __launch_bounds__(PGA_THREADS, NT == 1 ? 2 : 1) k_paged_attentio
     }
   }
   __syncthreads();
-  pga_join_block<D, NT>(a, plan, meta, q4a_smem, RING);
+  pga_join_block<D, NT, WARPS>(a, plan, meta, q4a_smem, RING);
 }
 
 }  // namespace decomoe
@@ -582,9 +591,9 @@ extern "C" {
 
 size_t decomoe_paged_attention_q4_workspace_bytes(int64_t B, int Hq, int Hkv, int D) {
   if (B <= 0 || Hkv <= 0 || Hq < Hkv || D <= 0) return 0;
-  // the pieces of every warp and of every block, two blocks per SM
+  // the pieces of every warp and of every block, one block per SM
   const size_t rows = static_cast<size_t>(pga_rows(Hq, Hkv)) * pga_row(D) * sizeof(float);
-  return static_cast<size_t>(std::min(2 * sm_count(), Q4A_BLOCKS)) * ((PGA_WARPS + 2) * rows + sizeof(int4));
+  return static_cast<size_t>(std::min(sm_count(), Q4A_BLOCKS)) * ((q4a_warps(pga_rows(Hq, Hkv) / 8) + 2) * rows + sizeof(int4));
 }
 
 int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const void* pages, int64_t num_pages,
@@ -660,19 +669,19 @@ int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const
   a.extra = Q4A_EXTRA;
   const int64_t most = B * ((max_pages * page_size + Q4A_KEYS - 1) / Q4A_KEYS + 1) * a.hv;  // tiles, at most
   DM_ARG_CHECK(most + Q4A_EXTRA * B * a.hv <= INT_MAX, "paged_attention_q4: B * max_pages * page_size * heads is too large");
-  const int per_sm = rows == 8 ? 2 : 1;
+  const int warps = q4a_warps(rows / 8);
   const int grid = static_cast<int>(
-      std::max<int64_t>(1, std::min<int64_t>(std::min(per_sm * sm_count(), Q4A_BLOCKS), (most + PGA_WARPS - 1) / PGA_WARPS)));
+      std::max<int64_t>(1, std::min<int64_t>(std::min(sm_count(), Q4A_BLOCKS), (most + warps - 1) / warps)));
   const size_t piece = static_cast<size_t>(rows) * pga_row(D);
   a.early = static_cast<float*>(ws);
-  a.part = a.early + static_cast<size_t>(grid) * PGA_WARPS * piece;
+  a.part = a.early + static_cast<size_t>(grid) * warps * piece;
   a.info = reinterpret_cast<int4*>(a.part + static_cast<size_t>(grid) * 2 * piece);
-  const size_t smem = static_cast<size_t>(PGA_WARPS) * q4a_stages(D) * Q4A_SETS * q4_tile_bytes(D, group) +
+  const size_t smem = static_cast<size_t>(warps) * q4a_stages(D) * Q4A_SETS * q4_tile_bytes(D, group) +
                       2 * (static_cast<size_t>(B) + 1) * sizeof(int);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   auto go = [&](auto main, auto join) -> int {
     DM_CUDA_CHECK(cudaFuncSetAttribute(main, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    DM_CUDA_CHECK(launch_pdl(main, dim3(grid), dim3(PGA_THREADS), smem, s, a));
+    DM_CUDA_CHECK(launch_pdl(main, dim3(grid), dim3(32 * warps), smem, s, a));
     DM_CUDA_CHECK(launch_pdl(join, dim3(grid), dim3(32 * PGM_WARPS), 0, s, static_cast<const PagedCommon&>(a)));
     return DECOMOE_OK;
   };

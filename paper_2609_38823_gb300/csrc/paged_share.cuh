@@ -1,8 +1,8 @@
 // What the attentions over paged caches share (bf16 pages: paged_attention.cu, 4-bit
 // pages: paged_attention_q4.cu): how the tiles of all requests are numbered and divided
 // among the warps of a launch, and how the pieces of a (request, KV head) pair that the
-// division cuts are joined. A kernel of PGA_WARPS warps keeps for each warp a ring in shared
-// memory, in which the warp's last piece waits once the ring is drained.
+// division cuts are joined. A kernel of W warps keeps for each warp a ring in shared memory,
+// in which the warp's last piece waits once the ring is drained.
 #pragma once
 
 #include <cfloat>
@@ -10,9 +10,6 @@
 #include "decomoe_internal.cuh"
 
 namespace decomoe {
-
-constexpr int PGA_WARPS = 8;
-constexpr int PGA_THREADS = 32 * PGA_WARPS;
 
 // Floats of a partial row: outputs, m, l (bank-conflict-free stores).
 constexpr int pga_row(int D) { return D + 4; }
@@ -94,7 +91,7 @@ __device__ __forceinline__ void pga_mma(float (&c)[4], const uint32_t (&a)[4], u
       : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// The C floats (2 or 4) of a partial row that a lane holds.
+// The C floats (1, 2 or 4) of a partial row that a lane holds.
 template <int C>
 struct PgaVec {
   float v[C];
@@ -104,6 +101,8 @@ __device__ __forceinline__ void pga_load(PgaVec<C>& d, const float* p) {
   if constexpr (C == 4) {
     const float4 u = PAST_L1 ? __ldcg(reinterpret_cast<const float4*>(p)) : *reinterpret_cast<const float4*>(p);
     d.v[0] = u.x, d.v[1] = u.y, d.v[2] = u.z, d.v[3] = u.w;
+  } else if constexpr (C == 1) {
+    d.v[0] = PAST_L1 ? __ldcg(p) : *p;
   } else {
     const float2 u = PAST_L1 ? __ldcg(reinterpret_cast<const float2*>(p)) : *reinterpret_cast<const float2*>(p);
     d.v[0] = u.x, d.v[1] = u.y;
@@ -112,6 +111,7 @@ __device__ __forceinline__ void pga_load(PgaVec<C>& d, const float* p) {
 template <int C>
 __device__ __forceinline__ void pga_store(float* p, const PgaVec<C>& d) {
   if constexpr (C == 4) *reinterpret_cast<float4*>(p) = make_float4(d.v[0], d.v[1], d.v[2], d.v[3]);
+  else if constexpr (C == 1) *p = d.v[0];
   else *reinterpret_cast<float2*>(p) = make_float2(d.v[0], d.v[1]);
 }
 // The result: the outputs over the sum (nothing seen: zeros), as bf16.
@@ -120,6 +120,8 @@ __device__ __forceinline__ void pga_result(__nv_bfloat16* dst, const PgaVec<C>& 
   const float f = l != 0.f ? 1.f / l : 0.f;
   if constexpr (C == 4)
     *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16x2(o.v[0] * f, o.v[1] * f), pack_bf16x2(o.v[2] * f, o.v[3] * f));
+  else if constexpr (C == 1)
+    *dst = __float2bfloat16_rn(o.v[0] * f);
   else
     *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(o.v[0] * f, o.v[1] * f);
 }
@@ -165,13 +167,14 @@ struct PgaWalk {
 // The start of a launch, by every thread of a block: the tiles of every request added up
 // in pre and nz (shared memory, [B + 1] each), zeros for the requests that see nothing, and
 // the division of the tiles among the launch's warps.
-template <class Tiles, int D>
+template <class Tiles, int D, int W>
 __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int* nz) {
-  __shared__ int scan_w[2][PGA_WARPS];
+  constexpr int THREADS = 32 * W;
+  __shared__ int scan_w[2][W];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   // ---- tiles of every request, added up
   {
-    const int per = (a.B + PGA_THREADS - 1) / PGA_THREADS;
+    const int per = (a.B + THREADS - 1) / THREADS;
     const int b0 = min(a.B, tid * per), b1 = min(a.B, b0 + per);
     bool bad = false;
     int sum = 0, some = 0;
@@ -198,7 +201,7 @@ __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int
     __syncthreads();
     int at = inc - sum, an = inn - some;
 #pragma unroll
-    for (int w = 0; w < PGA_WARPS; ++w)
+    for (int w = 0; w < W; ++w)
       if (w < warp) {
         at += scan_w[0][w];
         an += scan_w[1][w];
@@ -216,15 +219,15 @@ __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int
   for (int b = blockIdx.x; b < a.B; b += gridDim.x)
     if (pre[b] == pre[b + 1]) {
       uint4* o = reinterpret_cast<uint4*>(a.out + static_cast<int64_t>(b) * a.hq * D);
-      for (int i = tid; i < a.hq * D / 8; i += PGA_THREADS) o[i] = make_uint4(0, 0, 0, 0);
+      for (int i = tid; i < a.hq * D / 8; i += THREADS) o[i] = make_uint4(0, 0, 0, 0);
     }
   PgaPlan plan;
   plan.pre = pre;
   plan.nz = nz;
   plan.B = a.B;
   plan.hv = a.hv;
-  plan.extra = pre[a.B] * a.hv > static_cast<int>(gridDim.x) * PGA_WARPS ? a.extra : 0;
-  plan.divide(static_cast<int>(gridDim.x) * PGA_WARPS);
+  plan.extra = pre[a.B] * a.hv > static_cast<int>(gridDim.x) * W ? a.extra : 0;
+  plan.divide(static_cast<int>(gridDim.x) * W);
   return plan;
 }
 
@@ -233,45 +236,49 @@ __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int
 // the one in which the pair ends. What began before the block or goes on after it leaves
 // joined. All pieces are loaded ahead of the walk. meta: of each warp, whether its last piece
 // goes on (1: begun in its share, 2: before it), its request and head tile.
-template <int D, int NT>
+template <int D, int NT, int W>
 __device__ __forceinline__ void pga_join_block(const PagedCommon& a, const PgaPlan& plan, const int3* meta,
                                                const uint8_t* rings, int ring_bytes) {
   constexpr int ROWS = 8 * NT, ROW = pga_row(D);
+  constexpr int SHARERS = W > ROWS ? W / ROWS : 1;  // warps that share a row's features
+  constexpr bool AHEAD = W <= 8;  // with more warps only what comes from outside the block is loaded ahead
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int gs = a.hq / a.hkv;
   float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * ROWS * ROW;
-  constexpr int C = D / 32;
-  int kind[PGA_WARPS];  // of a warp's last piece: 0 ends there, 1 begun in its share and goes on, 2 its whole share
+  constexpr int C = D / 32 / SHARERS;
+  const int at = warp / ROWS * (D / SHARERS) + lane * C;
+  int kind[W];  // of a warp's last piece: 0 ends there, 1 begun in its share and goes on, 2 its whole share
 #pragma unroll
-  for (int w = 0; w < PGA_WARPS; ++w) kind[w] = meta[w].x;
+  for (int w = 0; w < W; ++w) kind[w] = meta[w].x;
 #pragma unroll 1
-  for (int r = warp; r < ROWS; r += PGA_WARPS) {
-    PgaVec<C> last[PGA_WARPS], early[PGA_WARPS];
-    float2 last_ml[PGA_WARPS], early_ml[PGA_WARPS];
+  for (int r = SHARERS > 1 ? warp % ROWS : warp; r < ROWS; r += W) {
+    PgaVec<C> last[W], early[W];
+    float2 last_ml[W], early_ml[W];
+    auto load_last = [&](int w) {
+      const float* p = reinterpret_cast<const float*>(rings + w * ring_bytes) + r * ROW;
+      last_ml[w] = *reinterpret_cast<const float2*>(p + D);
+      pga_load<false>(last[w], p + at);
+    };
 #pragma unroll
-    for (int w = 0; w < PGA_WARPS; ++w) {
-      if (kind[w] != 0) {
-        const float* p = reinterpret_cast<const float*>(rings + w * ring_bytes) + r * ROW;
-        last_ml[w] = *reinterpret_cast<const float2*>(p + D);
-        pga_load<false>(last[w], p + lane * C);
-      }
+    for (int w = 0; w < W; ++w) {
+      if (AHEAD && kind[w] != 0) load_last(w);
       if (w > 0 && kind[w - 1] != 0 && kind[w] != 2) {
-        const float* p = a.early + (static_cast<int64_t>(blockIdx.x * PGA_WARPS + w) * ROWS + r) * ROW;
+        const float* p = a.early + (static_cast<int64_t>(blockIdx.x * W + w) * ROWS + r) * ROW;
         early_ml[w] = *reinterpret_cast<const float2*>(p + D);
-        pga_load<false>(early[w], p + lane * C);
+        pga_load<false>(early[w], p + at);
       }
     }
     if (tid == 0) {
       // a pair that begins here and ends in a later block
       int4 info = make_int4(0, 0, 0, 0);
-      if (kind[PGA_WARPS - 1] != 0) {
-        int w0 = PGA_WARPS - 1;
+      if (kind[W - 1] != 0) {
+        int w0 = W - 1;
         while (w0 > 0 && kind[w0] == 2) --w0;
         if (meta[w0].x == 1) {
           info = make_int4(1, meta[w0].y, meta[w0].z, 0);
           const int tiles = plan.pre[info.y + 1] - plan.pre[info.y];
           const int end = plan.places(info.y) + (info.z + 1) * (tiles + plan.extra) - 1;
-          info.w = plan.holder(end) / PGA_WARPS;
+          info.w = plan.holder(end) / W;
         }
       }
       a.info[blockIdx.x] = info;
@@ -290,16 +297,17 @@ __device__ __forceinline__ void pga_join_block(const PagedCommon& a, const PgaPl
     auto leave = [&](bool open_begin, bool open_end) {
       if (open_begin || open_end) {
         float* dst = part + ((open_begin ? 0 : ROWS) + r) * ROW;
-        pga_store(dst + lane * C, o);
-        if (lane == 0) *reinterpret_cast<float2*>(dst + D) = make_float2(m, l);
+        pga_store(dst + at, o);
+        if (at == 0) *reinterpret_cast<float2*>(dst + D) = make_float2(m, l);
       } else {
         const int b = meta[w0].y, h = meta[w0].z, g = a.qt == 1 ? h : h / a.qt, q = (h - g * a.qt) * ROWS + r;
-        if (q < gs) pga_result(a.out + (static_cast<int64_t>(b) * a.hq + g * gs + q) * D + lane * C, o, l);
+        if (q < gs) pga_result(a.out + (static_cast<int64_t>(b) * a.hq + g * gs + q) * D + at, o, l);
       }
     };
     bool on = false;  // a chain goes on into warp w
 #pragma unroll
-    for (int w = 0; w < PGA_WARPS; ++w) {
+    for (int w = 0; w < W; ++w) {
+      if (!AHEAD && kind[w] != 0) load_last(w);
       if (on) {
         if (kind[w] == 2) {
           add(last_ml[w], last[w]);
