@@ -7,25 +7,28 @@
 
 namespace decomoe {
 
-// A row's vocabulary is read once, in vectors of 16 bytes, by a cluster of S blocks (S = 1
-// for many rows). A thread keeps, of its elements x, their maximum m and, with
-// d = (x - m) scale log2(e), the sums of 2^d and of 2^d d, both rescaled where the maximum
-// grows; the block's and then the cluster's follow in a fixed order. With the row's M, Z and
-// W = sum 2^d d: log p(x) = (x - M) scale - ln Z, entropy = ln Z - ln 2 W / Z.
+// With c = scale log2(e) and m the maximum of the elements x seen so far, a thread keeps the
+// sums z of 2^d and w of 2^d d over d = (x - m) c, rescaled where m grows (pairs of elements in
+// packed fp32 operations); threads, warps and blocks are added up in a fixed order against the
+// largest m. Then ln p(x) = (x - m) scale - ln z and the entropy is ln z - ln 2 w / z. Elements count as -2^100 at least, so that
+// masked ones (-inf, or a type's lowest value) need no case of their own: their 2^d is 0 and their
+// product with d finite. A row whose maximum is not below 2^97 in size (all masked, infinite,
+// enormous) is computed again with every case, by one warp.
 //
-// The n <= 32 best: of the threads' maxima (disjoint elements) the n-th largest is at most
-// the n-th largest element, so only elements from it on can be among the n; the few threads
-// that have one read their elements again and collect them, and the collected are ranked by
-// counting. Elements are compared as 64-bit keys of value and index, all different, so ties
-// go to the lowest index and no order of execution shows. Where more are collected than
-// there is room for (a row of equal values in an unlucky order), n rounds over the slice
-// take one each.
+// The n <= 32 best: the threads fall into 64 groups or more, and the n-th largest of the groups'
+// maxima bounds the n-th largest element from below, since groups have no element in common; about n to
+// 1.5 n elements reach it. The vectors of the few threads whose maxima do are read again, elements that reach it collected as 64-bit keys of value and index, all
+// different, and ranked by counting; ties go to the lowest index, and no order of execution
+// shows. Where more are collected than there is room for (rows of equal values), a warp reads the row
+// again and keeps the n best sorted in its lanes.
 constexpr int LP_THREADS = 256;
 constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_BEST = 32;
-constexpr int LP_ROOM = 1024;  // collected elements of a block
+constexpr int LP_ROOM = 512;  // collected elements of a block, or of a row
 constexpr int LP_CLUSTER = 16;
 constexpr float LP_LN2 = 0.6931471805599453f;
+constexpr float LP_LEAST = -0x1p100f;  // what elements count as at least
+constexpr float LP_PLAIN = 0x1p97f;    // rows with a maximum below this in size are in the plain range
 
 struct LpArgs {
   const void* x;
@@ -37,30 +40,171 @@ struct LpArgs {
   float scale, c;  // scale, scale * log2(e)
 };
 
-struct LpSums {
-  float m, z, w;
-};
+// ---------------------------------------------------------------- arithmetic
 
 __device__ __forceinline__ float lp_ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// The sums of a against the maximum to >= a.m; nothing (m = -inf) has none.
-__device__ __forceinline__ void lp_raise(LpSums& a, float to, float c) {
-  const float delta = a.m == to ? 0.f : fmaxf((a.m - to) * c, -1000.f);
-  const float f = lp_ex2(delta);
-  a.w = (a.w + a.z * delta) * f;
-  a.z *= f;
-  a.m = to;
+__device__ __forceinline__ uint64_t lp_pair(float lo, float hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+  return r;
 }
-__device__ __forceinline__ void lp_join(LpSums& a, LpSums b, float c) {
-  const float to = fmaxf(a.m, b.m);
-  lp_raise(a, to, c);
-  lp_raise(b, to, c);
-  a.z += b.z;
-  a.w += b.w;
+__device__ __forceinline__ float2 lp_split(uint64_t v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
 }
+__device__ __forceinline__ uint64_t lp_fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t lp_mul2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t lp_add2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ float lp_max_nan(float a, float b) {  // NaN where one is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// What a vector of 16 bytes holds: its elements, raised to LP_LEAST, as pairs; their largest;
+// and the elements as they are.
+template <typename E>
+struct LpVec;
+template <>
+struct LpVec<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+  static __device__ __forceinline__ uint4 raise(const uint4& u) {
+    uint4 r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r.x) : "r"(u.x), "r"(0xf180f180u));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r.y) : "r"(u.y), "r"(0xf180f180u));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r.z) : "r"(u.z), "r"(0xf180f180u));
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r.w) : "r"(u.w), "r"(0xf180f180u));
+    return r;
+  }
+  static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+  }
+  static __device__ __forceinline__ float largest(const uint4& u) {
+    const uint32_t m = max2(max2(u.x, u.y), max2(u.z, u.w));
+    return fmaxf(bf16_lo(m), bf16_hi(m));
+  }
+  static __device__ __forceinline__ uint64_t pair(const uint4& u, int i) {
+    return lp_pair(bf16_lo(word(u, i)), bf16_hi(word(u, i)));
+  }
+  static __device__ __forceinline__ float element(const uint4& u, int j) {
+    return j & 1 ? bf16_hi(word(u, j / 2)) : bf16_lo(word(u, j / 2));
+  }
+  static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+};
+template <>
+struct LpVec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ float element(const uint4& u, int j) {
+    return __uint_as_float(j == 0 ? u.x : j == 1 ? u.y : j == 2 ? u.z : u.w);
+  }
+  static __device__ __forceinline__ uint4 raise(const uint4& u) {
+    auto up = [](uint32_t v) { return __float_as_uint(lp_max_nan(__uint_as_float(v), LP_LEAST)); };
+    return make_uint4(up(u.x), up(u.y), up(u.z), up(u.w));
+  }
+  static __device__ __forceinline__ float largest(const uint4& u) {
+    return fmaxf(fmaxf(element(u, 0), element(u, 1)), fmaxf(element(u, 2), element(u, 3)));
+  }
+  static __device__ __forceinline__ uint64_t pair(const uint4& u, int i) {
+    return i == 0 ? lp_pair(element(u, 0), element(u, 1)) : lp_pair(element(u, 2), element(u, 3));
+  }
+  static __device__ __forceinline__ float one(const float* p) { return *p; }
+};
+
+// A thread's sums; m starts at LP_LEAST.
+struct LpAcc {
+  float m;
+  uint64_t z, w;  // pairs of partial sums
+  __device__ __forceinline__ void clear() {
+    m = LP_LEAST;
+    z = w = 0;
+  }
+  __device__ __forceinline__ void grow(float to, float c) {
+    const float d = fmaxf((m - to) * c, -1000.f), f = lp_ex2(d);
+    const uint64_t ff = lp_pair(f, f);
+    w = lp_mul2(lp_fma2(z, lp_pair(d, d), w), ff);
+    z = lp_mul2(z, ff);
+    m = to;
+  }
+  // U vectors
+  template <typename E, int U>
+  __device__ __forceinline__ void take(const uint4 (&u)[U], float c) {
+    using Vec = LpVec<E>;
+    uint4 x[U];
+    float most = LP_LEAST;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      x[i] = Vec::raise(u[i]);
+      most = fmaxf(most, Vec::largest(x[i]));
+    }
+    if (most > m) grow(most, c);
+    const uint64_t cc = lp_pair(c, c), mm = lp_pair(-m, -m);
+#pragma unroll
+    for (int i = 0; i < U; ++i)
+#pragma unroll
+      for (int j = 0; j < Vec::N / 2; ++j) {
+        const uint64_t d = lp_mul2(lp_add2(Vec::pair(x[i], j), mm), cc);
+        const float2 s = lp_split(d);
+        const uint64_t e = lp_pair(lp_ex2(s.x), lp_ex2(s.y));
+        z = lp_add2(z, e);
+        w = lp_fma2(e, d, w);
+      }
+  }
+  __device__ __forceinline__ void one(float v, float c) {
+    v = lp_max_nan(v, LP_LEAST);
+    if (v > m) grow(v, c);
+    const float d = (v - m) * c, e = lp_ex2(d);
+    z = lp_add2(z, lp_pair(e, 0.f));
+    w = lp_fma2(lp_pair(e, 0.f), lp_pair(d, 0.f), w);
+  }
+};
+
+struct LpSums {
+  float m, z, w;
+};
+// The sums of the L lanes of each L (a power of two), in every one of them.
+template <int L>
+__device__ __forceinline__ LpSums lp_reduce(LpSums s, float c) {
+  float m = s.m;
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float d = fmaxf((s.m - m) * c, -1000.f), f = lp_ex2(d);
+  s.w = (s.w + s.z * d) * f;
+  s.z *= f;
+#pragma unroll
+  for (int o = L / 2; o > 0; o >>= 1) {
+    s.z += __shfl_xor_sync(0xffffffffu, s.z, o);
+    s.w += __shfl_xor_sync(0xffffffffu, s.w, o);
+  }
+  s.m = m;
+  return s;
+}
+__device__ __forceinline__ LpSums lp_sums(const LpAcc& a) {
+  const float2 z = lp_split(a.z), w = lp_split(a.w);
+  return {a.m, z.x + z.y, w.x + w.y};
+}
+
+// ---------------------------------------------------------------- the best
+
 // Larger values first, then lower indexes: a key of every element, 0 for none. NaN ranks as
 // minus infinity, -0 as 0.
 __device__ __forceinline__ uint64_t lp_key(float x, uint32_t i) {
@@ -74,27 +218,266 @@ __device__ __forceinline__ float lp_key_value(uint64_t k) {
 }
 __device__ __forceinline__ uint32_t lp_key_index(uint64_t k) { return 0xffffffffu - static_cast<uint32_t>(k); }
 
+// A row, or a slice of it: vectors [v0, v0 + vecs) of its whole 16-byte vectors, and (the first
+// slice) up to 2 N - 2 elements around those.
 template <typename E>
-struct LpVec;
-template <>
-struct LpVec<__nv_bfloat16> {
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void split(const uint4& u, float (&x)[8]) {
-    x[0] = bf16_lo(u.x), x[1] = bf16_hi(u.x), x[2] = bf16_lo(u.y), x[3] = bf16_hi(u.y);
-    x[4] = bf16_lo(u.z), x[5] = bf16_hi(u.z), x[6] = bf16_lo(u.w), x[7] = bf16_hi(u.w);
+struct LpRow {
+  const E* x;
+  const uint4* xv;
+  int head, vecs, v0, edges, rest_at;
+  __device__ __forceinline__ LpRow(const LpArgs& a, int64_t row, int rank, int S) {
+    constexpr int N = LpVec<E>::N;
+    x = static_cast<const E*>(a.x) + row * a.ld;
+    head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / static_cast<int>(sizeof(E)));
+    const int all = (a.V - head) / N, rest = a.V - head - all * N;
+    v0 = static_cast<int>(static_cast<int64_t>(all) * rank / S);
+    vecs = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / S) - v0;
+    xv = reinterpret_cast<const uint4*>(x + head) + v0;
+    edges = rank == 0 ? head + rest : 0;
+    rest_at = a.V - rest;
   }
-  static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-};
-template <>
-struct LpVec<float> {
-  static constexpr int N = 4;
-  static __device__ __forceinline__ void split(const uint4& u, float (&x)[4]) {
-    x[0] = __uint_as_float(u.x), x[1] = __uint_as_float(u.y), x[2] = __uint_as_float(u.z), x[3] = __uint_as_float(u.w);
-  }
-  static __device__ __forceinline__ float one(const float* p) { return *p; }
+  __device__ __forceinline__ int edge_at(int i) const { return i < head ? i : rest_at + (i - head); }
+  __device__ __forceinline__ int index(int v) const { return head + (v0 + v) * LpVec<E>::N; }  // of a vector's first element
 };
 
-__device__ __forceinline__ uint32_t lp_rank() {
+// The keys (count[0] of them) with a value of `from` or more among a row's vectors v = t, t + stride, ...
+// of each thread t whose maximum is as large (mine; t = first + lane), by a warp: the vectors
+// of all such threads are spread over its lanes, so that one latency covers most rows. get(v)
+// reads one; who: 32 ints of the warp's own.
+template <typename E, class Get>
+__device__ __forceinline__ void lp_collect(const LpRow<E>& row, Get get, float from, float mine, int first, int stride,
+                                           uint64_t* keys, int* count, int* who) {
+  const int lane = threadIdx.x & 31;
+  auto push = [&](float y, int i) {
+    const int at = atomicAdd(count, 1);
+    if (at < LP_ROOM) keys[at] = lp_key(y, i);
+  };
+  const bool mine_too = mine >= from;
+  const uint32_t some = __ballot_sync(0xffffffffu, mine_too);
+  if (mine_too) who[__popc(some & ((1u << lane) - 1u))] = first + lane;
+  __syncwarp();
+  const unsigned each = static_cast<unsigned>(row.vecs + stride - 1) / static_cast<unsigned>(stride);
+  const unsigned all = __popc(some) * each;
+  for (unsigned i = lane; i < all; i += 32) {
+    const unsigned q = i / each;
+    const int v = who[q] + stride * static_cast<int>(i - q * each);
+    if (v >= row.vecs) continue;
+    const uint4 u = get(v);
+    if (LpVec<E>::largest(u) >= from) {
+#pragma unroll
+      for (int j = 0; j < LpVec<E>::N; ++j) {
+        const float y = LpVec<E>::element(u, j);
+        if (y >= from) push(y, row.index(v) + j);
+      }
+    }
+  }
+  if (first + lane < row.edges) {
+    const float y = LpVec<E>::one(row.x + row.edge_at(first + lane));
+    if (y >= from) push(y, row.edge_at(first + lane));
+  }
+  __syncwarp();
+}
+
+// The n best of a row read once more by a warp, sorted, key i in lane i (0: none): exact
+// whatever the row holds.
+template <typename E>
+__device__ __noinline__ uint64_t lp_sorted(LpRow<E> row, int n) {
+  const int lane = threadIdx.x & 31;
+  uint64_t list = 0, least = 0;  // least: the n-th
+  auto offer = [&](uint64_t k) {
+    uint32_t todo = __ballot_sync(0xffffffffu, k > least);
+    while (todo != 0) {
+      const uint64_t key = __shfl_sync(0xffffffffu, k, __ffs(todo) - 1);
+      const int at = __popc(__ballot_sync(0xffffffffu, list > key));
+      const uint64_t up = __shfl_up_sync(0xffffffffu, list, 1);
+      list = lane < at ? list : lane == at ? key : up;
+      least = __shfl_sync(0xffffffffu, list, n - 1);
+      todo &= todo - 1;
+      todo &= __ballot_sync(0xffffffffu, k > least);
+    }
+  };
+  offer(lane < row.edges ? lp_key(LpVec<E>::one(row.x + row.edge_at(lane)), row.edge_at(lane)) : 0);
+  for (int v = 0; v < row.vecs; v += 32) {
+    const bool have = v + lane < row.vecs;
+    const uint4 u = have ? __ldg(row.xv + v + lane) : make_uint4(0, 0, 0, 0);
+    for (int j = 0; j < LpVec<E>::N; ++j) {
+      float y = 0.f;
+#pragma unroll
+      for (int i = 0; i < LpVec<E>::N; ++i) y = i == j ? LpVec<E>::element(u, i) : y;
+      offer(have ? lp_key(y, row.index(v + lane) + j) : 0);
+    }
+  }
+  return list;
+}
+
+// The n best of `count` collected keys (zeros are none), key i in lane i, by a warp. Those behind the last
+// are the row's first elements of minus infinity or NaN, which are not collected.
+template <typename E>
+__device__ __forceinline__ uint64_t lp_rank(const uint64_t* keys, int count, int n, uint64_t* best) {
+  const int lane = threadIdx.x & 31;
+  if (lane < n) best[lane] = 0;
+  __syncwarp();
+  for (int i = lane; i < count; i += 32) {
+    const uint64_t k = keys[i];
+    int above = 0;
+#pragma unroll 4
+    for (int j = 0; j < count; ++j) above += keys[j] > k;
+    if (above < n && k != 0) best[above] = k;
+  }
+  __syncwarp();
+  return lane < n ? best[lane] : 0;
+}
+template <typename E>
+__device__ __noinline__ uint64_t lp_fill(const E* x, int V, int n, uint64_t list) {
+  const int lane = threadIdx.x & 31;
+  int have = __popc(__ballot_sync(0xffffffffu, lane < n && list != 0));
+  for (int i = 0; i < V && have < n; i += 32) {
+    const uint32_t gone = __ballot_sync(0xffffffffu, i + lane < V && !(LpVec<E>::one(x + min(i + lane, V - 1)) >= -FLT_MAX));
+    const uint32_t left = gone;
+    for (uint32_t todo = left; todo != 0 && have < n; todo &= todo - 1, ++have)
+      if (lane == have) list = lp_key(-INFINITY, i + __ffs(todo) - 1);
+  }
+  return list;
+}
+
+// Ordered as the floats are, none of them NaN; 0 is below all.
+__device__ __forceinline__ uint32_t lp_order(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+// The n-th largest of `count` (a multiple of 4) values is the largest that n of them reach: this thread's
+// value where that holds, raised to the warp's largest such (0: none).
+__device__ __forceinline__ uint32_t lp_nth(const float* values, int count, int n, float mine) {
+  int reach = 0;
+  const float4* v = reinterpret_cast<const float4*>(values);
+#pragma unroll 4
+  for (int i = 0; i < count / 4; ++i) {
+    const float4 u = v[i];
+    reach += (u.x >= mine) + (u.y >= mine) + (u.z >= mine) + (u.w >= mine);
+  }
+  return __reduce_max_sync(0xffffffffu, reach >= n ? lp_order(mine) : 0u);
+}
+// The least value to collect: the bound, or everything finite where some groups hold nothing plain.
+__device__ __forceinline__ float lp_from(uint32_t nth) {
+  const float t = __uint_as_float(nth & 0x80000000u ? nth & 0x7fffffffu : ~nth);
+  return nth != 0 && t > LP_LEAST ? t : -FLT_MAX;
+}
+
+// ---------------------------------------------------------------- results
+
+// A row in every case, by one warp: infinities, NaN, nothing but masks, maxima of any size.
+template <typename E>
+__device__ __noinline__ LpSums lp_any_case(const E* x, int V, float c) {
+  const int lane = threadIdx.x & 31;
+  float m = -INFINITY;
+  for (int i = lane; i < V; i += 32) m = fmaxf(m, LpVec<E>::one(x + i));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  float z = 0.f, w = 0.f;
+  for (int i = lane; i < V; i += 32) {
+    const float d = (LpVec<E>::one(x + i) - (m == -INFINITY ? 0.f : m)) * c, e = lp_ex2(d);
+    z += e;
+    w = fmaf(e, fmaxf(d, -1000.f), w);
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    z += __shfl_xor_sync(0xffffffffu, z, o);
+    w += __shfl_xor_sync(0xffffffffu, w, o);
+  }
+  return {m, z, w};
+}
+
+// A row's results, by a warp: s in every lane, the keys of the best in `list`.
+template <typename E>
+__device__ __forceinline__ void lp_results(const LpArgs& a, int64_t row, const E* x, int token, float logit, LpSums s,
+                                           uint64_t list) {
+  const int lane = threadIdx.x & 31;
+  const bool plain = fabsf(s.m) < LP_PLAIN && a.c < 0x1p20f && a.c > 0x1p-80f;
+  if (!plain) s = lp_any_case<E>(x, a.V, a.c);
+  const float lnz = logf(s.z);
+  auto logprob = [&](float y) {
+    // no probability anywhere (all logits minus infinity): -inf, and an entropy of 0
+    return s.z == 0.f ? -INFINITY : (y - s.m) * a.scale - lnz;
+  };
+  if (lane == 0) {
+    if (a.logprob != nullptr) a.logprob[row] = logprob(logit);
+    if (a.entropy != nullptr) a.entropy[row] = s.z == 0.f ? 0.f : lnz - LP_LN2 * (s.w / s.z);
+  }
+  if (a.n > 0) {
+    if (__any_sync(0xffffffffu, lane < a.n && list == 0)) list = lp_fill<E>(x, a.V, a.n, list);
+    if (lane < a.n) {
+      if (a.top_id != nullptr) a.top_id[row * a.n + lane] = static_cast<int32_t>(lp_key_index(list));
+      if (a.top_logprob != nullptr) a.top_logprob[row * a.n + lane] = logprob(lp_key_value(list));
+    }
+  }
+}
+
+__device__ __forceinline__ bool lp_wanted(const LpArgs& a, int token) { return token >= 0 && token < a.V; }
+
+// ---------------------------------------------------------------- short rows: a warp each
+
+template <typename E>
+__global__ void __launch_bounds__(LP_THREADS) k_logprobs_warp(LpArgs a) {
+  __shared__ uint64_t keys[LP_WARPS][LP_ROOM];
+  __shared__ uint64_t best[LP_WARPS][LP_BEST];
+  __shared__ int count[LP_WARPS], who[LP_WARPS][32];
+  __shared__ __align__(16) float maxima[LP_WARPS][64];
+  constexpr int U = 4;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_enter();
+  const int64_t r = static_cast<int64_t>(blockIdx.x) * LP_WARPS + warp;
+  if (r >= a.T) return;
+  const int token = a.tokens != nullptr ? a.tokens[r] : 0;
+  if (!lp_wanted(a, token)) {
+    if (token >= a.V && lane == 0) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
+    return;
+  }
+  const LpRow<E> row(a, r, 0, 1);
+  const float logit = LpVec<E>::one(row.x + token);
+  const float edge = lane < row.edges ? LpVec<E>::one(row.x + row.edge_at(lane)) : 0.f;
+  LpAcc acc;
+  acc.clear();
+  float first = LP_LEAST, other = LP_LEAST;  // maxima of even and odd vectors of the lane, the edge among the latter
+  int v = lane;
+  for (; v + (U - 1) * 32 < row.vecs; v += U * 32) {
+    uint4 u[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) u[i] = __ldg(row.xv + v + 32 * i);
+    acc.take<E, U>(u, a.c);
+    if (a.n > 0) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) (i & 1 ? other : first) = fmaxf(i & 1 ? other : first, LpVec<E>::largest(u[i]));
+    }
+  }
+  for (int i = 0; v < row.vecs; v += 32, ++i) {
+    const uint4 u[1] = {__ldg(row.xv + v)};
+    acc.take<E, 1>(u, a.c);
+    (i & 1 ? other : first) = fmaxf(i & 1 ? other : first, LpVec<E>::largest(u[0]));
+  }
+  if (lane < row.edges) {
+    acc.one(edge, a.c);
+    other = fmaxf(other, edge);
+  }
+  uint64_t list = 0;
+  if (a.n > 0) {
+    // two groups a lane: the maxima of the vectors of one parity, and of the others (and of the edge)
+    maxima[warp][lane] = first;
+    maxima[warp][lane + 32] = other;
+    __syncwarp();
+    const uint32_t t = max(lp_nth(maxima[warp], 64, a.n, first), lp_nth(maxima[warp], 64, a.n, other));
+    if (lane == 0) count[warp] = 0;
+    __syncwarp();
+    lp_collect<E>(row, [&](int i) { return __ldg(row.xv + i); }, lp_from(t), acc.m, 0, 32, keys[warp],
+                  &count[warp], who[warp]);
+    __syncwarp();
+    list = count[warp] <= LP_ROOM ? lp_rank<E>(keys[warp], count[warp], a.n, best[warp]) : lp_sorted<E>(row, a.n);
+  }
+  lp_results<E>(a, r, row.x, token, logit, lp_reduce<32>(lp_sums(acc), a.c), list);
+}
+
+// ---------------------------------------------------------------- few long rows: a cluster each
+
+__device__ __forceinline__ uint32_t lp_cluster_rank() {
   uint32_t r;
   asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
   return r;
@@ -104,264 +487,130 @@ __device__ __forceinline__ uint32_t lp_at_leader(uint32_t addr) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
   return r;
 }
+__device__ __forceinline__ void lp_store_at(uint32_t addr, int rank, float v) {
+  asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.f32 [a], %2;\n\t}" ::"r"(addr), "r"(rank),
+               "f"(v)
+               : "memory");
+}
 __device__ __forceinline__ void lp_store_leader(uint32_t addr, uint64_t v) {
   asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
 __device__ __forceinline__ void lp_cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void lp_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-// The n best of count keys (all different but for zeros, which are none), best first,
-// zeros after the last: by every thread of the block.
-__device__ __forceinline__ void lp_best(const uint64_t* keys, int count, int n, uint64_t* best) {
-  if (threadIdx.x < n) best[threadIdx.x] = 0;
-  __syncthreads();
-  for (int i = threadIdx.x; i < count; i += LP_THREADS) {
-    const uint64_t k = keys[i];
-    if (k == 0) continue;
-    int rank = 0;
-    for (int j = 0; j < count; ++j) rank += keys[j] > k;
-    if (rank < n) best[rank] = k;
-  }
-  __syncthreads();
-}
-
-template <typename E>
-__global__ void __launch_bounds__(LP_THREADS) k_token_logprobs(LpArgs a, int S) {
-  using Vec = LpVec<E>;
-  constexpr int N = Vec::N, AHEAD = 4;
+template <typename E, int W>
+__global__ void __launch_bounds__(32 * W) k_logprobs_cluster(LpArgs a, int S) {
+  constexpr int U = 4, THREADS = 32 * W;
   __shared__ uint64_t keys[LP_ROOM];
-  __shared__ uint64_t lists[LP_WARPS][LP_BEST];
   __shared__ uint64_t from_ranks[LP_CLUSTER * LP_BEST];
   __shared__ uint64_t best[LP_BEST];
-  __shared__ LpSums warp_sums[LP_WARPS];
-  __shared__ uint64_t rank_mz[LP_CLUSTER], rank_w[LP_CLUSTER];
-  __shared__ uint64_t from_key;
-  __shared__ int collected;
+  __shared__ LpSums warp_sums[W];
+  __shared__ __align__(16) float mine_max[64], maxima[8 * LP_CLUSTER];  // of the block's groups, and of all
+  __shared__ uint32_t nth;
+  __shared__ uint64_t rank_m[LP_CLUSTER], rank_zw[LP_CLUSTER];
+  __shared__ int collected, who[W][32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int rank = S > 1 ? static_cast<int>(lp_rank()) : 0;
+  const int rank = S > 1 ? static_cast<int>(lp_cluster_rank()) : 0;
   pdl_enter();
   if (S > 1) lp_cluster_arrive();  // waited for before another block's shared memory is written
-  const int64_t row = blockIdx.x / S;
-  const int token = a.tokens != nullptr ? a.tokens[row] : 0;
-  if (token < 0 || token >= a.V) {  // padding: every block of the cluster leaves
+  const int64_t r = blockIdx.x / S;
+  const int token = a.tokens != nullptr ? a.tokens[r] : 0;
+  if (!lp_wanted(a, token)) {  // every block of the cluster leaves
     if (token >= a.V && rank == 0 && tid == 0) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
+    __syncwarp();
     if (S > 1) lp_cluster_wait();
     return;
   }
-  const E* x = static_cast<const E*>(a.x) + row * a.ld;
-  // whole vectors from the first 16-byte boundary on; what lies around them is read by the first
-  // threads of the first block
-  const int head = min(a.V, static_cast<int>((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / static_cast<int>(sizeof(E)));
-  const int vecs = (a.V - head) / N, rest = a.V - head - vecs * N;
-  const int v0 = static_cast<int>(static_cast<int64_t>(vecs) * rank / S);
-  const int v1 = static_cast<int>(static_cast<int64_t>(vecs) * (rank + 1) / S);
-  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
-  const bool edge = rank == 0 && tid < head + rest;
-  const int edge_at = tid < head ? tid : a.V - rest + (tid - head);
-
-  // ---- one pass
-  LpSums s = {-INFINITY, 0.f, 0.f};
-  int best_v = -1;  // the first vector that holds this thread's maximum; -1: the edge element
-  if (edge) {
-    const float e = Vec::one(x + edge_at);
-    s.m = fmaxf(e, -INFINITY);  // (NaN: its sums will say so)
-    const float d = (e - (s.m == -INFINITY ? 0.f : s.m)) * a.c;
-    s.z = lp_ex2(d);
-    s.w = s.z * fmaxf(d, -1000.f);
+  const LpRow<E> row(a, r, rank, S);
+  const float edge = tid < row.edges ? LpVec<E>::one(row.x + row.edge_at(tid)) : 0.f;
+  const float logit = rank == 0 && warp == 0 ? LpVec<E>::one(row.x + token) : 0.f;
+  LpAcc acc;
+  acc.clear();
+  int v = tid;
+  for (; v + (U - 1) * THREADS < row.vecs; v += U * THREADS) {
+    uint4 u[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) u[i] = __ldg(row.xv + v + i * THREADS);
+    acc.take<E, U>(u, a.c);
   }
-  auto take = [&](const uint4& u, int v) {
-    float y[N];
-    Vec::split(u, y);
-    float most = y[0];
+  if (v < row.vecs) {  // what is left, its loads in flight together
+    uint4 u[U - 1];
 #pragma unroll
-    for (int j = 1; j < N; ++j) most = fmaxf(most, y[j]);
-    if (most > s.m) {
-      lp_raise(s, most, a.c);
-      best_v = v;
-    }
-    const float ref = s.m == -INFINITY ? 0.f : s.m;
+    for (int i = 0; i < U - 1; ++i)
+      if (v + i * THREADS < row.vecs) u[i] = __ldg(row.xv + v + i * THREADS);
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float d = (y[j] - ref) * a.c, e = lp_ex2(d);
-      s.z += e;
-      s.w = fmaf(e, fmaxf(d, -1000.f), s.w);
-    }
-  };
-  int v = v0 + tid;
-  for (; v + (AHEAD - 1) * LP_THREADS < v1; v += AHEAD * LP_THREADS) {
-    uint4 u[AHEAD];
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) u[i] = __ldg(xv + v + i * LP_THREADS);
-#pragma unroll
-    for (int i = 0; i < AHEAD; ++i) take(u[i], v + i * LP_THREADS);
+    for (int i = 0; i < U - 1; ++i)
+      if (v + i * THREADS < row.vecs) {
+        const uint4 w[1] = {u[i]};
+        acc.take<E, 1>(w, a.c);
+      }
   }
-  for (; v < v1; v += LP_THREADS) take(__ldg(xv + v), v);
-  const bool any = edge || v0 + tid < v1;
-  const float mine = s.m;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    LpSums b = {__shfl_down_sync(0xffffffffu, s.m, o), __shfl_down_sync(0xffffffffu, s.z, o),
-                __shfl_down_sync(0xffffffffu, s.w, o)};
-    lp_join(s, b, a.c);
-  }
+  if (tid < row.edges) acc.one(edge, a.c);
+  LpSums s = lp_reduce<32>(lp_sums(acc), a.c);
   if (lane == 0) warp_sums[warp] = s;
-
-  // ---- the best
+  // groups of THREADS S / 64 lanes, a warp at most: `groups` in the block, 64 to 128 in all
+  const int lanes = min(THREADS / 64 * S, 32), groups = THREADS / lanes;
   if (a.n > 0) {
-    // an element of this thread that holds its maximum
-    uint64_t k = 0;
-    auto scan = [&](auto f) {  // f(value, index) over this thread's elements
-      if (edge) f(Vec::one(x + edge_at), edge_at);
-      for (int i = v0 + tid; i < v1; i += LP_THREADS) {
-        float y[N];
-        Vec::split(__ldg(xv + i), y);
-#pragma unroll
-        for (int j = 0; j < N; ++j) f(y[j], head + i * N + j);
-      }
-    };
-    // no element of this thread has a larger key than the value's with index 0
-    const uint64_t reach = any ? lp_key(mine, 0) : 0;
-    if (any) {
-      if (best_v >= 0) {
-        float y[N];
-        Vec::split(__ldg(xv + best_v), y);
-#pragma unroll
-        for (int j = N - 1; j >= 0; --j)
-          if (y[j] == mine) k = lp_key(y[j], head + best_v * N + j);
-      } else if (edge) {
-        k = lp_key(mine, edge_at);
-      } else {
-        k = lp_key(-INFINITY, head + (v0 + tid) * N);
-      }
-    }
-    // the warp's 32 in order, best first
-    uint64_t t = k;
-#pragma unroll
-    for (int size = 2; size <= 32; size <<= 1)
-#pragma unroll
-      for (int o = size >> 1; o > 0; o >>= 1) {
-        const uint64_t other = __shfl_xor_sync(0xffffffffu, t, o);
-        const bool down = (lane & size) == 0 || size == 32, first = (lane & o) == 0;
-        t = (down == first) == (t > other) ? t : other;
-      }
-    lists[warp][lane] = t;
+    float most = acc.m;
+    for (int o = 1; o < lanes; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+    if (lane % lanes == 0) (S > 1 ? mine_max : maxima)[tid / lanes] = most;
     if (tid == 0) {
-      from_key = 1;  // fewer than n elements: all of them
       collected = 0;
-    }
-    __syncthreads();
-    if (lane < a.n && t != 0) {
-      int above = lane;
-#pragma unroll
-      for (int w = 0; w < LP_WARPS; ++w) {
-        if (w == warp) continue;
-        int lo = 0;  // how many of that list are larger
-#pragma unroll
-        for (int b = 16; b > 0; b >>= 1) lo += lists[w][lo + b - 1] > t ? b : 0;
-        above += lo + (lists[w][lo] > t);
-      }
-      if (above == a.n - 1) from_key = t;
-    }
-    __syncthreads();
-    const uint64_t from = from_key;
-    if (reach >= from)
-      scan([&](float y, int i) {
-        const uint64_t e = lp_key(y, i);
-        if (e >= from) {
-          const int at = atomicAdd(&collected, 1);
-          if (at < LP_ROOM) keys[at] = e;
-        }
-      });
-    __syncthreads();
-    if (collected <= LP_ROOM) {
-      lp_best(keys, collected, a.n, best);
-    } else {
-      if (tid == 0) from_key = ~0ull;
-      __syncthreads();
-      for (int i = 0; i < a.n; ++i) {
-        const uint64_t under = from_key;
-        uint64_t e = 0;
-        if (reach >= from)
-          scan([&](float y, int j) {
-            const uint64_t q = lp_key(y, j);
-            if (q < under && q > e) e = q;
-          });
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) {
-          const uint64_t other = __shfl_down_sync(0xffffffffu, e, o);
-          e = other > e ? other : e;
-        }
-        __syncthreads();  // from_key has been read
-        if (lane == 0) lists[0][warp] = e;
-        __syncthreads();
-        if (tid == 0) {
-          for (int w = 1; w < LP_WARPS; ++w) e = lists[0][w] > e ? lists[0][w] : e;
-          best[i] = from_key = e;
-        }
-        __syncthreads();
-      }
+      nth = 0;
     }
   }
   __syncthreads();
-
-  // ---- the block's sums, and the cluster's
-  if (warp == 0) {
-    s = lane < LP_WARPS ? warp_sums[lane] : LpSums{-INFINITY, 0.f, 0.f};
-#pragma unroll
-    for (int o = LP_WARPS / 2; o > 0; o >>= 1) {
-      LpSums b = {__shfl_down_sync(0xffffffffu, s.m, o), __shfl_down_sync(0xffffffffu, s.z, o),
-                  __shfl_down_sync(0xffffffffu, s.w, o)};
-      lp_join(s, b, a.c);
-    }
-  }
-  if (S > 1) {
-    lp_cluster_wait();  // every block of the cluster is running
-    if (tid == 0) {
-      lp_store_leader(lp_at_leader(smem_u32(&rank_mz[rank])),
-                      static_cast<uint64_t>(__float_as_uint(s.m)) << 32 | __float_as_uint(s.z));
-      lp_store_leader(lp_at_leader(smem_u32(&rank_w[rank])), __float_as_uint(s.w));
-    }
-    if (tid < a.n) lp_store_leader(lp_at_leader(smem_u32(&from_ranks[rank * a.n + tid])), best[tid]);
-    __syncwarp();
-    lp_cluster_arrive();
-    if (rank != 0) {
+  if (S > 1) lp_cluster_wait();  // every block of the cluster is running
+  uint64_t list = 0;
+  if (a.n > 0) {
+    if (S > 1) {
+      if (tid < S * groups) lp_store_at(smem_u32(&maxima[rank * groups + tid % groups]), tid / groups, mine_max[tid % groups]);
+      __syncwarp();
+      lp_cluster_arrive();
       lp_cluster_wait();
-      return;
     }
-    lp_cluster_wait();
-    if (a.n > 0) lp_best(from_ranks, S * a.n, a.n, best);
+    if (warp * 32 < S * groups) {
+      const uint32_t t = lp_nth(maxima, S * groups, a.n, maxima[tid]);
+      if (lane == 0 && t != 0) atomicMax(&nth, t);
+    }
+    __syncthreads();
+    const float from = lp_from(nth);
+    lp_collect<E>(row, [&](int i) { return __ldg(row.xv + i); }, from, acc.m, warp * 32, THREADS, keys, &collected,
+                  who[warp]);
+    __syncthreads();
+    if (warp == 0) list = collected <= LP_ROOM ? lp_rank<E>(keys, collected, a.n, best) : lp_sorted<E>(row, a.n);
+  }
+  if (warp == 0) s = lp_reduce<W>(warp_sums[lane & (W - 1)], a.c);
+  if (S > 1) {
     if (warp == 0) {
-      s = LpSums{-INFINITY, 0.f, 0.f};
-      if (lane < S) {
-        const uint64_t mz = rank_mz[lane];
-        s = LpSums{__uint_as_float(static_cast<uint32_t>(mz >> 32)), __uint_as_float(static_cast<uint32_t>(mz)),
-                   __uint_as_float(static_cast<uint32_t>(rank_w[lane]))};
+      auto two = [](float hi, float lo) { return static_cast<uint64_t>(__float_as_uint(hi)) << 32 | __float_as_uint(lo); };
+      if (lane == 0) {
+        lp_store_leader(lp_at_leader(smem_u32(&rank_m[rank])), two(0.f, s.m));
+        lp_store_leader(lp_at_leader(smem_u32(&rank_zw[rank])), two(s.z, s.w));
       }
-#pragma unroll
-      for (int o = LP_CLUSTER / 2; o > 0; o >>= 1) {
-        LpSums b = {__shfl_down_sync(0xffffffffu, s.m, o), __shfl_down_sync(0xffffffffu, s.z, o),
-                    __shfl_down_sync(0xffffffffu, s.w, o)};
-        lp_join(s, b, a.c);
+      if (lane < a.n) lp_store_leader(lp_at_leader(smem_u32(&from_ranks[rank * a.n + lane])), list);
+      __syncwarp();
+    }
+    lp_cluster_arrive();
+    lp_cluster_wait();
+    if (rank != 0 || warp != 0) return;
+    if (a.n > 0) {
+      int count = 0;
+      for (int i = 0; i < S * a.n; i += 32) {
+        const uint64_t k = i + lane < S * a.n ? from_ranks[i + lane] : 0;
+        const uint32_t some = __ballot_sync(0xffffffffu, k != 0);
+        if (k != 0) keys[count + __popc(some & ((1u << lane) - 1u))] = k;
+        count += __popc(some);
       }
+      __syncwarp();
+      list = lp_rank<E>(keys, count, a.n, best);
     }
+    auto hi = [](uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); };
+    auto lo = [](uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v)); };
+    s = lane < S ? LpSums{lo(rank_m[lane]), hi(rank_zw[lane]), lo(rank_zw[lane])} : LpSums{LP_LEAST, 0.f, 0.f};
+    s = lp_reduce<32>(s, a.c);
   }
-  if (warp == 0) {
-    s.m = __shfl_sync(0xffffffffu, s.m, 0);
-    s.z = __shfl_sync(0xffffffffu, s.z, 0);
-    s.w = __shfl_sync(0xffffffffu, s.w, 0);
-    const float lnz = logf(s.z);
-    // no probability anywhere (all logits minus infinity): -inf, and an entropy of 0
-    auto logprob = [&](float y) { return s.z == 0.f ? -INFINITY : (y - s.m) * a.scale - lnz; };
-    if (lane == 0) {
-      if (a.logprob != nullptr) a.logprob[row] = logprob(Vec::one(x + token));
-      if (a.entropy != nullptr) a.entropy[row] = s.z == 0.f ? 0.f : lnz - LP_LN2 * (s.w / s.z);
-    }
-    if (lane < a.n) {
-      const uint64_t k = best[lane];
-      if (a.top_id != nullptr) a.top_id[row * a.n + lane] = static_cast<int32_t>(lp_key_index(k));
-      if (a.top_logprob != nullptr) a.top_logprob[row * a.n + lane] = logprob(lp_key_value(k));
-    }
-  }
+  if (warp == 0) lp_results<E>(a, r, row.x, token, logit, s, list);
 }
 
 }  // namespace decomoe
@@ -405,14 +654,25 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
   a.n = top_id != nullptr || top_logprob != nullptr ? n : 0;
   a.scale = scale;
   a.c = scale * 1.4426950408889634f;
-  // blocks for every SM, and a slice of at least a vector per thread
-  int S = 1;
-  while (S < LP_CLUSTER && T * S < 2 * sm_count() && V * static_cast<int64_t>(e) > 16 * LP_THREADS * S) S *= 2;
-  auto go = [&](auto kern) -> int {
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+  const int64_t row_bytes = V * static_cast<int64_t>(e), sms = sm_count();
+  auto go = [&](auto warp_rows, auto cluster, auto many) -> int {
+    if (row_bytes <= 1024 || (row_bytes <= 8192 && T >= 2 * sms)) {
+      DM_CUDA_CHECK(launch_pdl(warp_rows, dim3(static_cast<unsigned>((T + LP_WARPS - 1) / LP_WARPS)), dim3(LP_THREADS), 0, s, a));
+      return DECOMOE_OK;
+    }
+    if (T >= 16 * sms) {
+      DM_CUDA_CHECK(launch_pdl(many, dim3(static_cast<unsigned>(T)), dim3(128), 0, s, a, 1));
+      return DECOMOE_OK;
+    }
+    // blocks for every SM, and a slice of at least a vector per thread
+    int S = 1;
+    const int cap = T <= 8 ? LP_CLUSTER : 8;
+    while (S < cap && T * S < 2 * sms && row_bytes > 16 * LP_THREADS * S) S *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(T * S));
     cfg.blockDim = dim3(LP_THREADS);
-    cfg.stream = reinterpret_cast<cudaStream_t>(stream);
+    cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = pdl_enabled(T * S) ? 1 : 0;
@@ -421,9 +681,11 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = S > 1 ? 2 : 1;
-    if (S > 8) DM_CUDA_CHECK(cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    DM_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kern, a, S));
+    if (S > 8) DM_CUDA_CHECK(cudaFuncSetAttribute(cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    DM_CUDA_CHECK(cudaLaunchKernelEx(&cfg, cluster, a, S));
     return DECOMOE_OK;
   };
-  return dtype == DECOMOE_BF16 ? go(k_token_logprobs<__nv_bfloat16>) : go(k_token_logprobs<float>);
+  return dtype == DECOMOE_BF16
+             ? go(k_logprobs_warp<__nv_bfloat16>, k_logprobs_cluster<__nv_bfloat16, 8>, k_logprobs_cluster<__nv_bfloat16, 4>)
+             : go(k_logprobs_warp<float>, k_logprobs_cluster<float, 8>, k_logprobs_cluster<float, 4>);
 }
