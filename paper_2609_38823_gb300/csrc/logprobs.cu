@@ -26,6 +26,7 @@ constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_BEST = 32;
 constexpr int LP_ROOM = 512;  // collected elements of a block, or of a row
 constexpr int LP_CLUSTER = 16;
+constexpr int LP_RESIDENT = 48;  // warps of an SM
 constexpr float LP_LN2 = 0.6931471805599453f;
 constexpr float LP_LEAST = -0x1p100f;  // what elements count as at least
 constexpr float LP_PLAIN = 0x1p97f;    // rows with a maximum below this in size are in the plain range
@@ -499,7 +500,7 @@ __device__ __forceinline__ void lp_cluster_arrive() { asm volatile("barrier.clus
 __device__ __forceinline__ void lp_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 template <typename E, int W>
-__global__ void __launch_bounds__(32 * W) k_logprobs_cluster(LpArgs a, int S) {
+__global__ void __launch_bounds__(32 * W, LP_RESIDENT / W) k_logprobs_cluster(LpArgs a, int S) {
   constexpr int U = 4, THREADS = 32 * W;
   __shared__ uint64_t keys[LP_ROOM];
   __shared__ uint64_t from_ranks[LP_CLUSTER * LP_BEST];
@@ -661,7 +662,13 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
       DM_CUDA_CHECK(launch_pdl(warp_rows, dim3(static_cast<unsigned>((T + LP_WARPS - 1) / LP_WARPS)), dim3(LP_THREADS), 0, s, a));
       return DECOMOE_OK;
     }
-    if (T >= 16 * sms) {
+    // A block per row: of four warps (twelve rows at a time on an SM) or of eight, whichever leaves fewer
+    // places empty in its last turn.
+    auto full = [&](int warps) {
+      const int64_t at_once = sms * (LP_RESIDENT / warps);
+      return static_cast<double>(T) / static_cast<double>((T + at_once - 1) / at_once * at_once);
+    };
+    if (T >= 2 * sms && full(4) >= full(8)) {
       DM_CUDA_CHECK(launch_pdl(many, dim3(static_cast<unsigned>(T)), dim3(128), 0, s, a, 1));
       return DECOMOE_OK;
     }
