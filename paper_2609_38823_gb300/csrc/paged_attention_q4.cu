@@ -12,6 +12,7 @@ constexpr int Q4A_KEYS = 32;     // rows of a tile
 constexpr int Q4A_SETS = Q4A_KEYS / 8;
 constexpr int Q4A_BLOCKS = 160;  // of a launch, at most
 constexpr int q4a_warps(int NT) { return NT == 1 ? 16 : 8; }  // of a block, one block per SM: as many as their registers allow
+constexpr int Q4A_FEW = 8;       // warps of a block that get tiles where there are few
 constexpr int Q4A_EXTRA = 3;     // what a (request, KV head) pair costs beside its tiles, in tiles
 constexpr int q4a_stages(int D) { return 2; }
 
@@ -160,11 +161,11 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
   if (lane < STAGES) mbar_init(smem_u32(&bars[warp][lane]), 1);
   fence_mbar_init();
   pdl_enter();
-  const PgaPlan plan = pga_begin<Q4aTiles, D, WARPS>(a, pre, nz);
-  const int me = blockIdx.x * WARPS + warp;
+  const PgaPlan plan = pga_begin<Q4aTiles, D, WARPS, Q4A_FEW>(a, pre, nz);
+  const int me = blockIdx.x * plan.active + min(warp, plan.active);
   // lane 0 seeks the start of this warp's share, lane 1 that of the next one's
   PgaWalk<Q4aTiles> seek;
-  const int from = plan.place(me + (lane & 1));
+  const int from = plan.place(warp < plan.active ? me + (lane & 1) : me);
   const int first = from < plan.total ? seek.seek(plan, from) : pre[a.B] * a.hv;
   const int r0 = __shfl_sync(0xffffffffu, first, 0), r1 = __shfl_sync(0xffffffffu, first, 1);
   const int gs = a.hq / a.hkv;
@@ -557,7 +558,7 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
           if (lane == 0) meta[warp] = make_int3(began ? 2 : 1, b, h);
         } else if (began) {
           // begun before the block: it is all that the block holds of its pair
-          keep_piece(warp == 0 ? part : a.early + static_cast<int64_t>(me) * ROWS * ROW);
+          keep_piece(warp == 0 ? part : a.early + static_cast<int64_t>(blockIdx.x * WARPS + warp) * ROWS * ROW);
         } else {
           const int g = a.qt == 1 ? h : h / a.qt, q0 = (h - g * a.qt) * ROWS;
 #pragma unroll
@@ -580,7 +581,7 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
     }
   }
   __syncthreads();
-  pga_join_block<D, NT, WARPS>(a, plan, meta, q4a_smem, RING);
+  pga_join_block<D, NT, WARPS, true>(a, plan, meta, q4a_smem, RING);
 }
 
 }  // namespace decomoe
@@ -671,7 +672,7 @@ int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const
   DM_ARG_CHECK(most + Q4A_EXTRA * B * a.hv <= INT_MAX, "paged_attention_q4: B * max_pages * page_size * heads is too large");
   const int warps = q4a_warps(rows / 8);
   const int grid = static_cast<int>(
-      std::max<int64_t>(1, std::min<int64_t>(std::min(sm_count(), Q4A_BLOCKS), (most + warps - 1) / warps)));
+      std::max<int64_t>(1, std::min<int64_t>(std::min(sm_count(), Q4A_BLOCKS), (most + Q4A_FEW - 1) / Q4A_FEW)));
   const size_t piece = static_cast<size_t>(rows) * pga_row(D);
   a.early = static_cast<float*>(ws);
   a.part = a.early + static_cast<size_t>(grid) * warps * piece;

@@ -57,6 +57,7 @@ struct PgaPlan {
   const int* pre;  // [B + 1] tiles per head tile before a request
   const int* nz;   // [B + 1] requests that see something before a request
   int B, hv, extra;
+  int active;      // warps of a block that have a share
   int total;       // places in all
   int per, more;   // places of a warp, and how many warps take one more
   __device__ __forceinline__ int places(int b) const {  // before request b
@@ -166,8 +167,9 @@ struct PgaWalk {
 
 // The start of a launch, by every thread of a block: the tiles of every request added up
 // in pre and nz (shared memory, [B + 1] each), zeros for the requests that see nothing, and
-// the division of the tiles among the launch's warps.
-template <class Tiles, int D, int W>
+// the division of the tiles among the launch's warps: W of every block, or where FEW is not 0 and there are
+// fewer tiles than that, the first FEW or more of every block.
+template <class Tiles, int D, int W, int FEW = 0>
 __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int* nz) {
   constexpr int THREADS = 32 * W;
   __shared__ int scan_w[2][W];
@@ -226,8 +228,10 @@ __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int
   plan.nz = nz;
   plan.B = a.B;
   plan.hv = a.hv;
-  plan.extra = pre[a.B] * a.hv > static_cast<int>(gridDim.x) * W ? a.extra : 0;
-  plan.divide(static_cast<int>(gridDim.x) * W);
+  const int blocks = static_cast<int>(gridDim.x), all = pre[a.B] * a.hv;
+  plan.extra = all > blocks * W ? a.extra : 0;
+  plan.active = FEW == 0 ? W : min(W, max(FEW, (all + blocks - 1) / blocks));
+  plan.divide(blocks * plan.active);
   return plan;
 }
 
@@ -236,7 +240,7 @@ __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int
 // the one in which the pair ends. What began before the block or goes on after it leaves
 // joined. All pieces are loaded ahead of the walk. meta: of each warp, whether its last piece
 // goes on (1: begun in its share, 2: before it), its request and head tile.
-template <int D, int NT, int W>
+template <int D, int NT, int W, bool FEW = false>
 __device__ __forceinline__ void pga_join_block(const PagedCommon& a, const PgaPlan& plan, const int3* meta,
                                                const uint8_t* rings, int ring_bytes) {
   constexpr int ROWS = 8 * NT, ROW = pga_row(D);
@@ -250,6 +254,7 @@ __device__ __forceinline__ void pga_join_block(const PagedCommon& a, const PgaPl
   int kind[W];  // of a warp's last piece: 0 ends there, 1 begun in its share and goes on, 2 its whole share
 #pragma unroll
   for (int w = 0; w < W; ++w) kind[w] = meta[w].x;
+  const int active = FEW ? plan.active : W;  // the others have nothing
 #pragma unroll 1
   for (int r = SHARERS > 1 ? warp % ROWS : warp; r < ROWS; r += W) {
     PgaVec<C> last[W], early[W];
@@ -262,7 +267,7 @@ __device__ __forceinline__ void pga_join_block(const PagedCommon& a, const PgaPl
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       if (AHEAD && kind[w] != 0) load_last(w);
-      if (w > 0 && kind[w - 1] != 0 && kind[w] != 2) {
+      if (w > 0 && w < active && kind[w - 1] != 0 && kind[w] != 2) {
         const float* p = a.early + (static_cast<int64_t>(blockIdx.x * W + w) * ROWS + r) * ROW;
         early_ml[w] = *reinterpret_cast<const float2*>(p + D);
         pga_load<false>(early[w], p + at);
@@ -271,14 +276,14 @@ __device__ __forceinline__ void pga_join_block(const PagedCommon& a, const PgaPl
     if (tid == 0) {
       // a pair that begins here and ends in a later block
       int4 info = make_int4(0, 0, 0, 0);
-      if (kind[W - 1] != 0) {
-        int w0 = W - 1;
-        while (w0 > 0 && kind[w0] == 2) --w0;
+      if (meta[active - 1].x != 0) {
+        int w0 = active - 1;
+        while (w0 > 0 && meta[w0].x == 2) --w0;
         if (meta[w0].x == 1) {
           info = make_int4(1, meta[w0].y, meta[w0].z, 0);
           const int tiles = plan.pre[info.y + 1] - plan.pre[info.y];
           const int end = plan.places(info.y) + (info.z + 1) * (tiles + plan.extra) - 1;
-          info.w = plan.holder(end) / W;
+          info.w = plan.holder(end) / active;
         }
       }
       a.info[blockIdx.x] = info;
@@ -307,6 +312,7 @@ __device__ __forceinline__ void pga_join_block(const PagedCommon& a, const PgaPl
     bool on = false;  // a chain goes on into warp w
 #pragma unroll
     for (int w = 0; w < W; ++w) {
+      if (w >= active) continue;
       if (!AHEAD && kind[w] != 0) load_last(w);
       if (on) {
         if (kind[w] == 2) {
