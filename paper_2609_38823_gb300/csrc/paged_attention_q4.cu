@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
   static_assert(ROWS * ROW * 4 <= RING, "a piece fits the ring");
   extern __shared__ __align__(1024) uint8_t q4a_smem[];
   __shared__ __align__(8) uint64_t bars[WARPS][STAGES];
-  __shared__ int4 tile_info[WARPS][2 * Q4A_BATCH];  // rows seen, request, head tile, whether the pair ends
+  __shared__ int4 tile_info[WARPS][2 * Q4A_BATCH];  // rows seen, request, head tile, whether the pair ends (1) and begins (2)
   __shared__ int3 meta[WARPS];
   __shared__ int abort_flag;
   int* pre = reinterpret_cast<int*>(q4a_smem + WARPS * RING);
@@ -206,18 +206,24 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
                ((look.at & ((1 << a.shift) - 1)) >> 3)) * L::BYTES;
       if (set == 0)
         tile_info[warp][(which & 1) * Q4A_BATCH + mine_of] =
-            make_int4(static_cast<int>(mask), look.b, look.h, look.t + 1 == look.tiles);
+            make_int4(static_cast<int>(mask), look.b, look.h, (look.t + 1 == look.tiles) | (look.t == 0) << 1);
       look.advance(a, pre, Q4A_BATCH);
       look.load(a, set, in_page);
       __syncwarp();
     };
     auto issue = [&](int tile, int slot) {
       if (tile % Q4A_BATCH == 0) begin_batch(tile / Q4A_BATCH);
-      if (mine_of == tile % Q4A_BATCH) {
-        const uint32_t bar = bar_s + slot * 8;
-        if (set == 0) mbar_arrive_expect_tx(bar, bytes);
-        __syncwarp(((1u << Q4A_SETS) - 1) << (lane & ~(Q4A_SETS - 1)));
-        if (there && leads) q4a_bulk(ring_s + slot * STAGE + set * L::BYTES, src, in_one * L::BYTES, bar);
+      const bool turn = mine_of == tile % Q4A_BATCH;
+      const uint32_t bar = bar_s + slot * 8, dst = ring_s + slot * STAGE + set * L::BYTES;
+      if (in_one == Q4A_SETS) {
+        if (turn && set == 0) {
+          mbar_arrive_expect_tx(bar, bytes);
+          if (there) q4a_bulk(dst, src, STAGE, bar);
+        }
+      } else {
+        if (turn && set == 0) mbar_arrive_expect_tx(bar, bytes);
+        __syncwarp();
+        if (turn && there && leads) q4a_bulk(dst, src, in_one * L::BYTES, bar);
       }
       __syncwarp();
     };
@@ -361,7 +367,8 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
         if (i == -1) begin_piece();
         continue;
       }
-      if (!__all_sync(0xffffffffu, mbar_wait(bar_s + slot * 8, parity, a.limit_ns, &abort_flag))) {
+      if (!__all_sync(0xffffffffu, mbar_try_wait(bar_s + slot * 8, parity)) &&
+          !__all_sync(0xffffffffu, mbar_wait(bar_s + slot * 8, parity, a.limit_ns, &abort_flag))) {
         if (lane == 0) report_status(a.status, DECOMOE_ERR_TIMEOUT);
         // no results; what is in flight gets the same time to land
         for (int k = 1; k < STAGES && i + k < n; ++k) {
@@ -372,7 +379,7 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
       }
       const uint32_t stage = ring_s + slot * STAGE;
       const int4 info = tile_info[warp][i % (2 * Q4A_BATCH)];
-      if (info.y != b || info.z != h) {  // a new pair
+      if ((info.w & 2) && i > 0) {  // a new pair
         b = info.y;
         h = info.z;
         began = false;
@@ -421,6 +428,11 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
             for (int i2 = 0; i2 < 4; ++i2) sc[u][x][i2] = fmaf(bf16_lo(kp[i2 >> 1][g]), acc[x][i2], sc[u][x][i2]);
         }
       }
+      uint32_t vp[SUB][2][G];
+#pragma unroll
+      for (int u = 0; u < SUB; ++u)
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) q4a_lds(stage + (2 * u + hf) * L::BYTES + L::VP + kr * L::PARAMS, vp[u][hf]);
       if (mask != 0xffffffffu) {
         __syncwarp();  // (a branch of its own: as predicates it would cost every tile)
 #pragma unroll
@@ -431,22 +443,9 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
               // anything may lie where nothing is seen
 #pragma unroll
               for (int x = 0; x < NT; ++x) sc[u][x][2 * hf] = sc[u][x][2 * hf + 1] = -INFINITY;
-            }
-      }
-      uint32_t vp[SUB][2][G];
-#pragma unroll
-      for (int u = 0; u < SUB; ++u)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) q4a_lds(stage + (2 * u + hf) * L::BYTES + L::VP + kr * L::PARAMS, vp[u][hf]);
-      if (mask != 0xffffffffu) {
-        __syncwarp();
-#pragma unroll
-        for (int u = 0; u < SUB; ++u)
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-            if (!((mask >> (16 * u + 8 * hf + kr)) & 1u))
 #pragma unroll
               for (int g = 0; g < G; ++g) vp[u][hf][g] = 0u;
+            }
       }
       // ---- a query's maximum, raised only where a score passes it by 2^8 (weights up to 2^8 cost no
       // digits), and the scale of the steps, which keeps weights times steps, the fp16 operands
@@ -551,9 +550,10 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
       }
       __syncwarp();
       slot = slot + 1 == STAGES ? (parity ^= 1, 0) : slot + 1;
-      if (info.w || i + 1 == n) {
+      const bool ends = info.w & 1;
+      if (ends || i + 1 == n) {
         end_piece();
-        if (!info.w) {  // goes on in the next share; the ring is empty
+        if (!ends) {  // goes on in the next share; the ring is empty
           keep_piece(mine);
           if (lane == 0) meta[warp] = make_int3(began ? 2 : 1, b, h);
         } else if (began) {
