@@ -51,53 +51,66 @@ __device__ __forceinline__ void q4_unpack8(const uint4& u, float (&x)[8]) {
   x[4] = bf16_lo(u.z), x[5] = bf16_hi(u.z), x[6] = bf16_lo(u.w), x[7] = bf16_hi(u.w);
 }
 
+__device__ __forceinline__ uint32_t q4_max2(uint32_t a, uint32_t b) {  // of two pairs of bf16 numbers, NaN where one is
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+
 // The codes of eight features of a group that GL lanes share, and the group's parameters.
 template <int GL>
 __device__ __forceinline__ uint32_t q4_quantise(const uint4& u, uint32_t* params) {
-  float x[8];
-  q4_unpack8(u, x);
-  // NaN where a value is not finite (its difference from itself is not zero)
-  float lo = x[0], hi = x[0], odd = 0.f;
+  // the largest of the values (high half) and of their negatives
+  const uint32_t big = q4_max2(q4_max2(u.x, u.y), q4_max2(u.z, u.w));
+  constexpr uint32_t MINUS = 0x80008000u;
+  const uint32_t neg = q4_max2(q4_max2(u.x ^ MINUS, u.y ^ MINUS), q4_max2(u.z ^ MINUS, u.w ^ MINUS));
+  uint32_t ends = q4_max2(__byte_perm(neg, big, 0x5410), __byte_perm(neg, big, 0x7632));
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    lo = fminf(lo, x[j]);
-    hi = fmaxf(hi, x[j]);
-    odd = fmaf(x[j], 0.f, odd);
-  }
-#pragma unroll
-  for (int w = 1; w < GL; w <<= 1) {
-    lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, w));
-    hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, w));
-    odd += __shfl_xor_sync(0xffffffffu, odd, w);
-  }
-  const float range = hi - lo;
-  const bool finite = odd == 0.f && range <= FLT_MAX;
-  const float step = __bfloat162float(__float2bfloat16_rn(__fdiv_rn(range, 15.f)));
+  for (int w = 1; w < GL; w <<= 1) ends = q4_max2(ends, __shfl_xor_sync(0xffffffffu, ends, w));
+  const float lo = -bf16_lo(ends), range = bf16_hi(ends) + bf16_lo(ends);
+  // range / 15, to nearest: Markstein's correction of a quotient from the rounded reciprocal
+  float step32 = range * (1.f / 15.f);
+  step32 = fmaf(fmaf(-15.f, step32, range), 1.f / 15.f, step32);
+  const bool small = range < 0x1p-100f;  // where remainders would be subnormal, divide
+  if (small) step32 = __fdiv_rn(range, 15.f);
+  const float step = __bfloat162float(__float2bfloat16_rn(step32));
+  const bool finite = range <= FLT_MAX;  // a value that is not gives NaN or infinity
   *params = finite ? pack_bf16x2(step, lo) : 0x7fff7fffu;
   if (!finite || step == 0.f) return 0;
-  // (x - lo) / step by the step's reciprocal: the addition of 3 * 2^22 rounds it to an integer in
-  // the low bits. It may miss the nearest code only where a value lies half way between two
-  // but for a rounding, which the exact remainder shows; those groups, and steps near or
-  // below the normal numbers, divide.
-  constexpr float MAGIC = 12582912.f;
-  const float inv = __frcp_rn(step);
+  float x[8];
+  q4_unpack8(u, x);
   uint32_t code = 0;
-  float far = 0.f;
+  if (small) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float r = x[j] - lo, t = fmaf(r, inv, MAGIC);
-    far = fmaxf(far, fabsf(fmaf(MAGIC - t, step, r)));
-    code += __float_as_uint(t) << (4 * j);
-  }
-  if (far < 0.5f * step && step >= 0x1p-110f) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) code -= 0x4b400000u << (4 * j);
+    for (int j = 0; j < 8; ++j)
+      code |= static_cast<uint32_t>(fminf(rintf(__fdiv_rn(x[j] - lo, step)), 15.f)) << (4 * j);
     return code;
   }
-  code = 0;
+  // (x - lo) / step by an approximate reciprocal; adding 3 * 2^22 rounds it to an integer in the
+  // low bits. That misses the nearest code only next to the middle between two, which the exact
+  // remainder shows: half a step or more.
+  constexpr float MAGIC = 12582912.f;
+  float inv, t[8], far = 0.f;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(step));
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    code |= static_cast<uint32_t>(fminf(rintf(__fdiv_rn(x[j] - lo, step)), 15.f)) << (4 * j);
+  for (int j = 0; j < 8; ++j) {
+    x[j] -= lo;
+    t[j] = fmaf(x[j], inv, MAGIC);
+    far = fmaxf(far, fabsf(fmaf(MAGIC - t[j], step, x[j])));
+  }
+  const float half = 0.5f * step;
+  if (far >= half) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float rest = fmaf(MAGIC - t[j], step, x[j]);
+      const bool odd = __float_as_uint(t[j]) & 1u;
+      if (fabsf(rest) > half || (fabsf(rest) == half && odd)) t[j] += copysignf(1.f, rest);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) code += __float_as_uint(t[j]) << (4 * j);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) code -= 0x4b400000u << (4 * j);
   return code;
 }
 
