@@ -15,7 +15,7 @@ namespace decomoe {
 // product with d finite. A row whose maximum is not below 2^97 in size (all masked, infinite,
 // enormous) is computed again with every case, by one warp.
 //
-// The n <= 32 best: the threads fall into 64 groups or more, and the n-th largest of the groups'
+// The n <= 32 best: the threads fall into 64 groups, and the n-th largest of the groups'
 // maxima bounds the n-th largest element from below, since groups have no element in common; about n to
 // 1.5 n elements reach it. The vectors of the few threads whose maxima do are read again, elements that reach it collected as 64-bit keys of value and index, all
 // different, and ranked by counting; ties go to the lowest index, and no order of execution
@@ -25,7 +25,7 @@ constexpr int LP_THREADS = 256;
 constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_BEST = 32;
 constexpr int LP_ROOM = 512;  // collected elements of a block, or of a row
-constexpr int LP_CLUSTER = 16;
+constexpr int LP_CLUSTER = 8;  // blocks of a row, at most
 constexpr int LP_RESIDENT = 48;  // warps of an SM
 constexpr float LP_LN2 = 0.6931471805599453f;
 constexpr float LP_LEAST = -0x1p100f;  // what elements count as at least
@@ -346,13 +346,13 @@ __device__ __forceinline__ uint32_t lp_order(float x) {
   const uint32_t u = __float_as_uint(x);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-// The n-th largest of `count` (a multiple of 4) values is the largest that n of them reach: this thread's
-// value where that holds, raised to the warp's largest such (0: none).
-__device__ __forceinline__ uint32_t lp_nth(const float* values, int count, int n, float mine) {
+// The n-th largest of 64 values is the largest that n of them reach: this thread's value where
+// that holds, raised to the warp's largest such (0: none).
+__device__ __forceinline__ uint32_t lp_nth(const float* values, int n, float mine) {
   int reach = 0;
   const float4* v = reinterpret_cast<const float4*>(values);
 #pragma unroll 4
-  for (int i = 0; i < count / 4; ++i) {
+  for (int i = 0; i < 16; ++i) {
     const float4 u = v[i];
     reach += (u.x >= mine) + (u.y >= mine) + (u.z >= mine) + (u.w >= mine);
   }
@@ -465,7 +465,7 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_warp(LpArgs a) {
     maxima[warp][lane] = first;
     maxima[warp][lane + 32] = other;
     __syncwarp();
-    const uint32_t t = max(lp_nth(maxima[warp], 64, a.n, first), lp_nth(maxima[warp], 64, a.n, other));
+    const uint32_t t = max(lp_nth(maxima[warp], a.n, first), lp_nth(maxima[warp], a.n, other));
     if (lane == 0) count[warp] = 0;
     __syncwarp();
     lp_collect<E>(row, [&](int i) { return __ldg(row.xv + i); }, lp_from(t), acc.m, 0, 32, keys[warp],
@@ -506,7 +506,7 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT / W) k_logprobs_cluster(Lp
   __shared__ uint64_t from_ranks[LP_CLUSTER * LP_BEST];
   __shared__ uint64_t best[LP_BEST];
   __shared__ LpSums warp_sums[W];
-  __shared__ __align__(16) float mine_max[64], maxima[8 * LP_CLUSTER];  // of the block's groups, and of all
+  __shared__ __align__(16) float mine_max[64], maxima[64];  // of the block's groups, and of all
   __shared__ uint32_t nth;
   __shared__ uint64_t rank_m[LP_CLUSTER], rank_zw[LP_CLUSTER];
   __shared__ int collected, who[W][32];
@@ -549,8 +549,9 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT / W) k_logprobs_cluster(Lp
   if (tid < row.edges) acc.one(edge, a.c);
   LpSums s = lp_reduce<32>(lp_sums(acc), a.c);
   if (lane == 0) warp_sums[warp] = s;
-  // groups of THREADS S / 64 lanes, a warp at most: `groups` in the block, 64 to 128 in all
-  const int lanes = min(THREADS / 64 * S, 32), groups = THREADS / lanes;
+  // 64 groups of THREADS S / 64 lanes (a warp at most: S <= 8), `groups` of them in the block
+  static_assert(THREADS / 64 * LP_CLUSTER <= 32, "groups lie in warps");
+  const int lanes = THREADS / 64 * S, groups = 64 / S;
   if (a.n > 0) {
     float most = acc.m;
     for (int o = 1; o < lanes; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
@@ -565,13 +566,13 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT / W) k_logprobs_cluster(Lp
   uint64_t list = 0;
   if (a.n > 0) {
     if (S > 1) {
-      if (tid < S * groups) lp_store_at(smem_u32(&maxima[rank * groups + tid % groups]), tid / groups, mine_max[tid % groups]);
+      if (tid < 64) lp_store_at(smem_u32(&maxima[rank * groups + tid % groups]), tid / groups, mine_max[tid % groups]);
       __syncwarp();
       lp_cluster_arrive();
       lp_cluster_wait();
     }
-    if (warp * 32 < S * groups) {
-      const uint32_t t = lp_nth(maxima, S * groups, a.n, maxima[tid]);
+    if (warp < 2) {
+      const uint32_t t = lp_nth(maxima, a.n, maxima[tid]);
       if (lane == 0 && t != 0) atomicMax(&nth, t);
     }
     __syncthreads();
@@ -623,7 +624,7 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
                                       int32_t* top_id, float* top_logprob, int32_t* status_dev, decomoe_stream_t stream) {
   clear_error();
   DM_ARG_CHECK(dtype == DECOMOE_BF16 || dtype == DECOMOE_F32, "token_logprobs: logits must be bf16 or f32");
-  DM_ARG_CHECK(T >= 0 && T <= INT_MAX / LP_CLUSTER, "token_logprobs: bad number of rows");
+  DM_ARG_CHECK(T >= 0 && T <= INT_MAX / 16, "token_logprobs: bad number of rows");
   DM_ARG_CHECK(V >= 1 && V <= (1 << 24), "token_logprobs: a vocabulary of 1 to 2^24 expected");
   DM_ARG_CHECK(row_stride >= V, "token_logprobs: row stride below the vocabulary's size");
   DM_ARG_CHECK(scale > 0.f && scale <= FLT_MAX, "token_logprobs: scale must be positive and finite");
@@ -674,8 +675,7 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
     }
     // blocks for every SM, and a slice of at least a vector per thread
     int S = 1;
-    const int cap = T <= 8 ? LP_CLUSTER : 8;
-    while (S < cap && T * S < 2 * sms && row_bytes > 16 * LP_THREADS * S) S *= 2;
+    while (S < LP_CLUSTER && T * S < 2 * sms && row_bytes > 16 * LP_THREADS * S) S *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(T * S));
     cfg.blockDim = dim3(LP_THREADS);
@@ -688,7 +688,6 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = S > 1 ? 2 : 1;
-    if (S > 8) DM_CUDA_CHECK(cudaFuncSetAttribute(cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     DM_CUDA_CHECK(cudaLaunchKernelEx(&cfg, cluster, a, S));
     return DECOMOE_OK;
   };
