@@ -17,7 +17,7 @@ namespace decomoe {
 //
 // The n <= 32 best: the threads fall into 64 groups, and the n-th largest of the groups'
 // maxima bounds the n-th largest element from below, since groups have no element in common; about n to
-// 1.5 n elements reach it. The vectors of the few threads whose maxima do are read again, elements that reach it collected as 64-bit keys of value and index, all
+// 1.5 n elements reach it. The vectors of the few runs of a thread's vectors whose maxima do are read again, elements that reach it collected as 64-bit keys of value and index, all
 // different, and ranked by counting; ties go to the lowest index, and no order of execution
 // shows. Where more are collected than there is room for (rows of equal values), a warp reads the row
 // again and keeps the n best sorted in its lanes.
@@ -26,7 +26,7 @@ constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_BEST = 32;
 constexpr int LP_ROOM = 512;  // collected elements of a block, or of a row
 constexpr int LP_CLUSTER = 8;  // blocks of a row, at most
-constexpr int LP_RESIDENT = 48;  // warps of an SM
+constexpr int LP_RESIDENT(int W) { return W == 4 ? 48 : 40; }  // warps of an SM, for blocks of W
 constexpr float LP_LN2 = 0.6931471805599453f;
 constexpr float LP_LEAST = -0x1p100f;  // what elements count as at least
 constexpr float LP_PLAIN = 0x1p97f;    // rows with a maximum below this in size are in the plain range
@@ -146,9 +146,9 @@ struct LpAcc {
     z = lp_mul2(z, ff);
     m = to;
   }
-  // U vectors
+  // U vectors; their largest element.
   template <typename E, int U>
-  __device__ __forceinline__ void take(const uint4 (&u)[U], float c) {
+  __device__ __forceinline__ float take(const uint4 (&u)[U], float c) {
     using Vec = LpVec<E>;
     uint4 x[U];
     float most = LP_LEAST;
@@ -169,6 +169,7 @@ struct LpAcc {
         z = lp_add2(z, e);
         w = lp_fma2(e, d, w);
       }
+    return most;
   }
   __device__ __forceinline__ void one(float v, float c) {
     v = lp_max_nan(v, LP_LEAST);
@@ -241,35 +242,103 @@ struct LpRow {
   __device__ __forceinline__ int index(int v) const { return head + (v0 + v) * LpVec<E>::N; }  // of a vector's first element
 };
 
-// The keys (count[0] of them) with a value of `from` or more among a row's vectors v = t, t + stride, ...
-// of each thread t whose maximum is as large (mine; t = first + lane), by a warp: the vectors
-// of all such threads are spread over its lanes, so that one latency covers most rows. get(v)
-// reads one; who: 32 ints of the warp's own.
-template <typename E, class Get>
-__device__ __forceinline__ void lp_collect(const LpRow<E>& row, Get get, float from, float mine, int first, int stride,
-                                           uint64_t* keys, int* count, int* who) {
+// A row's vectors are taken in batches of LP_U a thread, thread t's vectors being t, t + threads, ...;
+// up to SLOTS runs of batches leave their maxima, so that few vectors are read again.
+constexpr int LP_U = 4;
+constexpr int LP_SLOTS = 8;
+struct LpRuns {
+  int per, slots;  // batches of a run, and runs
+  __device__ __forceinline__ LpRuns(int vecs, int threads) {
+    const int batches = (vecs + threads * LP_U - 1) / (threads * LP_U);
+    per = (batches + LP_SLOTS - 1) / LP_SLOTS;
+    slots = per > 0 ? (batches + per - 1) / per : 0;
+  }
+};
+
+// Thread t of `threads` takes its vectors; with KEEP the maxima of its runs go to slots[run * threads],
+// and those of its even and odd vectors to halves, if given.
+template <typename E, bool KEEP>
+__device__ __forceinline__ void lp_pass(const LpRow<E>& row, LpAcc& acc, float c, int t, int threads, LpRuns runs, float* slots,
+                                        float (*halves)[2] = nullptr) {
+  int v = t, left = runs.per;
+  float most = LP_LEAST;
+  auto ran = [&](float x) {
+    if (!KEEP) return;
+    most = fmaxf(most, x);
+    if (--left > 0) return;
+    *slots = most;
+    slots += threads;
+    --runs.slots;
+    most = LP_LEAST;
+    left = runs.per;
+  };
+  for (; v + (LP_U - 1) * threads < row.vecs; v += LP_U * threads) {
+    uint4 u[LP_U];
+#pragma unroll
+    for (int i = 0; i < LP_U; ++i) u[i] = __ldg(row.xv + v + i * threads);
+    ran(acc.template take<E, LP_U>(u, c));
+    if (KEEP && halves != nullptr) {
+#pragma unroll
+      for (int i = 0; i < LP_U; ++i) (*halves)[i & 1] = fmaxf((*halves)[i & 1], LpVec<E>::largest(u[i]));
+    }
+  }
+  if (v < row.vecs) {  // what is left, its loads in flight together
+    uint4 u[LP_U - 1];
+#pragma unroll
+    for (int i = 0; i < LP_U - 1; ++i)
+      if (v + i * threads < row.vecs) u[i] = __ldg(row.xv + v + i * threads);
+    float x = LP_LEAST;
+#pragma unroll
+    for (int i = 0; i < LP_U - 1; ++i)
+      if (v + i * threads < row.vecs) {
+        const uint4 w[1] = {u[i]};
+        const float y = acc.template take<E, 1>(w, c);
+        x = fmaxf(x, y);
+        if (KEEP && halves != nullptr) (*halves)[i & 1] = fmaxf((*halves)[i & 1], y);
+      }
+    ran(x);
+  }
+  if (KEEP)
+    for (; runs.slots > 0; --runs.slots, slots += threads, most = LP_LEAST) *slots = most;
+}
+
+// The keys (count[0] of them) of the elements of `from` or more, by a warp for its threads first + lane: the
+// vectors of the runs whose maxima are as large are spread over its lanes, so that one latency
+// covers most rows. who: 64 ints of the warp's own.
+template <typename E>
+__device__ __forceinline__ void lp_collect(const LpRow<E>& row, float from, const LpRuns& runs, const float* slots, int first,
+                                           int threads, uint64_t* keys, int* count, int* who) {
   const int lane = threadIdx.x & 31;
   auto push = [&](float y, int i) {
     const int at = atomicAdd(count, 1);
     if (at < LP_ROOM) keys[at] = lp_key(y, i);
   };
-  const bool mine_too = mine >= from;
-  const uint32_t some = __ballot_sync(0xffffffffu, mine_too);
-  if (mine_too) who[__popc(some & ((1u << lane) - 1u))] = first + lane;
-  __syncwarp();
-  const unsigned each = static_cast<unsigned>(row.vecs + stride - 1) / static_cast<unsigned>(stride);
-  const unsigned all = __popc(some) * each;
-  for (unsigned i = lane; i < all; i += 32) {
-    const unsigned q = i / each;
-    const int v = who[q] + stride * static_cast<int>(i - q * each);
-    if (v >= row.vecs) continue;
-    const uint4 u = get(v);
-    if (LpVec<E>::largest(u) >= from) {
+  const unsigned each = LP_U * runs.per;
+  int have = 0;
+  for (int s = 0; s <= runs.slots; ++s) {
+    if (s == runs.slots || have > 32) {
+      __syncwarp();
+      for (unsigned i = lane; i < have * each; i += 32) {
+        const unsigned q = i / each;
+        const int v = (who[q] & 0xffff) + threads * static_cast<int>((who[q] >> 16) * each + (i - q * each));
+        if (v >= row.vecs) continue;
+        const uint4 u = __ldg(row.xv + v);
+        if (LpVec<E>::largest(u) >= from) {
 #pragma unroll
-      for (int j = 0; j < LpVec<E>::N; ++j) {
-        const float y = LpVec<E>::element(u, j);
-        if (y >= from) push(y, row.index(v) + j);
+          for (int j = 0; j < LpVec<E>::N; ++j) {
+            const float y = LpVec<E>::element(u, j);
+            if (y >= from) push(y, row.index(v) + j);
+          }
+        }
       }
+      __syncwarp();
+      have = 0;
+    }
+    if (s < runs.slots) {
+      const bool some = slots[s * threads + first + lane] >= from;
+      const uint32_t all = __ballot_sync(0xffffffffu, some);
+      if (some) who[have + __popc(all & ((1u << lane) - 1u))] = (first + lane) | s << 16;
+      have += __popc(all);
     }
   }
   if (first + lane < row.edges) {
@@ -421,9 +490,9 @@ template <typename E>
 __global__ void __launch_bounds__(LP_THREADS) k_logprobs_warp(LpArgs a) {
   __shared__ uint64_t keys[LP_WARPS][LP_ROOM];
   __shared__ uint64_t best[LP_WARPS][LP_BEST];
-  __shared__ int count[LP_WARPS], who[LP_WARPS][32];
+  __shared__ int count[LP_WARPS], who[LP_WARPS][64];
   __shared__ __align__(16) float maxima[LP_WARPS][64];
-  constexpr int U = 4;
+  __shared__ float slots[LP_WARPS][LP_SLOTS * 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_enter();
   const int64_t r = static_cast<int64_t>(blockIdx.x) * LP_WARPS + warp;
@@ -438,39 +507,21 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_warp(LpArgs a) {
   const float edge = lane < row.edges ? LpVec<E>::one(row.x + row.edge_at(lane)) : 0.f;
   LpAcc acc;
   acc.clear();
-  float first = LP_LEAST, other = LP_LEAST;  // maxima of even and odd vectors of the lane, the edge among the latter
-  int v = lane;
-  for (; v + (U - 1) * 32 < row.vecs; v += U * 32) {
-    uint4 u[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) u[i] = __ldg(row.xv + v + 32 * i);
-    acc.take<E, U>(u, a.c);
-    if (a.n > 0) {
-#pragma unroll
-      for (int i = 0; i < U; ++i) (i & 1 ? other : first) = fmaxf(i & 1 ? other : first, LpVec<E>::largest(u[i]));
-    }
-  }
-  for (int i = 0; v < row.vecs; v += 32, ++i) {
-    const uint4 u[1] = {__ldg(row.xv + v)};
-    acc.take<E, 1>(u, a.c);
-    (i & 1 ? other : first) = fmaxf(i & 1 ? other : first, LpVec<E>::largest(u[0]));
-  }
-  if (lane < row.edges) {
-    acc.one(edge, a.c);
-    other = fmaxf(other, edge);
-  }
+  const LpRuns runs(row.vecs, 32);
+  float halves[2] = {LP_LEAST, LP_LEAST};
+  if (a.n > 0) lp_pass<E, true>(row, acc, a.c, lane, 32, runs, slots[warp] + lane, &halves);
+  else lp_pass<E, false>(row, acc, a.c, lane, 32, runs, nullptr);
+  if (lane < row.edges) acc.one(edge, a.c);
   uint64_t list = 0;
   if (a.n > 0) {
-    // two groups a lane: the maxima of the vectors of one parity, and of the others (and of the edge)
-    maxima[warp][lane] = first;
-    maxima[warp][lane + 32] = other;
-    __syncwarp();
-    const uint32_t t = max(lp_nth(maxima[warp], a.n, first), lp_nth(maxima[warp], a.n, other));
+    // two groups a lane: its even vectors, and the others and the edge
+    if (lane < row.edges) halves[1] = fmaxf(halves[1], edge);
+    maxima[warp][lane] = halves[0];
+    maxima[warp][lane + 32] = halves[1];
     if (lane == 0) count[warp] = 0;
     __syncwarp();
-    lp_collect<E>(row, [&](int i) { return __ldg(row.xv + i); }, lp_from(t), acc.m, 0, 32, keys[warp],
-                  &count[warp], who[warp]);
-    __syncwarp();
+    const uint32_t t = max(lp_nth(maxima[warp], a.n, halves[0]), lp_nth(maxima[warp], a.n, halves[1]));
+    lp_collect<E>(row, lp_from(t), runs, slots[warp], 0, 32, keys[warp], &count[warp], who[warp]);
     list = count[warp] <= LP_ROOM ? lp_rank<E>(keys[warp], count[warp], a.n, best[warp]) : lp_sorted<E>(row, a.n);
   }
   lp_results<E>(a, r, row.x, token, logit, lp_reduce<32>(lp_sums(acc), a.c), list);
@@ -500,8 +551,8 @@ __device__ __forceinline__ void lp_cluster_arrive() { asm volatile("barrier.clus
 __device__ __forceinline__ void lp_cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
 template <typename E, int W>
-__global__ void __launch_bounds__(32 * W, LP_RESIDENT / W) k_logprobs_cluster(LpArgs a, int S) {
-  constexpr int U = 4, THREADS = 32 * W;
+__global__ void __launch_bounds__(32 * W, LP_RESIDENT(W) / W) k_logprobs_cluster(LpArgs a, int S) {
+  constexpr int THREADS = 32 * W;
   __shared__ uint64_t keys[LP_ROOM];
   __shared__ uint64_t from_ranks[LP_CLUSTER * LP_BEST];
   __shared__ uint64_t best[LP_BEST];
@@ -509,7 +560,8 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT / W) k_logprobs_cluster(Lp
   __shared__ __align__(16) float mine_max[64], maxima[64];  // of the block's groups, and of all
   __shared__ uint32_t nth;
   __shared__ uint64_t rank_m[LP_CLUSTER], rank_zw[LP_CLUSTER];
-  __shared__ int collected, who[W][32];
+  __shared__ int collected, who[W][64];
+  __shared__ float slots[LP_SLOTS * THREADS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = S > 1 ? static_cast<int>(lp_cluster_rank()) : 0;
   pdl_enter();
@@ -527,25 +579,9 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT / W) k_logprobs_cluster(Lp
   const float logit = rank == 0 && warp == 0 ? LpVec<E>::one(row.x + token) : 0.f;
   LpAcc acc;
   acc.clear();
-  int v = tid;
-  for (; v + (U - 1) * THREADS < row.vecs; v += U * THREADS) {
-    uint4 u[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) u[i] = __ldg(row.xv + v + i * THREADS);
-    acc.take<E, U>(u, a.c);
-  }
-  if (v < row.vecs) {  // what is left, its loads in flight together
-    uint4 u[U - 1];
-#pragma unroll
-    for (int i = 0; i < U - 1; ++i)
-      if (v + i * THREADS < row.vecs) u[i] = __ldg(row.xv + v + i * THREADS);
-#pragma unroll
-    for (int i = 0; i < U - 1; ++i)
-      if (v + i * THREADS < row.vecs) {
-        const uint4 w[1] = {u[i]};
-        acc.take<E, 1>(w, a.c);
-      }
-  }
+  const LpRuns runs(row.vecs, THREADS);
+  if (a.n > 0) lp_pass<E, true>(row, acc, a.c, tid, THREADS, runs, slots + tid);
+  else lp_pass<E, false>(row, acc, a.c, tid, THREADS, runs, nullptr);
   if (tid < row.edges) acc.one(edge, a.c);
   LpSums s = lp_reduce<32>(lp_sums(acc), a.c);
   if (lane == 0) warp_sums[warp] = s;
@@ -577,8 +613,7 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT / W) k_logprobs_cluster(Lp
     }
     __syncthreads();
     const float from = lp_from(nth);
-    lp_collect<E>(row, [&](int i) { return __ldg(row.xv + i); }, from, acc.m, warp * 32, THREADS, keys, &collected,
-                  who[warp]);
+    lp_collect<E>(row, from, runs, slots, warp * 32, THREADS, keys, &collected, who[warp]);
     __syncthreads();
     if (warp == 0) list = collected <= LP_ROOM ? lp_rank<E>(keys, collected, a.n, best) : lp_sorted<E>(row, a.n);
   }
@@ -663,13 +698,16 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
       DM_CUDA_CHECK(launch_pdl(warp_rows, dim3(static_cast<unsigned>((T + LP_WARPS - 1) / LP_WARPS)), dim3(LP_THREADS), 0, s, a));
       return DECOMOE_OK;
     }
-    // A block per row: of four warps (twelve rows at a time on an SM) or of eight, whichever leaves fewer
-    // places empty in its last turn.
+    // A block per row: of four warps (twelve rows at a time on an SM) where there are rows for half of the
+    // SMs' places and a row is not long, else of four or of eight, whichever leaves fewer
+    // places empty in its last turn (1552 rows of 64 KB 20 and 23 us, 5947 of 25 KB 60 and 71, 2000 of
+    // 302 KB 139 and 113, 700 of 64 KB 16 and 14).
     auto full = [&](int warps) {
-      const int64_t at_once = sms * (LP_RESIDENT / warps);
+      const int64_t at_once = sms * (LP_RESIDENT(warps) / warps);
       return static_cast<double>(T) / static_cast<double>((T + at_once - 1) / at_once * at_once);
     };
-    if (T >= 2 * sms && full(4) >= full(8)) {
+    const bool four = row_bytes <= 65536 ? T >= 6 * sms : full(4) >= full(8);
+    if (T >= 2 * sms && four) {
       DM_CUDA_CHECK(launch_pdl(many, dim3(static_cast<unsigned>(T)), dim3(128), 0, s, a, 1));
       return DECOMOE_OK;
     }

@@ -8,13 +8,44 @@
 
 namespace decomoe {
 
+// The tiles (32 rows of a KV head) of all requests are numbered and divided evenly among the
+// warps as in paged_attention.cu, whose joins of cut pairs this shares (paged_share.cuh): sixteen
+// warps of 128 registers on every SM (eight where 16 query heads share a tile), each with a ring of two
+// tiles of its own, filled by bulk copies, one for as many rows as lie in one page.
+//
+// out = sum_j p_j v_j / sum_j p_j with p_j = exp(scale q k_j - m), k = low + step code and the same
+// for v, group by group of features:
+//   q k_j = sum_g step_jg (sum_f q_f code_jf) + low_jg (sum_f q_f)
+//   sum_j p_j v_jf = sum_j (p_j step_jg) code_jf + sum_j p_j low_jg
+// so codes are never turned into values. Both inner sums run transposed on the tensor cores
+// (mma.m16n8k16, fp16 in, fp32 accumulate: 16 keys, or features, by 8 queries). A code masked in
+// place has the bits of the fp16 number code 2^-24 or code 2^-20, which the products take as they
+// are: one operation makes two operands, and nothing is rounded or subtracted. Queries are
+// scaled into fp16's range per row, where their eight digits are exact (but below 2^-27 of the row's
+// largest). p step is rounded to fp16 (2^-11 of it at most; bf16, as the bf16 cache has it, would be
+// 2^-8), scaled so that the largest step seen stays in range. low (sum q) is one more product, with
+// the sum as three bf16 numbers; p low, sums, maxima and outputs are fp32.
+//
+// Bound: instructions. 96 requests of 2000 to 16385 rows (153 MB) 39 us, 3.9 TB/s: copies
+// alone take 29 + 7 us of start and joins; of 590 instructions a tile 192 unpack codes on a pipe of half
+// rate and 34 are products, issue slots are 60 % busy. The bf16 cache takes 95 us. One request of 2049 rows
+// 10.2 us, all of it latency (scan, lookup, copy, a tile, join, the joining launch: each a
+// stretch of code that runs once).
+// Steps: codes to bf16 numbers by shift, mask and subtraction, one copy per eight rows, 304
+// blocks of eight warps 74 us; (code - 8) / 64 by one multiply-add, tiles of 32 rows, maxima raised
+// rarely 55; fp16 subnormal operands, lookups eight tiles at a time 49; 152 blocks of sixteen warps, so
+// that the joining launch is programmatic and joins half as many pieces 40; fewer branches 39.
 constexpr int Q4A_KEYS = 32;     // rows of a tile
 constexpr int Q4A_SETS = Q4A_KEYS / 8;
+constexpr int Q4A_STAGES = 2;    // tiles of a warp's ring (three: no faster)
 constexpr int Q4A_BLOCKS = 160;  // of a launch, at most
 constexpr int q4a_warps(int NT) { return NT == 1 ? 16 : 8; }  // of a block, one block per SM: as many as their registers allow
-constexpr int Q4A_FEW = 8;       // warps of a block that get tiles where there are few
-constexpr int Q4A_EXTRA = 3;     // what a (request, KV head) pair costs beside its tiles, in tiles
-constexpr int q4a_stages(int D) { return 2; }
+// Warps of a block that get tiles where there are few: one request of 2049 rows over 33 blocks
+// of eight warps 10.2 us, over 17 of sixteen 11.0, over 130 of two (33 pieces a pair to join) 11.9.
+constexpr int Q4A_FEW = 8;
+// What a (request, KV head) pair costs beside its tiles, in tiles: 97 requests of 5 to 1553 rows
+// take 21.2 us with 1, 20.9 with 2, 21.2 with 3, 22.9 with 5.
+constexpr int Q4A_EXTRA = 3;
 
 // A tile: KEYS consecutive rows of a request from a multiple of KEYS on (so that eight rows
 // always lie together in a page), those that are hidden or past the length left out of
@@ -141,7 +172,7 @@ template <int D, int G, int NT>
 __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(PagedQ4Args a) {
   using L = Q4Tile<D, G>;
   constexpr int WARPS = q4a_warps(NT);
-  constexpr int STAGES = q4a_stages(D);
+  constexpr int STAGES = Q4A_STAGES;
   constexpr int STAGE = Q4A_SETS * L::BYTES;
   constexpr int SUB = Q4A_KEYS / 16;
   constexpr int BLK = D / 32;      // blocks of 32 features
@@ -677,7 +708,7 @@ int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const
   a.early = static_cast<float*>(ws);
   a.part = a.early + static_cast<size_t>(grid) * warps * piece;
   a.info = reinterpret_cast<int4*>(a.part + static_cast<size_t>(grid) * 2 * piece);
-  const size_t smem = static_cast<size_t>(warps) * q4a_stages(D) * Q4A_SETS * q4_tile_bytes(D, group) +
+  const size_t smem = static_cast<size_t>(warps) * Q4A_STAGES * Q4A_SETS * q4_tile_bytes(D, group) +
                       2 * (static_cast<size_t>(B) + 1) * sizeof(int);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   auto go = [&](auto main, auto join) -> int {

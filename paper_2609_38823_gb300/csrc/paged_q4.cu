@@ -1,6 +1,12 @@
 // A paged key-value cache in 4 bits: new rows quantised into their slots, and rows
 // read back in bf16 (decoding on the text-only cache, DecoMoE Section 3.2 and Algorithm
 // 2, last step, with a cache of a quarter of the size).
+//
+// Bound: memory for long calls, launches for a decode batch. 16381 rows of 8 heads of 64: store
+// 13.5 us, 3.3 TB/s (its pool lies in L2; 595 instructions for a row's 1024 values, as many as there are places
+// for, is what remains), read 9.6 us, 4.6 TB/s; 23 rows of 4 heads of 128: 2.3 and 1.7 us. The
+// first store divided twice a value and found its row by 64-bit division: 33 us; ties between two codes by exact
+// remainders, in a branch that 40 % of the warps took: 18.5.
 #include "paged_q4.cuh"
 
 namespace decomoe {
