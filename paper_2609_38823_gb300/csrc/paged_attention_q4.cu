@@ -646,7 +646,7 @@ int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const
   // a length rounded up to a tile of (at most) 32 keys is counted in 32 bits
   DM_ARG_CHECK(max_pages >= 0 && max_pages <= (INT_MAX - 31) / page_size,
                "paged_attention_q4: max_pages * page_size must be at most 2^31 - 32");
-  const int64_t page = Hkv * (page_size / 8) * q4_tile_bytes(D, group);
+  const int64_t page = q4_tile_bytes(D, group) * (page_size / 8) * Hkv;
   DM_ARG_CHECK(page_stride >= page && page_stride % 16 == 0,
                "paged_attention_q4: page_stride below a page's bytes, or no multiple of 16");
   DM_ARG_CHECK(q_stride >= static_cast<int64_t>(Hq) * D && q_stride % 8 == 0,

@@ -209,7 +209,7 @@ static int q4_rows(const char* name, const void* k, int64_t k_row_stride, const 
   DM_ARG_CHECK(N >= 0 && N <= INT_MAX && Hkv >= 1 && Hkv <= 1024, "%s: bad sizes", name);
   DM_ARG_CHECK(page_size >= 8 && (page_size & (page_size - 1)) == 0, "%s: page_size must be a power of two, 8 at least", name);
   DM_ARG_CHECK(num_pages >= 0 && num_pages <= INT_MAX / page_size, "%s: num_pages * page_size must be below 2^31", name);
-  const int64_t page = Hkv * (page_size / 8) * q4_tile_bytes(D, group);
+  const int64_t page = q4_tile_bytes(D, group) * (page_size / 8) * Hkv;
   DM_ARG_CHECK(page_stride >= page && page_stride % 16 == 0, "%s: page_stride below a page's bytes, or no multiple of 16", name);
   const int64_t width = static_cast<int64_t>(Hkv) * D;
   DM_ARG_CHECK(k_row_stride >= width && v_row_stride >= width && k_row_stride % 8 == 0 && v_row_stride % 8 == 0,
@@ -232,7 +232,7 @@ static int q4_rows(const char* name, const void* k, int64_t k_row_stride, const 
 }
 
 static Bytes q4_pool(const void* pages, int64_t num_pages, int page_size, int64_t page_stride, int Hkv, int D, int group) {
-  const int64_t page = Hkv * (page_size / 8) * q4_tile_bytes(D, group);
+  const int64_t page = q4_tile_bytes(D, group) * (page_size / 8) * Hkv;
   return {pages, num_pages == 0 ? 0 : static_cast<size_t>((num_pages - 1) * page_stride + page)};
 }
 

@@ -126,6 +126,20 @@ def test_logprobs_arguments():
     assert call(T=0, x=None) == dm.DECOMOE_OK
 
 
+@off_gpu
+def test_pages_whose_size_passes_32_bits():
+    """1024 heads of 2^27 tiles: 2^37 tiles a page, which no stride given here holds."""
+    for ps in (1 << 25, 1 << 30):
+        for read in (False, True):
+            assert _rows_call(read, hkv=1024, ks=1 << 17, vs=1 << 17, pages=1, ps=ps, stride=1 << 31) == dm.DECOMOE_ERR_INVALID_ARG
+            assert b"page_stride" in dm.lib().decomoe_last_error()
+        p = [_p(a) for a in _places("q pages table lens out ws").values()]
+        assert dm.lib().decomoe_paged_attention_q4(p[0], 1 << 17, 1, p[1], 1, ps, 1 << 31, 64, p[2], 1, p[3], None, None, 1024, 1024,
+                                                   128, 0.0, p[4], p[5], 1 << 31, None, None) == dm.DECOMOE_ERR_INVALID_ARG
+        assert b"page_stride" in dm.lib().decomoe_last_error()
+    assert dm.decomoe_paged_q4_page_bytes(1 << 30, 1024, 128, 64) == 1152 << 37
+
+
 def test_page_bytes():
     assert dm.decomoe_paged_q4_page_bytes(16, 4, 128, 64) == 4 * 2 * 1152
     assert dm.decomoe_paged_q4_page_bytes(8, 1, 64, 32) == 640
