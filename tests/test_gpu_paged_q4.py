@@ -450,6 +450,44 @@ def test_scale_streams_and_the_same_bits_again():
         assert torch.equal(again, out)
 
 
+def _job(lens, seed):
+    """run(n, stream): n rounds of all four calls on tensors of the job's own, their results stacked."""
+    q, pool, table = _case(lens, 16, 2, 128, 64, 16, seed)
+    k, v = _rows(3, 2, 128, seed + 10).to(DEV), _rows(3, 2, 128, seed + 20).to(DEV)
+    x = torch.randn(5, 40001, generator=torch.Generator().manual_seed(seed)).to(DEV)
+    q, table, seq, where, tokens = q.to(DEV), _i32(table), _i32(lens), _i32([2, 9, 15]), _i32([0, 7, 40000, -1, 3])
+    ws = dm.workspace(dm.decomoe_paged_attention_q4_workspace_bytes(len(lens), 16, 2, 128), DEV)
+    scratch = _pool(1, 16, 2, 128, 64)
+
+    def outputs(n):
+        bf = dict(dtype=torch.bfloat16, device=DEV)
+        return torch.zeros(n, len(lens), 16, 128, **bf), torch.zeros(n, 2, 3, 2, 128, **bf), torch.zeros(n, 5, device=DEV)
+
+    def run(to, stream):
+        for out, kv, lp in zip(*to):
+            dm.decomoe_paged_attention_q4(q, pool, table, seq, out, ws, stream=stream)
+            dm.decomoe_paged_append_q4(k, v, where, scratch, stream=stream)
+            dm.decomoe_paged_read_q4(where, scratch, kv[0], kv[1], stream=stream)
+            dm.decomoe_token_logprobs(x, tokens, lp, stream=stream)
+
+    return outputs, run
+
+
+def test_calls_at_once_on_two_streams():
+    """A workspace and a pool each, many calls under way together: every result as if it were alone."""
+    jobs = [_job([4000, 9, 700], 20), _job([2500] * 7, 60)]
+    alone, many = [o(1) for o, _ in jobs], [o(40) for o, _ in jobs]
+    for (_, run), to in zip(jobs, alone):
+        run(to, None)
+    torch.cuda.synchronize()
+    for (_, run), to, side in zip(jobs, many, [torch.cuda.Stream() for _ in jobs]):
+        run(to, side)
+    torch.cuda.synchronize()
+    for a, b in zip(alone, many):
+        for one, got in zip(a, b):
+            assert torch.equal(got, one.expand_as(got))
+
+
 def test_a_wait_that_ends_in_time_leaves_no_mark():
     """The smallest time limit that a call can meet is not taken for a fault: copies arrive."""
     lens = [2000] * 8
