@@ -26,15 +26,17 @@ namespace decomoe {
 // 2^-8), scaled so that the largest step seen stays in range. low (sum q) is one more product, with
 // the sum as three bf16 numbers; p low, sums, maxima and outputs are fp32.
 //
-// Bound: instructions. 96 requests of 2000 to 16385 rows (153 MB) 39 us, 3.9 TB/s: copies
-// alone take 29 + 7 us of start and joins; of 590 instructions a tile 192 unpack codes on a pipe of half
-// rate and 34 are products, issue slots are 60 % busy. The bf16 cache takes 95 us. One request of 2049 rows
-// 10.2 us, all of it latency (scan, lookup, copy, a tile, join, the joining launch: each a
-// stretch of code that runs once).
+// Bound: 96 requests of 2000 to 16385 rows (153 MB) 38 us, 4.0 TB/s: 4 us until the first copies are on their way
+// (lengths, their sum, search, tables), 24 us of copies at 6.3 TB/s, 2.5 us of joins in the blocks and 4 for the joining
+// launch; without a tile's arithmetic it would take 34. Of 590 instructions a tile 192 unpack codes on a pipe of
+// half rate and 34 are products, issue slots are 60 % busy. The bf16 cache takes 95 us. One request of 2049 rows
+// 10.2 us, all of it latency: 2.5 us to its first copies, 1 for them, 1.5 for a tile, 2 for the join in the block, 3
+// for the launch that joins blocks, each a stretch of code that runs once.
 // Steps: codes to bf16 numbers by shift, mask and subtraction, one copy per eight rows, 304
 // blocks of eight warps 74 us; (code - 8) / 64 by one multiply-add, tiles of 32 rows, maxima raised
 // rarely 55; fp16 subnormal operands, lookups eight tiles at a time 49; 152 blocks of sixteen warps, so
-// that the joining launch is programmatic and joins half as many pieces 40; fewer branches 39.
+// that the joining launch is programmatic and joins half as many pieces 40; fewer branches 39; a search by half
+// warps, tables and first queries brought into L2 ahead 37.9.
 constexpr int Q4A_KEYS = 32;     // rows of a tile
 constexpr int Q4A_SETS = Q4A_KEYS / 8;
 constexpr int Q4A_STAGES = 2;    // tiles of a warp's ring (three: no faster)
@@ -192,13 +194,14 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
   if (lane < STAGES) mbar_init(smem_u32(&bars[warp][lane]), 1);
   fence_mbar_init();
   pdl_enter();
-  const PgaPlan plan = pga_begin<Q4aTiles, D, WARPS, Q4A_FEW>(a, pre, nz);
+  const PgaPlan plan = pga_begin<Q4aTiles, D, WARPS, Q4A_FEW, true>(a, pre, nz);
   const int me = blockIdx.x * plan.active + min(warp, plan.active);
-  // lane 0 seeks the start of this warp's share, lane 1 that of the next one's
+  // the lower half of the warp seeks the start of its share, the upper half that of the next one's
   PgaWalk<Q4aTiles> seek;
-  const int from = plan.place(warp < plan.active ? me + (lane & 1) : me);
-  const int first = from < plan.total ? seek.seek(plan, from) : pre[a.B] * a.hv;
-  const int r0 = __shfl_sync(0xffffffffu, first, 0), r1 = __shfl_sync(0xffffffffu, first, 1);
+  const int from = plan.place(warp < plan.active ? me + (lane >> 4) : me);
+  const int found = seek.seek_by_halves(plan, from);
+  const int first = from < plan.total ? found : pre[a.B] * a.hv;
+  const int r0 = __shfl_sync(0xffffffffu, first, 0), r1 = __shfl_sync(0xffffffffu, first, 16);
   const int gs = a.hq / a.hkv;
 
   uint8_t* ring = q4a_smem + warp * RING;
@@ -213,6 +216,14 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
     int b = __shfl_sync(0xffffffffu, seek.b, 0), h = __shfl_sync(0xffffffffu, seek.h, 0);  // of the piece
     const int t0 = __shfl_sync(0xffffffffu, seek.t, 0);
     bool began = t0 > 0;  // the piece's pair began in an earlier share
+    // the first queries on their way into L2 while the pages are looked up (96 requests 39.0 -> 38.5 us, 97
+    // short ones 20.4 -> 20.15; with 16 queries a tile 13.3 -> 13.6, so not there)
+    if constexpr (NT == 1) {
+      const int g = a.qt == 1 ? h : h / a.qt, row = (h - g * a.qt) * ROWS + (lane >> 2);
+      if (row < gs)
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(a.q + b * a.q_stride + static_cast<int64_t>(g * gs + row) * D +
+                                                      (lane & 3) * (D / 4)));
+    }
     const int set = lane & (Q4A_SETS - 1), mine_of = lane / Q4A_SETS;
     Q4aLook look = {b, h, t0, pre[b + 1] - pre[b], n, 0, 0, 0};
     // sets of a tile in one page, which one copy takes: those of this lane's, and whether it is the first

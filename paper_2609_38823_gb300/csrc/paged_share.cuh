@@ -146,7 +146,22 @@ struct PgaWalk {
       if (plan.places(mid) <= p) lo = mid;
       else hi = mid;
     }
-    b = lo;
+    return at(plan, lo, p);
+  }
+  // The same by all lanes of a warp, a place for each half of it (p <= total, where it is meaningless).
+  __device__ __forceinline__ int seek_by_halves(const PgaPlan& plan, int p) {
+    const int lane = threadIdx.x & 15;
+    int lo = 0;
+    for (int n = plan.B; n > 1;) {
+      n = (n + 15) >> 4;
+      const int b = lo + lane * n;
+      const uint32_t le = __ballot_sync(0xffffffffu, b < plan.B && plan.places(b) <= p);
+      lo += (__popc(le & 0xffffu << (threadIdx.x & 16)) - 1) * n;
+    }
+    return at(plan, lo, p);
+  }
+  __device__ __forceinline__ int at(const PgaPlan& plan, int request, int p) {
+    b = request;
     tiles = plan.pre[b + 1] - plan.pre[b];
     const int in = p - plan.places(b), each = tiles + plan.extra;
     h = in / each;
@@ -168,8 +183,9 @@ struct PgaWalk {
 // The start of a launch, by every thread of a block: the tiles of every request added up
 // in pre and nz (shared memory, [B + 1] each), zeros for the requests that see nothing, and
 // the division of the tiles among the launch's warps: W of every block, or where FEW is not 0 and there are
-// fewer tiles than that, the first FEW or more of every block.
-template <class Tiles, int D, int W, int FEW = 0>
+// fewer tiles than that, the first FEW or more of every block. TABLE: the blocks bring the tables' lines into L2
+// together, ahead of the lookups.
+template <class Tiles, int D, int W, int FEW = 0, bool TABLE = false>
 __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int* nz) {
   constexpr int THREADS = 32 * W;
   __shared__ int scan_w[2][W];
@@ -181,9 +197,15 @@ __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int
     bool bad = false;
     int sum = 0, some = 0;
     for (int b = b0; b < b1; ++b) {
-      const int n = Tiles::count(pga_request(a, b, &bad));
+      const PgaReq r = pga_request(a, b, &bad);
+      const int n = Tiles::count(r);
       pre[b + 1] = n;
       sum += n;
+      if (TABLE) {
+        const int32_t* row = a.table + b * a.max_pages;
+        const int used = static_cast<int>((static_cast<int64_t>(r.seen) + r.hc + (1 << a.shift) - 1) >> a.shift);
+        for (int i = blockIdx.x * 32; i < used; i += gridDim.x * 32) asm volatile("prefetch.global.L2 [%0];" ::"l"(row + i));
+      }
       some += n > 0;
     }
     if (bad && blockIdx.x == 0) report_status(a.status, DECOMOE_ERR_BAD_INPUT);
