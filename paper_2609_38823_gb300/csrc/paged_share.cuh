@@ -189,7 +189,8 @@ template <class Tiles, int D, int W, int FEW = 0, bool TABLE = false>
 __device__ __forceinline__ PgaPlan pga_begin(const PagedCommon& a, int* pre, int* nz) {
   constexpr int THREADS = 32 * W;
   __shared__ int scan_w[2][W];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // (warp numbers that the compiler sees to be the same in all lanes spare branches and joins of lanes)
+  const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
   // ---- tiles of every request, added up
   {
     const int per = (a.B + THREADS - 1) / THREADS;
@@ -371,7 +372,7 @@ __global__ void __launch_bounds__(32 * PGM_WARPS) k_paged_join(PagedCommon a) {
   __shared__ __align__(16) float so[PGM_WARPS][D];
   __shared__ float factor[PGM_WARPS][BLOCKS];
   pdl_trigger();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);
   const int r = warp / PER, s = warp % PER;
   auto piece = [&](int i) {
     return a.part + ((static_cast<int64_t>(blockIdx.x + i) * 2 + (i == 0 ? 1 : 0)) * ROWS + r) * pga_row(D);
