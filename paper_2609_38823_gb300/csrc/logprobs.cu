@@ -10,17 +10,25 @@ namespace decomoe {
 // With c = scale log2(e) and m the maximum of the elements x seen so far, a thread keeps the
 // sums z of 2^d and w of 2^d d over d = (x - m) c, rescaled where m grows (pairs of elements in
 // packed fp32 operations); threads, warps and blocks are added up in a fixed order against the
-// largest m. Then ln p(x) = (x - m) scale - ln z and the entropy is ln z - ln 2 w / z. Elements count as -2^100 at least, so that
-// masked ones (-inf, or a type's lowest value) need no case of their own: their 2^d is 0 and their
-// product with d finite. A row whose maximum is not below 2^97 in size (all masked, infinite,
-// enormous) is computed again with every case, by one warp.
+// largest m. Then ln p(x) = (x - m) scale - ln z and the entropy is ln z - ln 2 w / z. Elements
+// count as -2^100 at least, so that masked ones (-inf, or a type's lowest value) need no case of
+// their own: their 2^d is 0 and their product with d finite. A row whose maximum is not below 2^97
+// in size (all masked, infinite, enormous) is computed again with every case, by one warp.
 //
 // The n <= 32 best: the threads fall into 64 groups, and the n-th largest of the groups'
-// maxima bounds the n-th largest element from below, since groups have no element in common; about n to
-// 1.5 n elements reach it. The vectors of the few runs of a thread's vectors whose maxima do are read again, elements that reach it collected as 64-bit keys of value and index, all
+// maxima bounds the n-th largest element from below, since groups have no element in common; about
+// n to 1.5 n elements reach it. The vectors of the few runs of a thread's vectors whose maxima
+// reach it are read again, elements that do are collected as 64-bit keys of value and index, all
 // different, and ranked by counting; ties go to the lowest index, and no order of execution
-// shows. Where more are collected than there is room for (rows of equal values), a warp reads the row
-// again and keeps the n best sorted in its lanes.
+// shows. Where more are collected than there is room for (rows of equal values), a warp reads the
+// row again and keeps the n best sorted in its lanes.
+//
+// Bound: memory for many long rows, else latency and instructions of the best. 16384 rows of 64 KB 152 us
+// without alternatives (all of the measured copy rate), 180 with five: while a row's best are found (a third of its
+// time) its block loads nothing. One row of 64 KB 3.3 and 5.9 us over a cluster of eight blocks. 5238 rows of 4 KB,
+// a warp each, 7.6 us without and 21 with 32. Steps of 16384 rows with five: a pass for the sums and one for the
+// best 444 us; both in one, blocks per row 203; runs of vectors instead of all vectors read again 191; warp
+// numbers that are uniform to the compiler 186; the groups' n-th largest bit by bit, shifts for divisions 180.
 constexpr int LP_THREADS = 256;
 constexpr int LP_WARPS = LP_THREADS / 32;
 constexpr int LP_BEST = 32;
@@ -247,11 +255,12 @@ struct LpRow {
 constexpr int LP_U = 4;
 constexpr int LP_SLOTS = 8;
 struct LpRuns {
-  int per, slots;  // batches of a run, and runs
+  int per, shift, slots;  // batches of a run (1 << shift), and runs
   __device__ __forceinline__ LpRuns(int vecs, int threads) {
     const int batches = (vecs + threads * LP_U - 1) / (threads * LP_U);
-    per = (batches + LP_SLOTS - 1) / LP_SLOTS;
-    slots = per > 0 ? (batches + per - 1) / per : 0;
+    shift = 32 - __clz((batches - 1) / LP_SLOTS);
+    per = 1 << shift;
+    slots = (batches + per - 1) >> shift;
   }
 };
 
@@ -313,14 +322,15 @@ __device__ __forceinline__ void lp_collect(const LpRow<E>& row, float from, cons
     const int at = atomicAdd(count, 1);
     if (at < LP_ROOM) keys[at] = lp_key(y, i);
   };
-  const unsigned each = LP_U * runs.per;
+  static_assert(LP_U == 4, "a run is 4 << shift vectors");
+  const unsigned each = LP_U << runs.shift;
   int have = 0;
   for (int s = 0; s <= runs.slots; ++s) {
     if (s == runs.slots || have > 32) {
       __syncwarp();
       for (unsigned i = lane; i < have * each; i += 32) {
-        const unsigned q = i / each;
-        const int v = (who[q] & 0xffff) + threads * static_cast<int>((who[q] >> 16) * each + (i - q * each));
+        const unsigned q = i >> (runs.shift + 2);
+        const int v = (who[q] & 0xffff) + threads * static_cast<int>((who[q] >> 16) * each + (i & (each - 1)));
         if (v >= row.vecs) continue;
         const uint4 u = __ldg(row.xv + v);
         if (LpVec<E>::largest(u) >= from) {
@@ -415,23 +425,17 @@ __device__ __forceinline__ uint32_t lp_order(float x) {
   const uint32_t u = __float_as_uint(x);
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
-// The n-th largest of 64 values is the largest that n of them reach: of the 64 / W values that warp w
-// of W looks after the largest such one (0: none), each compared by W / 2 lanes with a share of the others.
-template <int W>
-__device__ __forceinline__ uint32_t lp_nth(const float* values, int n, int w) {
-  constexpr int MINE = 64 / W, PARTS = 32 / MINE, EACH = 16 / PARTS;
-  const int lane = threadIdx.x & 31;
-  const float mine = values[w * MINE + lane % MINE];
-  const float4* v = reinterpret_cast<const float4*>(values) + lane / MINE * EACH;
-  int reach = 0;
-#pragma unroll 4
-  for (int i = 0; i < EACH; ++i) {
-    const float4 u = v[i];
-    reach += (u.x >= mine) + (u.y >= mine) + (u.z >= mine) + (u.w >= mine);
+// A bound of the n-th largest of 64 values from below, two a lane: its upper 16 bits, found bit by bit
+// between those of the least and of the largest value (seven steps or so).
+__device__ __forceinline__ uint32_t lp_nth(float a, float b, int n) {
+  const uint32_t x = lp_order(a) >> 16, y = lp_order(b) >> 16;
+  uint32_t at = __reduce_min_sync(0xffffffffu, min(x, y));
+  const uint32_t range = __reduce_max_sync(0xffffffffu, max(x, y)) - at;
+  for (uint32_t step = range == 0 ? 0 : 1u << (31 - __clz(range)); step != 0; step >>= 1) {
+    const uint32_t to = at + step;
+    if (__popc(__ballot_sync(0xffffffffu, x >= to)) + __popc(__ballot_sync(0xffffffffu, y >= to)) >= n) at = to;
   }
-#pragma unroll
-  for (int o = MINE; o < 32; o <<= 1) reach += __shfl_xor_sync(0xffffffffu, reach, o);
-  return __reduce_max_sync(0xffffffffu, reach >= n ? lp_order(mine) : 0u);
+  return at << 16;
 }
 // The least value to collect: the bound, or everything finite where some groups hold nothing plain.
 __device__ __forceinline__ float lp_from(uint32_t nth) {
@@ -497,7 +501,6 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_warp(LpArgs a) {
   __shared__ uint64_t keys[LP_WARPS][LP_ROOM];
   __shared__ uint64_t best[LP_WARPS][LP_BEST];
   __shared__ int count[LP_WARPS], who[LP_WARPS][64];
-  __shared__ __align__(16) float maxima[LP_WARPS][64];
   __shared__ float slots[LP_WARPS][LP_SLOTS * 32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_enter();
@@ -522,11 +525,9 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_warp(LpArgs a) {
   if (a.n > 0) {
     // two groups a lane: its even vectors, and the others and the edge
     if (lane < row.edges) halves[1] = fmaxf(halves[1], edge);
-    maxima[warp][lane] = halves[0];
-    maxima[warp][lane + 32] = halves[1];
     if (lane == 0) count[warp] = 0;
     __syncwarp();
-    const uint32_t t = max(lp_nth<2>(maxima[warp], a.n, 0), lp_nth<2>(maxima[warp], a.n, 1));
+    const uint32_t t = lp_nth(halves[0], halves[1], a.n);
     lp_collect<E>(row, lp_from(t), runs, slots[warp], 0, 32, keys[warp], &count[warp], who[warp]);
     list = count[warp] <= LP_ROOM ? lp_rank<E>(keys[warp], count[warp], a.n, best[warp]) : lp_sorted<E>(row, a.n);
   }
@@ -564,7 +565,6 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT(W) / W) k_logprobs_cluster
   __shared__ uint64_t best[LP_BEST];
   __shared__ LpSums warp_sums[W];
   __shared__ __align__(16) float mine_max[64], maxima[64];  // of the block's groups, and of all
-  __shared__ uint32_t nth;
   __shared__ uint64_t rank_m[LP_CLUSTER], rank_zw[LP_CLUSTER];
   __shared__ int collected, who[W][64];
   __shared__ float slots[LP_SLOTS * THREADS];
@@ -599,10 +599,7 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT(W) / W) k_logprobs_cluster
     float most = acc.m;
     for (int o = 1; o < lanes; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
     if (lane % lanes == 0) (S > 1 ? mine_max : maxima)[tid / lanes] = most;
-    if (tid == 0) {
-      collected = 0;
-      nth = 0;
-    }
+    if (tid == 0) collected = 0;
   }
   __syncthreads();
   if (S > 1) lp_cluster_wait();  // every block of the cluster is running
@@ -614,10 +611,7 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT(W) / W) k_logprobs_cluster
       lp_cluster_arrive();
       lp_cluster_wait();
     }
-    const uint32_t t = lp_nth<W>(maxima, a.n, warp);
-    if (lane == 0 && t != 0) atomicMax(&nth, t);
-    __syncthreads();
-    const float from = lp_from(nth);
+    const float from = lp_from(lp_nth(maxima[lane], maxima[lane + 32], a.n));
     lp_collect<E>(row, from, runs, slots, warp * 32, THREADS, keys, &collected, who[warp]);
     __syncthreads();
     if (warp == 0) {
