@@ -1,6 +1,7 @@
 // Log probabilities of given tokens from a model's logits, with each row's entropy and its
 // most probable alternatives: what a server returns beside the tokens it answers with
 // (the base model's last step, which the method leaves unchanged).
+#include <algorithm>
 #include <cfloat>
 
 #include "decomoe_internal.cuh"
@@ -700,16 +701,20 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
       DM_CUDA_CHECK(launch_pdl(warp_rows, dim3(static_cast<unsigned>((T + LP_WARPS - 1) / LP_WARPS)), dim3(LP_THREADS), 0, s, a));
       return DECOMOE_OK;
     }
-    // A block per row: of four warps (twelve rows at a time on an SM) where there are rows for half of the
-    // SMs' places and a row is not long, else of four or of eight, whichever leaves fewer
-    // places empty in its last turn (1552 rows of 64 KB 20 and 23 us, 5947 of 25 KB 60 and 71, 2000 of
-    // 302 KB 139 and 113, 700 of 64 KB 16 and 14).
-    auto full = [&](int warps) {
-      const int64_t at_once = sms * (LP_RESIDENT(warps) / warps);
-      return static_cast<double>(T) / static_cast<double>((T + at_once - 1) / at_once * at_once);
+    // A block per row, of four warps (twelve rows at a time on an SM) or of eight (five): whichever is sooner
+    // done by this estimate, in us. Full turns and the rest go at the copy rate, the rest at least as long as a
+    // block takes alone (a warp has 2 KB on their way in a us); a turn costs 4 us beside its bytes, and 4 for every
+    // time that a warp reads runs again (1.25 runs an alternative). Measured with four and with eight: 700 rows of
+    // 64 KB 16 and 14, 803 of 20 KB 8.2 and 10.6, 803 of 150 KB 28.6 and 33.8, 1552 of 64 KB 20 and 23, 2000 of 302
+    // KB 119 and 106, 4413 of 86 KB 88 and 96, 3419 of 307 KB with 32 alternatives 243 and 196.
+    auto estimate = [&](int warps) {
+      const int64_t at_once = sms * (LP_RESIDENT(warps) / warps), rest = T % at_once;
+      const double row = static_cast<double>(row_bytes), rate = 6.7e6, alone = 2048. * warps;
+      const double run = std::max<double>(LP_U, row / (16 * 32 * warps) / LP_SLOTS);  // vectors
+      return static_cast<double>(T - rest) * row / rate + (rest > 0 ? std::max(static_cast<double>(rest) * row / rate, row / alone) : 0.) +
+             (4. + 5. * a.n * run / (32 * warps)) * static_cast<double>((T + at_once - 1) / at_once);
     };
-    const bool four = row_bytes <= 65536 ? T >= 6 * sms : full(4) >= full(8);
-    if (T >= 2 * sms && four) {
+    if (T >= 2 * sms && estimate(4) < estimate(8)) {
       DM_CUDA_CHECK(launch_pdl(many, dim3(static_cast<unsigned>(T)), dim3(128), 0, s, a, 1));
       return DECOMOE_OK;
     }
