@@ -77,6 +77,26 @@ def test_parity(T, V, n, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,V,n", [(770, 4201, 32), (1900, 9001, 5), (400, 9003, 20), (1100, 20011, 0), (330, 40003, 32)])
+def test_a_block_per_row(T, V, n, dtype):
+    """Rows enough for a block of four or eight warps each; some masked in long stretches, some padding, unaligned."""
+    x, tokens = _logits(T, V + 3, dtype, T + V)
+    x[::3, 100:V // 2] = float("-inf")
+    x[5, 1:] = float("-inf")
+    tokens = torch.where(torch.arange(T) % 7 == 6, -1, tokens.clamp(max=V - 1)).to(I32)
+    x = x[:, 1:V + 1]
+    got = [None if t is None else t[tokens >= 0] for t in _run(_shifted(x), tokens.to(DEV), n)]
+    _compare(x[tokens >= 0], tokens[tokens >= 0].tolist(), got, n)
+
+
+def _shifted(x):
+    """On the GPU, as a slice of wider rows."""
+    wide = torch.zeros(x.shape[0], x.shape[1] + 3, dtype=x.dtype, device=DEV)
+    wide[:, 1:-2] = x.to(DEV)
+    return wide[:, 1:-2]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("off", range(9))
 def test_rows_at_any_alignment(dtype, off):
     """Rows inside wider ones, at every place of a 16-byte vector."""
