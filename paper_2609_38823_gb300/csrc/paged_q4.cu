@@ -2,11 +2,11 @@
 // read back in bf16 (decoding on the text-only cache, DecoMoE Section 3.2 and Algorithm
 // 2, last step, with a cache of a quarter of the size).
 //
-// Bound: memory for long calls, launches for a decode batch. 16381 rows of 8 heads of 64: store
-// 13.5 us, 3.3 TB/s (its pool lies in L2; 595 instructions for a row's 1024 values, as many as there are places
-// for, is what remains), read 9.6 us, 4.6 TB/s; 23 rows of 4 heads of 128: 2.3 and 1.7 us. The
-// first store divided twice a value and found its row by 64-bit division: 33 us; ties between two codes by exact
-// remainders, in a branch that 40 % of the warps took: 18.5.
+// Bound: instructions and latency for long calls, launches for a decode batch. 16381 rows of 8 heads of 64: store
+// 13.0 us, 3.4 TB/s (its pool lies in L2), read 9.25 us, 4.8 TB/s; 5000 rows of 8 heads of 128 in groups of 32: 8.2 and
+// 5.7 us; 23 rows of 4 heads of 128: 2.3 and 1.7 us. The first store divided twice a value and found its row by 64-bit
+// division: 33 us; ties between two codes by exact remainders, in a branch that 40 % of the warps took: 18.5; values one
+// at a time instead of in packed pairs 13.5, the read 9.6.
 #include "paged_q4.cuh"
 
 namespace decomoe {
@@ -59,6 +59,34 @@ __device__ __forceinline__ void q4_unpack8(const uint4& u, float (&x)[8]) {
   x[4] = bf16_lo(u.z), x[5] = bf16_hi(u.z), x[6] = bf16_lo(u.w), x[7] = bf16_hi(u.w);
 }
 
+// Two fp32 numbers at a time.
+__device__ __forceinline__ uint64_t q4_two(float a, float b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t q4_two(uint32_t a, uint32_t b) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ void q4_split(uint64_t v, uint32_t& a, uint32_t& b) { asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t q4_fma(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ uint64_t q4_mul(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t q4_add(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 __device__ __forceinline__ uint32_t q4_max2(uint32_t a, uint32_t b) {  // of two pairs of bf16 numbers, NaN where one is
   uint32_t r;
   asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -101,9 +129,12 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint4& u, uint32_t* params
   constexpr uint32_t HIGH = 0x4b400000u;
   const float inv = __frcp_rn(step);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float r = x[j] - lo, q = r * inv, t = fmaf(fmaf(-step, q, r), inv, q) + MAGIC;
-    code += __float_as_uint(t) * (1u << (4 * j));
+  for (int j = 0; j < 8; j += 2) {
+    const uint64_t r = q4_add(q4_two(x[j], x[j + 1]), q4_two(-lo, -lo)), q = q4_mul(r, q4_two(inv, inv));
+    const uint64_t t = q4_add(q4_fma(q4_fma(q4_two(-step, -step), q, r), q4_two(inv, inv), q), q4_two(MAGIC, MAGIC));
+    uint32_t t0, t1;
+    q4_split(t, t0, t1);
+    code += t0 * (1u << (4 * j)) + t1 * (16u << (4 * j));
   }
   return code - (HIGH + (HIGH << 4) + (HIGH << 8) + (HIGH << 12) + (HIGH << 16) + (HIGH << 20) + (HIGH << 24) + (HIGH << 28));
 }
@@ -154,16 +185,27 @@ __global__ void __launch_bounds__(Q4_THREADS) k_paged_append_q4(Q4Rows a, const 
 __device__ __forceinline__ uint4 q4_values8(uint32_t code, uint32_t params) {
   const float step = bf16_lo(params), lo = bf16_hi(params);
   float x[8];
+  const uint32_t high = code >> 16;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const float q = __uint_as_float(((code >> (4 * j)) & 15u) | 0x4b000000u) - 8388608.f;
-    x[j] = fmaf(step, q, lo);
+  for (int j = 0; j < 8; j += 2) {
+    // 2^23 + code 2^s of a code masked in place, back to the code
+    const uint32_t w = j < 4 ? code : high;
+    constexpr uint32_t BASE = 0x4b000000u;
+    const int s = 4 * (j & 3);
+    const float f = 1.f / (1 << s), f1 = f / 16.f;
+    const uint64_t q = q4_fma(q4_two((w & (15u << s)) | BASE, (w & (240u << s)) | BASE), q4_two(f, f1), q4_two(-8388608.f * f, -8388608.f * f1));
+    uint32_t a, b;
+    q4_split(q4_fma(q4_two(step, step), q, q4_two(lo, lo)), a, b);
+    x[j] = __uint_as_float(a);
+    x[j + 1] = __uint_as_float(b);
   }
   return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
 }
 
+// (sixteen blocks an SM, so 32 registers: with the 40 that it would take 9.8 us for 16381 rows, not 9.25. The store's 50
+// squeezed to 40 take 12.6 there, but 9.1, not 8.2, for 5000 rows of 8 heads of 128)
 template <int D, int G>
-__global__ void __launch_bounds__(Q4_THREADS) k_paged_read_q4(Q4Rows a, __nv_bfloat16* k, __nv_bfloat16* v) {
+__global__ void __launch_bounds__(Q4_THREADS, 16) k_paged_read_q4(Q4Rows a, __nv_bfloat16* k, __nv_bfloat16* v) {
   using L = Q4Lane<D, G>;
   using T = Q4Tile<D, G>;
   pdl_wait();
