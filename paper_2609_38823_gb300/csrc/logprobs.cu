@@ -95,7 +95,9 @@ struct LpVec;
 template <>
 struct LpVec<__nv_bfloat16> {
   static constexpr int N = 8;
-  static __device__ __forceinline__ uint32_t word(const uint4& u, int i) { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+  static __device__ __forceinline__ uint32_t word(const uint4& u, int i) {
+    return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w;
+  }
   static __device__ __forceinline__ uint4 raise(const uint4& u) {
     uint4 r;
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r.x) : "r"(u.x), "r"(0xf180f180u));
@@ -711,8 +713,9 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
       const int64_t at_once = sms * (LP_RESIDENT(warps) / warps), rest = T % at_once;
       const double row = static_cast<double>(row_bytes), rate = 6.7e6, alone = 2048. * warps;
       const double run = std::max<double>(LP_U, row / (16 * 32 * warps) / LP_SLOTS);  // vectors
-      return static_cast<double>(T - rest) * row / rate + (rest > 0 ? std::max(static_cast<double>(rest) * row / rate, row / alone) : 0.) +
-             (4. + 5. * a.n * run / (32 * warps)) * static_cast<double>((T + at_once - 1) / at_once);
+      const double last = rest > 0 ? std::max(static_cast<double>(rest) * row / rate, row / alone) : 0.;
+      const double turns = static_cast<double>((T + at_once - 1) / at_once);
+      return static_cast<double>(T - rest) * row / rate + last + (4. + 5. * a.n * run / (32 * warps)) * turns;
     };
     if (T >= 2 * sms && estimate(4) < estimate(8)) {
       DM_CUDA_CHECK(launch_pdl(many, dim3(static_cast<unsigned>(T)), dim3(128), 0, s, a, 1));

@@ -70,7 +70,9 @@ __device__ __forceinline__ uint64_t q4_two(uint32_t a, uint32_t b) {
   asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
   return r;
 }
-__device__ __forceinline__ void q4_split(uint64_t v, uint32_t& a, uint32_t& b) { asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v)); }
+__device__ __forceinline__ void q4_split(uint64_t v, uint32_t& a, uint32_t& b) {
+  asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
+}
 __device__ __forceinline__ uint64_t q4_fma(uint64_t a, uint64_t b, uint64_t c) {
   uint64_t r;
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
@@ -193,7 +195,8 @@ __device__ __forceinline__ uint4 q4_values8(uint32_t code, uint32_t params) {
     constexpr uint32_t BASE = 0x4b000000u;
     const int s = 4 * (j & 3);
     const float f = 1.f / (1 << s), f1 = f / 16.f;
-    const uint64_t q = q4_fma(q4_two((w & (15u << s)) | BASE, (w & (240u << s)) | BASE), q4_two(f, f1), q4_two(-8388608.f * f, -8388608.f * f1));
+    const uint64_t at = q4_two((w & (15u << s)) | BASE, (w & (240u << s)) | BASE);
+    const uint64_t q = q4_fma(at, q4_two(f, f1), q4_two(-8388608.f * f, -8388608.f * f1));
     uint32_t a, b;
     q4_split(q4_fma(q4_two(step, step), q, q4_two(lo, lo)), a, b);
     x[j] = __uint_as_float(a);

@@ -163,7 +163,7 @@ struct PgaWalk {
   __device__ __forceinline__ int at(const PgaPlan& plan, int request, int p) {
     b = request;
     tiles = plan.pre[b + 1] - plan.pre[b];
-    const int in = p - plan.places(b), each = tiles + plan.extra;
+    const int in = p - plan.places(b), each = max(tiles + plan.extra, 1);  // (p = total may lie behind an empty request)
     h = in / each;
     t = max(in - h * each - plan.extra, 0);
     return plan.pre[b] * plan.hv + h * tiles + t;

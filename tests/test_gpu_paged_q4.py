@@ -169,6 +169,23 @@ def test_read_values(d, group, n, hkv, ps):
     assert (got[:, 2 * hkv] == 7.0).all()
 
 
+@pytest.mark.parametrize("size", [1e-40, 1e-38, 1e-30, 1e30])
+def test_read_values_of_any_size(size):
+    """Steps and lows down to subnormal numbers, as low + step * code in fp32 gives them."""
+    d, group, n = 128, 32, 24
+    k, v = _rows(n, 2, d, 5, size), _rows(n, 2, d, 6, size)
+    k[:, :, 64:] *= 100
+    pool = _pool(3, 8, 2, d, group, 0)
+    slots = _i32(range(n))
+    dm.decomoe_paged_append_q4(k.to(DEV), v.to(DEV), slots, pool)
+    out = torch.empty(2, n, 2, d, dtype=torch.bfloat16, device=DEV)
+    dm.decomoe_paged_read_q4(slots, pool, out[0], out[1])
+    for got, ref in zip(out, O.q4_values(pool.cpu().numpy(), d, group)[:2]):
+        # low + step * code in one rounding to fp32, then to bf16
+        ref = ref.reshape(n, 2, d).astype(np.float32).astype(np.float64)
+        assert np.array_equal(f64(got), O.bf16(ref))
+
+
 def test_slots_outside_the_pool_are_skipped_and_marked():
     d, group, n = 64, 64, 5
     k = _rows(n, 2, d, 5).to(DEV)
