@@ -790,7 +790,7 @@ DECOMOE_API int decomoe_w4_linear(const void* x, int x_dtype, int64_t x_stride, 
  * were; a token of V or more too, and it marks DECOMOE_ERR_BAD_INPUT. tokens NULL: all rows, no
  * logprob. logprob, entropy, top_id and top_logprob may each be NULL (not wanted; without the last
  * two n does not matter). fp32 throughout, each row in a fixed order: the same call gives the same
- * bits (the last ones go by T, V, the rows' alignment and the number of SMs). Logits of minus infinity have probability 0; a row of
+ * bits (the last ones go by T, V, n, the rows' alignment and the number of SMs). Logits of minus infinity have probability 0; a row of
  * nothing else gives -inf and an entropy of 0. NaN or +inf anywhere in a row make its
  * probabilities NaN; among alternatives NaN ranks as minus infinity. V <= 2^24, T <= (2^31 - 1) / 16. One launch, no
  * workspace, no host synchronisation; no output overlaps anything else.
