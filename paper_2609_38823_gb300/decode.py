@@ -102,10 +102,24 @@ class PagedCache:
             decomoe_paged_attention(q, self.k(layer), self.v(layer), self.table, self.seq_len, out, ws,
                                     hide_begin=self.hide_begin, hide_count=self.hide_count[layer], status=self.status)
 
-    def slots_of(self, request: int, rows: int) -> torch.Tensor:
-        """Slots of a request's first `rows` rows, in order."""
-        j = torch.arange(rows, dtype=torch.int32, device=self.table.device)
-        return self.table[request, j // self.page_size] * self.page_size + j % self.page_size
+    def slots_of(self, request: int, rows: int, layer: Optional[int] = None) -> torch.Tensor:
+        """Slots of a request's first `rows` rows, in order, without those that `layer` hides; with no
+        layer given nothing may be hidden among them. A row without a page is refused. Reads the
+        request's table and hidden block on the host, between steps."""
+        if not 0 <= rows <= self.table.shape[1] * self.page_size:
+            raise ValueError(f"a request has at most {self.table.shape[1] * self.page_size} rows, not {rows}")
+        begin = min(max(int(self.hide_begin[request]), 0), rows)
+        counts = self.hide_count[:, request] if layer is None else self.hide_count[layer, request].view(1)
+        count = min(max(int(counts.max()), 0), rows - begin)
+        if layer is None and count > 0:
+            raise ValueError("rows of this request are hidden: name the layer whose slots are wanted")
+        # from here on the attention's reading: rows [begin, begin + count) are not seen
+        j = torch.cat([torch.arange(begin), torch.arange(begin + count, rows)])
+        pages = self.table[request].cpu().long()[j // self.page_size]
+        none = (pages < 0) | (pages >= self.pool.shape[1])
+        if none.any():
+            raise ValueError(f"row {int(j[none][0])} of the request has no page")
+        return (pages * self.page_size + j % self.page_size).to(torch.int32).to(self.table.device)
 
     def attend_chunk(self, layer: int, q: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                      out: torch.Tensor, ws: torch.Tensor) -> None:
