@@ -124,11 +124,13 @@ class PagedCache:
     def attend_chunk(self, layer: int, q: torch.Tensor, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
                      out: torch.Tensor, ws: torch.Tensor) -> None:
         """A prompt's next chunk on a cache in 4 bits: q and out [n, Hq, D] of the last n of the
-        rows in `slots` [C] (stored already), which are read into k and v [C, Hkv, D] bf16 and
-        attended causally; ws as decomoe_attention has it."""
+        rows in `slots` [C] (stored already; ``slots_of`` the layer), which are read into k and v
+        [C, Hkv, D] bf16 and attended causally; ws as decomoe_attention has it. Every row counts, so a
+        slot outside the pool, -1 among them, marks DECOMOE_ERR_BAD_INPUT."""
         if self.bits != 4:
             raise ValueError("a chunk over the pages is for a cache in 4 bits")
-        decomoe_paged_read_q4(slots, self.pool[layer], k, v, status=self.status)
+        # (the read alone skips a slot of -1 without a mark, and would leave an old row to be attended)
+        decomoe_paged_read_q4(slots.masked_fill(slots < 0, -2), self.pool[layer], k, v, status=self.status)
         decomoe_attention(q, k, v, out, ws, status=self.status)
 
     def plan(self, fresh: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None) -> None:

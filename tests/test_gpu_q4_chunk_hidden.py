@@ -1,5 +1,5 @@
 """A prompt's chunk on a cache in 4 bits whose request hides a block: what one token's attention
-leaves out, the chunk's does too."""
+leaves out, the chunk's does too; rows without a slot are marked."""
 import numpy as np
 import pytest
 import torch
@@ -59,3 +59,17 @@ def test_chunk_leaves_the_hidden_block_out(begin, count):
     cache.attend(1, torch.stack([q[0], q[-1]]), one, dm.workspace(cache.workspace_bytes(2, HQ), DEV))
     assert_close_out(f64(one[1]), O.attention(f64(q[-1:]), flat[0][at[keep]], flat[1][at[keep]])[0], BF16_REL_L2, BF16_MAX_ABS, "one")
     assert dm.decomoe_read_status(cache.status) == dm.DECOMOE_OK
+
+
+@pytest.mark.parametrize("bad", [-1, -2, 20 * PS])
+def test_chunk_marks_rows_without_a_slot(bad):
+    cache = _cache()
+    C = N1 + N2
+    slots = cache.slots_of(1, C)
+    slots[40] = bad
+    q = _rows(N2, HQ, D, 3).to(DEV)
+    k, v = (torch.zeros(C, HKV, D, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ws = dm.workspace(dm.decomoe_attention_workspace_bytes(N2, C, HQ, HKV, D), DEV)
+    cache.attend_chunk(0, q, slots, k, v, torch.empty_like(q), ws)
+    assert dm.decomoe_read_status(cache.status) == dm.DECOMOE_ERR_BAD_INPUT
+    assert slots[40] == bad  # the caller's slots are left as they were
