@@ -3,7 +3,7 @@
 // 2, last step, with a cache of a quarter of the size).
 //
 // Bound: instructions and latency for long calls, launches for a decode batch. 16381 rows of 8 heads of 64: store
-// 13.0 us, 3.4 TB/s (its pool lies in L2), read 9.25 us, 4.8 TB/s; 5000 rows of 8 heads of 128 in groups of 32: 8.2 and
+// 13.4 us, 3.3 TB/s (its pool lies in L2), read 9.25 us, 4.8 TB/s; 5000 rows of 8 heads of 128 in groups of 32: 8.2 and
 // 5.7 us; 23 rows of 4 heads of 128: 2.3 and 1.7 us. The first store divided twice a value and found its row by 64-bit
 // division: 33 us; ties between two codes by exact remainders, in a branch that 40 % of the warps took: 18.5; values one
 // at a time instead of in packed pairs 13.5, the read 9.6.
@@ -88,6 +88,13 @@ __device__ __forceinline__ uint64_t q4_add(uint64_t a, uint64_t b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
   return r;
 }
+// Sums >= 0 cut off, but their last digit odd where something was cut off.
+__device__ __forceinline__ uint64_t q4_add_odd(uint64_t a, uint64_t b) {
+  uint64_t r, up;
+  asm("add.rz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  asm("add.rp.f32x2 %0, %1, %2;" : "=l"(up) : "l"(a), "l"(b));
+  return r | (up & 0x0000000100000001ull);  // (the two are neighbours where they differ: one of them is odd)
+}
 
 __device__ __forceinline__ uint32_t q4_max2(uint32_t a, uint32_t b) {  // of two pairs of bf16 numbers, NaN where one is
   uint32_t r;
@@ -118,21 +125,27 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint4& u, uint32_t* params
   float x[8];
   q4_unpack8(u, x);
   uint32_t code = 0;
+  // A place half way between two codes is (2 k + 1) step / 2, 13 digits at most. x - lo can need more than fp32's
+  // 24: cut off, with an odd last digit where something was lost, it lies on the same side of every such place, and
+  // on none; rounded to nearest it could fall on one. (An addition and two operations a pair: store and read of 16381 rows
+  // 21.6 -> 22.0 us.)
   if (small) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      code |= static_cast<uint32_t>(fminf(rintf(__fdiv_rn(x[j] - lo, step)), 15.f)) << (4 * j);
+    for (int j = 0; j < 8; ++j) {
+      const float r = __uint_as_float(__float_as_uint(__fsub_rz(x[j], lo)) | (__float_as_uint(__fsub_ru(x[j], lo)) & 1u));
+      code |= static_cast<uint32_t>(fminf(rintf(__fdiv_rn(r, step)), 15.f)) << (4 * j);
+    }
     return code;
   }
   // (x - lo) / step to nearest by the same correction, so that a value half way between two codes
-  // gives exactly that; adding 3 * 2^22 then rounds to the integer (ties to even), which stands in
+  // and no other gives exactly that; adding 3 * 2^22 then rounds to the integer (ties to even), which stands in
   // the low bits. The high ones leave the sum of all eight at once.
   constexpr float MAGIC = 12582912.f;
   constexpr uint32_t HIGH = 0x4b400000u;
   const float inv = __frcp_rn(step);
 #pragma unroll
   for (int j = 0; j < 8; j += 2) {
-    const uint64_t r = q4_add(q4_two(x[j], x[j + 1]), q4_two(-lo, -lo)), q = q4_mul(r, q4_two(inv, inv));
+    const uint64_t r = q4_add_odd(q4_two(x[j], x[j + 1]), q4_two(-lo, -lo)), q = q4_mul(r, q4_two(inv, inv));
     const uint64_t t = q4_add(q4_fma(q4_fma(q4_two(-step, -step), q, r), q4_two(inv, inv), q), q4_two(MAGIC, MAGIC));
     uint32_t t0, t1;
     q4_split(t, t0, t1);
