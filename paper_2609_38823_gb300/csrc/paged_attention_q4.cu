@@ -469,6 +469,11 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
 #pragma unroll
             for (int i2 = 0; i2 < 4; ++i2) sc[u][x][i2] = fmaf(bf16_lo(kp[i2 >> 1][g]), acc[x][i2], sc[u][x][i2]);
         }
+        // (before the mask: a factor next to nothing counts as 0, and minus infinity times that is NaN)
+#pragma unroll
+        for (int x = 0; x < NT; ++x)
+#pragma unroll
+          for (int i2 = 0; i2 < 4; ++i2) sc[u][x][i2] *= sl2[x][i2 & 1];
       }
       uint32_t vp[SUB][2][G];
 #pragma unroll
@@ -508,8 +513,6 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
         for (int i2 = 0; i2 < 2; ++i2) {
 #pragma unroll
           for (int u = 0; u < SUB; ++u) {
-            sc[u][x][i2] *= sl2[x][i2];
-            sc[u][x][i2 + 2] *= sl2[x][i2];
             const float y = fmaxf(sc[u][x][i2], sc[u][x][i2 + 2]);
             mx[x][i2] = u == 0 ? y : fmaxf(mx[x][i2], y);
           }
