@@ -717,7 +717,9 @@ DECOMOE_API int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t
  * arguments otherwise and the same readings of lengths, hidden rows, tables, status,
  * shares and bits. Keys and values are low + step * q, not rounded on the way; weights times steps
  * are rounded to fp16 for the value product (2^-11 of each, or 2^-26 of the largest step where a product is below
- * fp16's range); queries are exact but for values below 2^-27 of a head's largest; all else is fp32. A group
+ * fp16's range); queries are exact but for values below 2^-27 of a head's largest; all else is fp32. (The
+ * factor of a head's scores, scale times 2^24 times the power of two that brings its largest query to 2^14, counts
+ * as fp32's largest number where it is above that, from queries of 2^121 or so on.) A group
  * that reads back as NaN, or a query that is not finite, gives NaN in its own request and KV head. Rows that are hidden
  * or behind the last one may be loaded with those beside them; what they hold does not matter. ws:
  * decomoe_paged_attention_q4_workspace_bytes(...) bytes. A wait for a copy that runs past the

@@ -317,7 +317,10 @@ __global__ void __launch_bounds__(32 * q4a_warps(NT), 1) k_paged_attention_q4(Pa
           qf[x][i][3] = q4a_half2(v[i][3] * 0.0625f, v[i][7] * 0.0625f);
         }
         // what brings a score of these back (codes are 2^-24), and softmax's factor
-        const float back = 0x1p24f * a.sl2 * __uint_as_float((254u - up) << 23);
+        // (multiplied so that nothing on the way is larger or smaller than they and the result are; at most the largest
+        // number, or scores of 0 would be NaN: one key takes all the weight there)
+        const float unscale = __uint_as_float((254u - up) << 23);
+        const float back = fminf(up < 128u ? 0x1p24f * (a.sl2 * unscale) : a.sl2 * (0x1p24f * unscale), FLT_MAX);
 #pragma unroll
         for (int i = 0; i < 2; ++i) sl2[x][i] = __shfl_sync(0xffffffffu, back, 4 * (2 * c + i));
         // a group's sum (times 2^-24, as the codes) in three bf16 numbers, 24 bits: factors of low

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 import paper_2609_38823_gb300 as dm
+from oracle import decomoe_oracle as O
 from tests.helpers import f64
 from tests.test_gpu_paged_q4 import DEV, I32, _attend, _case, _ref
 
@@ -30,3 +31,30 @@ def test_a_scale_next_to_nothing(scale, group):
     ref, tol = _ref(q, pool, table, lens, group, hide, scale=scale)
     assert torch.isfinite(out).all()
     assert (np.abs(f64(out) - ref) <= tol).all()
+
+
+@pytest.mark.parametrize("group", [32, 64])
+@pytest.mark.parametrize("size", [2.0 ** 117, 2.0 ** 120, 2.0 ** 122])
+def test_queries_next_to_the_largest_number(size, group):
+    """Finite queries whose factor fp32 cannot hold: the key of the largest score takes all the weight."""
+    lens = [37, 200, 1]
+    q, pool, table = _case(lens, 8, 2, 128, group, 16, 22)
+    q = (q.double() * size).to(torch.bfloat16)
+    assert torch.isfinite(q).all()
+    out = f64(_attend(q.to(DEV), pool, table, lens))
+    assert np.isfinite(out).all()
+    q, (kd, vd, span, code) = f64(q), O.q4_values(pool.cpu().numpy(), 128, group)
+    seen = 0
+    for b, n in enumerate(lens):
+        at = (table[b, np.arange(n) // 16], np.arange(n) % 16)
+        for h in range(8):
+            k, v, vs = (x[at][:, h // 4] for x in (kd, vd, code))
+            s = k @ q[b, h]
+            best, size_of = int(s.argmax()), ((span[at][:, h // 4] + np.abs(k - span[at][:, h // 4])) @ np.abs(q[b, h])).max()
+            # (128 + 32) 2^-23: what a score is off by at most, of the sum of its terms
+            if n > 1 and s[best] - np.sort(s)[-2] <= 2 * 160 * 2.0 ** -23 * size_of:
+                continue
+            tol = 2.0 ** -8 * np.abs(v[best]) + 2.0 ** -11 * vs[best] + n * 2.0 ** -26 * vs.max() + 2.0 ** -20 * np.abs(v[best])
+            assert (np.abs(out[b, h] - v[best]) <= tol).all()
+            seen += 1
+    assert seen >= 20
