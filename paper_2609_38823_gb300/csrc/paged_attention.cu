@@ -409,10 +409,15 @@ int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t B, const vo
   a.info = reinterpret_cast<int4*>(a.part + static_cast<size_t>(grid) * 2 * piece);
   a.extra = PGA_EXTRA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
-  const size_t smem = static_cast<size_t>(PGA_WARPS) * PGA_STAGES * PGA_STAGE + 2 * (static_cast<size_t>(B) + 1) * sizeof(int);
+  auto smem = [](int64_t requests) {
+    return static_cast<size_t>(PGA_WARPS) * PGA_STAGES * PGA_STAGE + 2 * (static_cast<size_t>(requests) + 1) * sizeof(int);
+  };
   auto go = [&](auto main, auto join) -> int {
-    DM_CUDA_CHECK(cudaFuncSetAttribute(main, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    DM_CUDA_CHECK(launch_pdl(main, dim3(grid), dim3(PGA_THREADS), smem, s, a));
+    // the limit belongs to the kernel, not to the call: one for every batch, or a smaller one on another thread
+    // could lower it before this launch
+    DM_CUDA_CHECK(cudaFuncSetAttribute(main, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(smem(DECOMOE_MAX_REQUESTS))));
+    DM_CUDA_CHECK(launch_pdl(main, dim3(grid), dim3(PGA_THREADS), smem(B), s, a));
     DM_CUDA_CHECK(launch_pdl(join, dim3(grid), dim3(32 * PGM_WARPS), 0, s, static_cast<const PagedCommon&>(a)));
     return DECOMOE_OK;
   };

@@ -725,12 +725,17 @@ int decomoe_paged_attention_q4(const void* q, int64_t q_stride, int64_t B, const
   a.early = static_cast<float*>(ws);
   a.part = a.early + static_cast<size_t>(grid) * warps * piece;
   a.info = reinterpret_cast<int4*>(a.part + static_cast<size_t>(grid) * 2 * piece);
-  const size_t smem = static_cast<size_t>(warps) * Q4A_STAGES * Q4A_SETS * q4_tile_bytes(D, group) +
-                      2 * (static_cast<size_t>(B) + 1) * sizeof(int);
+  auto smem = [&](int64_t requests) {
+    return static_cast<size_t>(warps) * Q4A_STAGES * Q4A_SETS * q4_tile_bytes(D, group) +
+           2 * (static_cast<size_t>(requests) + 1) * sizeof(int);
+  };
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   auto go = [&](auto main, auto join) -> int {
-    DM_CUDA_CHECK(cudaFuncSetAttribute(main, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    DM_CUDA_CHECK(launch_pdl(main, dim3(grid), dim3(32 * warps), smem, s, a));
+    // the limit belongs to the kernel, not to the call: one for every batch, or a smaller one on another thread
+    // could lower it before this launch
+    DM_CUDA_CHECK(cudaFuncSetAttribute(main, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                       static_cast<int>(smem(DECOMOE_MAX_REQUESTS))));
+    DM_CUDA_CHECK(launch_pdl(main, dim3(grid), dim3(32 * warps), smem(B), s, a));
     DM_CUDA_CHECK(launch_pdl(join, dim3(grid), dim3(32 * PGM_WARPS), 0, s, static_cast<const PagedCommon&>(a)));
     return DECOMOE_OK;
   };
