@@ -249,9 +249,12 @@ class DecodeStep:
 class DecodeHead:
     """The end of a step: norm, vocabulary projection [V, d] in 4 bits as a (bytes, scales)
     pair, and what a server returns beside the tokens. Each call overwrites `logits` [B, V],
-    `logprob` and `entropy` [B] and, for n > 0, `top_id` and `top_logprob` [B, n]."""
+    `logprob` and `entropy` [B] and, for n > 0, `top_id` and `top_logprob` [B, n]. A token outside the
+    vocabulary marks `status` (one int32, its own if none is given) with DECOMOE_ERR_BAD_INPUT, and its
+    row's results are left as they were."""
 
-    def __init__(self, norm, w_vocab, B: int, n: int = 0, eps: float = 1e-6, dtype=torch.float32):
+    def __init__(self, norm, w_vocab, B: int, n: int = 0, eps: float = 1e-6, dtype=torch.float32,
+                 status: Optional[torch.Tensor] = None):
         w, scale = w_vocab
         V, d, dev = w.shape[0], 2 * w.shape[1], w.device
         f32 = dict(dtype=torch.float32, device=dev)
@@ -261,6 +264,7 @@ class DecodeHead:
         self.logprob, self.entropy = torch.zeros(B, **f32), torch.zeros(B, **f32)
         self.top_id = torch.zeros(B, n, dtype=torch.int32, device=dev) if n else None
         self.top_logprob = torch.zeros(B, n, **f32) if n else None
+        self.status = torch.zeros(1, dtype=torch.int32, device=dev) if status is None else status
 
     def __call__(self, h: torch.Tensor) -> torch.Tensor:
         """The logits of hidden states [B, d]."""
@@ -272,4 +276,4 @@ class DecodeHead:
         """Log probabilities of tokens [B] int32 (negative: a slot without one, left as it
         was), or without tokens each row's entropy and alternatives alone."""
         decomoe_token_logprobs(self.logits, tokens, None if tokens is None else self.logprob, self.entropy, self.top_id,
-                               self.top_logprob, scale=1.0 / temperature)
+                               self.top_logprob, scale=1.0 / temperature, status=self.status)
