@@ -668,8 +668,8 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
   DM_ARG_CHECK(V >= 1 && V <= (1 << 24), "token_logprobs: a vocabulary of 1 to 2^24 expected");
   DM_ARG_CHECK(row_stride >= V, "token_logprobs: row stride below the vocabulary's size");
   DM_ARG_CHECK(scale > 0.f && scale <= FLT_MAX, "token_logprobs: scale must be positive and finite");
-  DM_ARG_CHECK(n >= 0 && n <= LP_BEST && n <= V, "token_logprobs: 0 to %d alternatives, at most the vocabulary's size", LP_BEST);
-  DM_ARG_CHECK(n > 0 || (top_id == nullptr && top_logprob == nullptr), "token_logprobs: alternatives without a number of them");
+  if (top_id == nullptr && top_logprob == nullptr) n = 0;
+  else DM_ARG_CHECK(n >= 1 && n <= LP_BEST && n <= V, "token_logprobs: 1 to %d alternatives, at most the vocabulary's size", LP_BEST);
   DM_ARG_CHECK(logprob == nullptr || tokens != nullptr, "token_logprobs: log probabilities need tokens");
   if (T == 0) return DECOMOE_OK;
   const size_t e = dtype_bytes(dtype), rows = static_cast<size_t>(T);
@@ -693,7 +693,7 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
   a.T = T;
   a.ld = row_stride;
   a.V = static_cast<int>(V);
-  a.n = top_id != nullptr || top_logprob != nullptr ? n : 0;
+  a.n = n;
   a.scale = scale;
   a.c = scale * 1.4426950408889634f;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
