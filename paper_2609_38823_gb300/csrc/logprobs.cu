@@ -36,7 +36,7 @@ constexpr int LP_BEST = 32;
 constexpr int LP_ROOM = 512;  // collected elements of a block, or of a row
 constexpr int LP_CLUSTER = 8;  // blocks of a row, at most
 constexpr int LP_RESIDENT(int W) { return W == 4 ? 48 : 40; }  // warps of an SM, for blocks of W
-constexpr float LP_LN2 = 0.6931471805599453f;
+constexpr float LP_LN2 = 0.6931471805599453f, LP_LOG2E = 1.4426950408889634f;
 constexpr float LP_LEAST = -0x1p100f;  // what elements count as at least
 constexpr float LP_PLAIN = 0x1p97f;    // rows with a maximum below this in size are in the plain range
 
@@ -47,7 +47,8 @@ struct LpArgs {
   int32_t *top_id, *status;
   int64_t T, ld;
   int V, n;
-  float scale, c;  // scale, scale * log2(e)
+  float c;         // scale * log2(e)
+  float half, per; // (x - m) scale is (half x - half m) per: half is 1/2 where x - m may not fit fp32 but the product does
 };
 
 // ---------------------------------------------------------------- arithmetic
@@ -448,17 +449,19 @@ __device__ __forceinline__ float lp_from(uint32_t nth) {
 
 // ---------------------------------------------------------------- results
 
-// A row in every case, by one warp: infinities, NaN, nothing but masks, maxima of any size.
+// A row in every case, by one warp: infinities, NaN, nothing but masks, maxima and scales of any size.
 template <typename E>
-__device__ __noinline__ LpSums lp_any_case(const E* x, int V, float c) {
+__device__ __noinline__ LpSums lp_any_case(const E* x, int V, float half, float per) {
   const int lane = threadIdx.x & 31;
   float m = -INFINITY;
   for (int i = lane; i < V; i += 32) m = fmaxf(m, LpVec<E>::one(x + i));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  const float least = m == -INFINITY ? 0.f : half * m;
   float z = 0.f, w = 0.f;
   for (int i = lane; i < V; i += 32) {
-    const float d = (LpVec<E>::one(x + i) - (m == -INFINITY ? 0.f : m)) * c, e = lp_ex2(d);
+    // (c would be infinite for the largest scales)
+    const float d = (half * LpVec<E>::one(x + i) - least) * per * LP_LOG2E, e = lp_ex2(d);
     z += e;
     w = fmaf(e, fmaxf(d, -1000.f), w);
   }
@@ -476,11 +479,11 @@ __device__ __forceinline__ void lp_results(const LpArgs& a, int64_t row, const E
                                            uint64_t list) {
   const int lane = threadIdx.x & 31;
   const bool plain = fabsf(s.m) < LP_PLAIN && a.c < 0x1p20f && a.c > 0x1p-80f;
-  if (!plain) s = lp_any_case<E>(x, a.V, a.c);
+  if (!plain) s = lp_any_case<E>(x, a.V, a.half, a.per);
   const float lnz = logf(s.z);
   auto logprob = [&](float y) {
     // no probability anywhere (all logits minus infinity): -inf, and an entropy of 0
-    return s.z == 0.f ? -INFINITY : (y - s.m) * a.scale - lnz;
+    return s.z == 0.f ? -INFINITY : fmaf(a.half * y - a.half * s.m, a.per, -lnz);
   };
   if (lane == 0) {
     if (a.logprob != nullptr) a.logprob[row] = logprob(logit);
@@ -694,8 +697,9 @@ extern "C" int decomoe_token_logprobs(const void* logits, int64_t T, int64_t V, 
   a.ld = row_stride;
   a.V = static_cast<int>(V);
   a.n = n;
-  a.scale = scale;
-  a.c = scale * 1.4426950408889634f;
+  a.c = scale * LP_LOG2E;
+  a.half = scale < 1.f ? 0.5f : 1.f;
+  a.per = scale / a.half;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   const int64_t row_bytes = V * static_cast<int64_t>(e), sms = sm_count();
   auto go = [&](auto warp_rows, auto cluster, auto many) -> int {
