@@ -446,6 +446,30 @@ __device__ __forceinline__ float lp_from(uint32_t nth) {
   const float t = __uint_as_float(nth & 0x80000000u ? nth & 0x7fffffffu : ~nth);
   return nth != 0 && t > LP_LEAST ? t : -FLT_MAX;
 }
+// The same bound from the maxima of a block's threads, found by one warp in what lp_pass left: for rows whose plain elements
+// lie next to each other, of which few of the 64 groups see any.
+template <int W>
+__device__ __noinline__ float lp_from_threads(const float* slots, int runs, int n) {
+  const int lane = threadIdx.x & 31;
+  uint32_t x[W], least = 0xffffffffu, most = 0;
+#pragma unroll
+  for (int j = 0; j < W; ++j) {
+    float m = LP_LEAST;
+    for (int r = 0; r < runs; ++r) m = fmaxf(m, slots[(r * W + j) * 32 + lane]);
+    x[j] = lp_order(m) >> 16;
+    least = min(least, x[j]);
+    most = max(most, x[j]);
+  }
+  uint32_t at = __reduce_min_sync(0xffffffffu, least);
+  const uint32_t range = __reduce_max_sync(0xffffffffu, most) - at;
+  for (uint32_t step = range == 0 ? 0 : 1u << (31 - __clz(range)); step != 0; step >>= 1) {
+    int count = 0;
+#pragma unroll
+    for (int j = 0; j < W; ++j) count += __popc(__ballot_sync(0xffffffffu, x[j] >= at + step));
+    if (count >= n) at += step;
+  }
+  return lp_from(at << 16);
+}
 
 // ---------------------------------------------------------------- results
 
@@ -572,6 +596,7 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT(W) / W) k_logprobs_cluster
   __shared__ LpSums warp_sums[W];
   __shared__ __align__(16) float mine_max[64], maxima[64];  // of the block's groups, and of all
   __shared__ uint64_t rank_m[LP_CLUSTER], rank_zw[LP_CLUSTER];
+  __shared__ float rank_from[LP_CLUSTER];
   __shared__ int collected, who[W][64];
   __shared__ float slots[LP_SLOTS * THREADS];
   // (the warp's number as the compiler can see to be one for all lanes: 16384 rows 162 -> 155.5 us without alternatives)
@@ -617,7 +642,20 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT(W) / W) k_logprobs_cluster
       lp_cluster_arrive();
       lp_cluster_wait();
     }
-    const float from = lp_from(lp_nth(maxima[lane], maxima[lane + 32], a.n));
+    float from = lp_from(lp_nth(maxima[lane], maxima[lane + 32], a.n));
+    if (from == -FLT_MAX) {
+      // fewer than n groups see a plain element: the largest of the blocks' own bounds (24 rows of 151001 with 600 to 5000
+      // neighbours left, measured with events and a cold L2, 88 -> 20 us; with none masked 16: without a bound all of them
+      // were collected, and the slice that has them read once more by one warp)
+      from = lp_from_threads<W>(slots, runs.slots, a.n);
+      if (S > 1) {  // (all blocks of the cluster come here, with the same maxima)
+        if (tid < S) lp_store_at(smem_u32(&rank_from[rank]), tid, from);
+        __syncwarp();
+        lp_cluster_arrive();
+        lp_cluster_wait();
+        for (int i = 0; i < S; ++i) from = fmaxf(from, rank_from[i]);
+      }
+    }
     lp_collect<E>(row, from, runs, slots, warp * 32, THREADS, keys, &collected, who[warp]);
     __syncthreads();
     if (warp == 0) {
