@@ -76,11 +76,16 @@ class PagedCache:
         self.hide_count = torch.zeros(layers, requests, **i32)
         self.status = torch.zeros(1, **i32)
 
+    def _bf16(self, layer: int) -> torch.Tensor:
+        if self.bits != 16:
+            raise ValueError("a cache in 4 bits has one pool of bytes, pool[layer]")
+        return self.pool[layer]
+
     def k(self, layer: int) -> torch.Tensor:
-        return self.pool[layer, :, 0]
+        return self._bf16(layer)[:, 0]
 
     def v(self, layer: int) -> torch.Tensor:
-        return self.pool[layer, :, 1]
+        return self._bf16(layer)[:, 1]
 
     def append(self, layer: int, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor) -> None:
         """New rows [N, Hkv, D] of a layer into their slots."""

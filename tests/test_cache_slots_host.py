@@ -74,3 +74,12 @@ def test_rows_without_a_page_are_refused():
         assert c.slots_of(0, 16).tolist() == [_slot(c, 0, j) for j in range(16)]
         with pytest.raises(ValueError, match="page"):
             c.slots_of(0, 17)
+
+
+def test_a_cache_in_4_bits_has_no_bf16_pools():
+    c = _cache()
+    for f in (c.k, c.v):
+        with pytest.raises(ValueError, match="4 bits"):
+            f(0)
+    b = PagedCache(2, 1, pages=3, page_size=PS, max_pages=2, hkv=2, d=64, device="cpu")
+    assert b.k(1).shape == b.v(1).shape == (3, PS, 2, 64) and b.k(1).data_ptr() != b.v(1).data_ptr()
