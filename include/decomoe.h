@@ -697,7 +697,8 @@ DECOMOE_API int decomoe_paged_attention(const void* q, int64_t q_stride, int64_t
  * features 32 i + 8 c .. + 7, the 16-bit word r * (D / 32) + i of a row of value codes
  * features 32 i + 4 r .. + 3. D 64 with groups of 32 or 64, or D 128 with groups of 32, 64
  * or 128; page_size a power of two, 8 at least. The pool is 16-byte aligned; any content
- * will do at the start. decomoe_paged_q4_page_bytes: a page's bytes (0: no such shape).
+ * will do at the start. decomoe_paged_q4_page_bytes: a page's bytes (0: no such shape, or more
+ * than 1024 KV heads).
  *
  * decomoe_paged_append_q4: new rows into their slots, as decomoe_paged_append. k_new, v_new:
  * [N, Hkv, D] bf16, rows k_row_stride and v_row_stride elements apart (multiples of 8). Of

@@ -301,7 +301,7 @@ using namespace decomoe;
 extern "C" {
 
 size_t decomoe_paged_q4_page_bytes(int page_size, int Hkv, int D, int group) {
-  if (page_size < 8 || (page_size & (page_size - 1)) != 0 || Hkv < 1 || !q4_shape_ok(D, group)) return 0;
+  if (page_size < 8 || (page_size & (page_size - 1)) != 0 || Hkv < 1 || Hkv > 1024 || !q4_shape_ok(D, group)) return 0;
   return static_cast<size_t>(Hkv) * (page_size / 8) * q4_tile_bytes(D, group);
 }
 

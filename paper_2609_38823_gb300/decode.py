@@ -59,8 +59,8 @@ class PagedCache:
         elif bits == 4:
             size = decomoe_paged_q4_page_bytes(page_size, hkv, d, group)
             if size == 0:
-                raise ValueError("a cache in 4 bits has heads of 64 or 128, groups of 32, 64 or (heads of 128) 128, and "
-                                 "pages of a power of two of rows, 8 at least")
+                raise ValueError("a cache in 4 bits has at most 1024 heads of 64 or 128, groups of 32, 64 or (heads of 128) 128, "
+                                 "and pages of a power of two of rows, 8 at least")
             self.pool = torch.zeros(layers, pages, hkv, page_size // 8, size // (hkv * (page_size // 8)), dtype=torch.uint8,
                                     device=device)
         else:
