@@ -122,6 +122,7 @@ struct LpVec<__nv_bfloat16> {
   static __device__ __forceinline__ float element(const uint4& u, int j) {
     return j & 1 ? bf16_hi(word(u, j / 2)) : bf16_lo(word(u, j / 2));
   }
+  static __device__ __forceinline__ uint4 masked() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
   static __device__ __forceinline__ float one(const __nv_bfloat16* p) { return __bfloat162float(*p); }
 };
 template <>
@@ -140,6 +141,7 @@ struct LpVec<float> {
   static __device__ __forceinline__ uint64_t pair(const uint4& u, int i) {
     return i == 0 ? lp_pair(element(u, 0), element(u, 1)) : lp_pair(element(u, 2), element(u, 3));
   }
+  static __device__ __forceinline__ uint4 masked() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
 };
 
@@ -473,28 +475,53 @@ __device__ __noinline__ float lp_from_threads(const float* slots, int runs, int 
 
 // ---------------------------------------------------------------- results
 
-// A row in every case, by one warp: infinities, NaN, nothing but masks, maxima and scales of any size.
+// A row in every case, by one warp: infinities, NaN, nothing but masks, maxima and scales of any size. Where the
+// maximum is not finite it says all: minus infinity for nothing but masks, NaN or infinity for no probabilities.
+// A lane has four partial sums, and three loads on their way at a time (a fourth costs the kernels that call this their
+// registers: 16384 rows 182 -> 188 us). 24 rows of 151001 fp32, one of them empty, 65 us (element by element with one sum: 150).
 template <typename E>
 __device__ __noinline__ LpSums lp_any_case(const E* x, int V, float half, float per) {
+  using Vec = LpVec<E>;
   const int lane = threadIdx.x & 31;
-  float m = -INFINITY;
-  for (int i = lane; i < V; i += 32) m = fmaxf(m, LpVec<E>::one(x + i));
+  LpArgs whole;
+  whole.x = x;
+  whole.V = V;
+  whole.ld = 0;
+  const LpRow<E> row(whole, 0, 0, 1);
+  const float edge = lane < row.edges ? Vec::one(x + row.edge_at(lane)) : -INFINITY;
+  auto walk = [&](auto take) {
+    for (int v = lane; v < row.vecs; v += 3 * 32) {
+      uint4 u[3];
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-  const float least = m == -INFINITY ? 0.f : half * m;
-  float z = 0.f, w = 0.f;
-  for (int i = lane; i < V; i += 32) {
+      for (int i = 0; i < 3; ++i) u[i] = v + 32 * i < row.vecs ? __ldg(row.xv + v + 32 * i) : Vec::masked();
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int j = 0; j < Vec::N; ++j) take(j & 3, Vec::element(u[i], j));
+    }
+  };
+  float m = edge;
+  walk([&](int, float y) { m = lp_max_nan(m, y); });
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m = lp_max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (!(fabsf(m) <= FLT_MAX)) return {m, m == -INFINITY ? 0.f : NAN, 0.f};
+  float z[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](int j, float y) {
     // (c would be infinite for the largest scales)
-    const float d = (half * LpVec<E>::one(x + i) - least) * per * LP_LOG2E, e = lp_ex2(d);
-    z += e;
-    w = fmaf(e, fmaxf(d, -1000.f), w);
-  }
+    const float d = (half * y - half * m) * per * LP_LOG2E, e = lp_ex2(d);
+    z[j] += e;
+    w[j] = fmaf(e, fmaxf(d, -1000.f), w[j]);
+  };
+  add(0, edge);
+  walk(add);
+  z[0] = (z[0] + z[1]) + (z[2] + z[3]);
+  w[0] = (w[0] + w[1]) + (w[2] + w[3]);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    z += __shfl_xor_sync(0xffffffffu, z, o);
-    w += __shfl_xor_sync(0xffffffffu, w, o);
+    z[0] += __shfl_xor_sync(0xffffffffu, z[0], o);
+    w[0] += __shfl_xor_sync(0xffffffffu, w[0], o);
   }
-  return {m, z, w};
+  return {m, z[0], w[0]};
 }
 
 // A row's results, by a warp: s in every lane, the keys of the best in `list`.
