@@ -398,7 +398,6 @@ __device__ __noinline__ uint64_t lp_sorted(LpRow<E> row, int n) {
 
 // The n best of `count` collected keys (zeros are none), key i in lane i, by a warp. Those behind the last
 // are the row's first elements of minus infinity or NaN, which are not collected.
-template <typename E>
 __device__ __forceinline__ uint64_t lp_rank(const uint64_t* keys, int count, int n, uint64_t* best) {
   const int lane = threadIdx.x & 31;
   if (lane < n) best[lane] = 0;
@@ -419,8 +418,7 @@ __device__ __noinline__ uint64_t lp_fill(const E* x, int V, int n, uint64_t list
   int have = __popc(__ballot_sync(0xffffffffu, lane < n && list != 0));
   for (int i = 0; i < V && have < n; i += 32) {
     const uint32_t gone = __ballot_sync(0xffffffffu, i + lane < V && !(LpVec<E>::one(x + min(i + lane, V - 1)) >= -FLT_MAX));
-    const uint32_t left = gone;
-    for (uint32_t todo = left; todo != 0 && have < n; todo &= todo - 1, ++have)
+    for (uint32_t todo = gone; todo != 0 && have < n; todo &= todo - 1, ++have)
       if (lane == have) list = lp_key(-INFINITY, i + __ffs(todo) - 1);
   }
   return list;
@@ -526,7 +524,7 @@ __device__ __noinline__ LpSums lp_any_case(const E* x, int V, float half, float 
 
 // A row's results, by a warp: s in every lane, the keys of the best in `list`.
 template <typename E>
-__device__ __forceinline__ void lp_results(const LpArgs& a, int64_t row, const E* x, int token, float logit, LpSums s,
+__device__ __forceinline__ void lp_results(const LpArgs& a, int64_t row, const E* x, float logit, LpSums s,
                                            uint64_t list) {
   const int lane = threadIdx.x & 31;
   const bool plain = fabsf(s.m) < LP_PLAIN && a.c < 0x1p20f && a.c > 0x1p-80f;
@@ -586,9 +584,9 @@ __global__ void __launch_bounds__(LP_THREADS) k_logprobs_warp(LpArgs a) {
     __syncwarp();
     const uint32_t t = lp_nth(halves[0], halves[1], a.n);
     lp_collect<E>(row, lp_from(t), runs, slots[warp], 0, 32, keys[warp], &count[warp], who[warp]);
-    list = count[warp] <= LP_ROOM ? lp_rank<E>(keys[warp], count[warp], a.n, best[warp]) : lp_sorted<E>(row, a.n);
+    list = count[warp] <= LP_ROOM ? lp_rank(keys[warp], count[warp], a.n, best[warp]) : lp_sorted<E>(row, a.n);
   }
-  lp_results<E>(a, r, row.x, token, logit, lp_reduce<32>(lp_sums(acc), a.c), list);
+  lp_results<E>(a, r, row.x, logit, lp_reduce<32>(lp_sums(acc), a.c), list);
 }
 
 // ---------------------------------------------------------------- few long rows: a cluster each
@@ -687,7 +685,7 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT(W) / W) k_logprobs_cluster
     __syncthreads();
     if (warp == 0) {
       if (S > 1 && collected <= a.n) list = lane < collected ? keys[lane] : 0;  // the cluster's first block ranks them all
-      else list = collected <= LP_ROOM ? lp_rank<E>(keys, collected, a.n, best) : lp_sorted<E>(row, a.n);
+      else list = collected <= LP_ROOM ? lp_rank(keys, collected, a.n, best) : lp_sorted<E>(row, a.n);
     }
   }
   if (warp == 0) s = lp_reduce<W>(warp_sums[lane & (W - 1)], a.c);
@@ -713,14 +711,14 @@ __global__ void __launch_bounds__(32 * W, LP_RESIDENT(W) / W) k_logprobs_cluster
         count += __popc(some);
       }
       __syncwarp();
-      list = lp_rank<E>(keys, count, a.n, best);
+      list = lp_rank(keys, count, a.n, best);
     }
     auto hi = [](uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v >> 32)); };
     auto lo = [](uint64_t v) { return __uint_as_float(static_cast<uint32_t>(v)); };
     s = lane < S ? LpSums{lo(rank_m[lane]), hi(rank_zw[lane]), lo(rank_zw[lane])} : LpSums{LP_LEAST, 0.f, 0.f};
     s = lp_reduce<32>(s, a.c);
   }
-  if (warp == 0) lp_results<E>(a, r, row.x, token, logit, s, list);
+  if (warp == 0) lp_results<E>(a, r, row.x, logit, s, list);
 }
 
 }  // namespace decomoe
