@@ -29,8 +29,10 @@ namespace decomoe {
 // Bound: 96 requests of 2000 to 16385 rows (153 MB) 37 us, 4.2 TB/s: 4 us until the first copies are on their way
 // (lengths, their sum, search, tables), 24 us of copies at 6.3 TB/s, 2 us of joins in the blocks and 4 for the joining
 // launch. Of 590 instructions a tile 192 unpack codes on a pipe of
-// half rate and 34 are products, issue slots are 60 % busy. The bf16 cache takes 95 us. One request of 2049 rows
-// 10.2 us, all of it latency: 2.5 us to its first copies, 1 for them, 1.5 for a tile, 2 for the join in the block, 3
+// half rate and 34 are products, issue slots are 60 % busy. The bf16 cache takes 95 us. With groups of 32 (170 MB)
+// 43 us, of 128 (149 MB) 35: four groups cost four times the parameters' operations, and their 128 registers do not
+// hold all that is live (56 bytes stored and 100 loaded again; with 16 queries a tile 16). One request of 2049 rows
+// 10.0 us, all of it latency: 2.5 us to its first copies, 1 for them, 1.5 for a tile, 2 for the join in the block, 3
 // for the launch that joins blocks, each a stretch of code that runs once.
 // Steps: codes to bf16 numbers by shift, mask and subtraction, one copy per eight rows, 304
 // blocks of eight warps 74 us; (code - 8) / 64 by one multiply-add, tiles of 32 rows, maxima raised
@@ -43,10 +45,12 @@ constexpr int Q4A_STAGES = 2;    // tiles of a warp's ring (three: no faster)
 constexpr int Q4A_BLOCKS = 160;  // of a launch, at most
 constexpr int q4a_warps(int NT) { return NT == 1 ? 16 : 8; }  // of a block, one block per SM: as many as their registers allow
 // Warps of a block that get tiles where there are few: one request of 2049 rows over 33 blocks
-// of eight warps 10.2 us, over 17 of sixteen 11.0, over 130 of two (33 pieces a pair to join) 11.9.
+// of eight warps 10.2 us (now 10.0), over 17 of sixteen 11.0, over 130 of two (33 pieces a pair to join) 11.9.
 constexpr int Q4A_FEW = 8;
-// What a (request, KV head) pair costs beside its tiles, in tiles: 97 requests of 5 to 1553 rows
-// take 21.2 us with 1, 20.9 with 2, 21.2 with 3, 22.9 with 5.
+// What a (request, KV head) pair costs beside its tiles, in tiles. With 1, 2, 3, 4 and 5 of them: 97 requests of 5 to 1553
+// rows 20.5, 19.8, 20.0, 21.0 and 21.6 us, 200 of 5 to 600 21.1, 21.7, 22.5, 24.1 and 24.5; 96 of 2000 to 16385, 60 of up to
+// 3000, 30 of 8000 and fewer ones within 1 %. 2 would be up to 3 % sooner for short requests alone; it stays 3 since
+// the division decides the last bits of results.
 constexpr int Q4A_EXTRA = 3;
 
 // A tile: KEYS consecutive rows of a request from a multiple of KEYS on (so that eight rows

@@ -3,10 +3,10 @@
 // 2, last step, with a cache of a quarter of the size).
 //
 // Bound: instructions and latency for long calls, launches for a decode batch. 16381 rows of 8 heads of 64: store
-// 13.4 us, 3.3 TB/s (its pool lies in L2), read 9.25 us, 4.8 TB/s; 5000 rows of 8 heads of 128 in groups of 32: 8.2 and
-// 5.7 us; 23 rows of 4 heads of 128: 2.3 and 1.7 us. The first store divided twice a value and found its row by 64-bit
-// division: 33 us; ties between two codes by exact remainders, in a branch that 40 % of the warps took: 18.5; values one
-// at a time instead of in packed pairs 13.5, the read 9.6.
+// 13.2 us, 3.4 TB/s (its pool lies in L2), read 9.0 us, 4.9 TB/s; 5000 rows of 8 heads of 128 in groups of 32: 9.9 and
+// 6.5 us; 23 rows of 4 heads of 128: 2.1 and 1.5 us (in a graph, six sets of tensors in turn). Steps: the first store
+// divided twice a value and found its row by 64-bit division: 33 us; ties between two codes by exact remainders, in a
+// branch that 40 % of the warps took: 18.5; values one at a time instead of in packed pairs 13.5, the read 9.6.
 #include "paged_q4.cuh"
 
 namespace decomoe {
@@ -127,8 +127,8 @@ __device__ __forceinline__ uint32_t q4_quantise(const uint4& u, uint32_t* params
   uint32_t code = 0;
   // A place half way between two codes is (2 k + 1) step / 2, 13 digits at most. x - lo can need more than fp32's
   // 24: cut off, with an odd last digit where something was lost, it lies on the same side of every such place, and
-  // on none; rounded to nearest it could fall on one. (An addition and two operations a pair: store and read of 16381 rows
-  // 21.6 -> 22.0 us.)
+  // on none; rounded to nearest it could fall on one. (An addition and two operations a pair: 16381 rows 12.8 -> 13.2 us, 5000
+  // of 8 heads of 128 8.9 -> 9.9. Held to nine blocks an SM, as many as before, these take 13.4 and 9.3.)
   if (small) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -219,7 +219,7 @@ __device__ __forceinline__ uint4 q4_values8(uint32_t code, uint32_t params) {
 }
 
 // (sixteen blocks an SM, so 32 registers: with the 40 that it would take 9.8 us for 16381 rows, not 9.25. The store's 50
-// squeezed to 40 take 12.6 there, but 9.1, not 8.2, for 5000 rows of 8 heads of 128)
+// squeezed to 40 took 12.6 there, not 13.0, but 9.1, not 8.2, for 5000 rows of 8 heads of 128)
 template <int D, int G>
 __global__ void __launch_bounds__(Q4_THREADS, 16) k_paged_read_q4(Q4Rows a, __nv_bfloat16* k, __nv_bfloat16* v) {
   using L = Q4Lane<D, G>;
